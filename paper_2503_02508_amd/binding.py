@@ -14,6 +14,8 @@ __all__ = [
     "LIB_PATH", "WS", "KERNEL_CLASSES",
     "qc_tap_workspace_bytes", "qc_tap_similarity", "qc_tap_normalise", "qc_tap_embed", "qc_tap_kmeans",
     "qc_tap_aggregate", "qc_tap_cluster", "qc_tap_profile_begin", "qc_tap_profile_end",
+    "W4Weight", "QC_ACT_SILU", "QC_ACT_GELU", "qc_w4_quantize", "qc_w4_expand", "qc_w4_linear", "qc_w4_gated",
+    "qc_w4_linear_grad", "qc_w4_gated_grad",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libqc.so")
@@ -27,7 +29,9 @@ QC_CACHE_ATTN, QC_CACHE_MLP = 0, 1
 SITES = ("ada", "qkv", "proj", "fc1", "fc2")
 WS = {"tokens": 0, "qact_ln": 1, "qact_attn": 2, "qact_mlp": 3, "qkv": 4, "mod": 5, "cond": 6, "eps": 7, "qkv_heads": 8}
 
-vp, i32, f32, f64, sz = C.c_void_p, C.c_int, C.c_float, C.c_double, C.c_size_t
+QC_ACT_SILU, QC_ACT_GELU = 0, 1
+
+vp, i32, i64, f32, f64, sz = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_double, C.c_size_t
 
 
 class ModelDesc(C.Structure):
@@ -45,6 +49,11 @@ class Weights(C.Structure):
                                   "fada_w", "fada_b", "flin_w", "flin_b")] + [("blocks", C.POINTER(BlockWeights))]
 
 
+class W4WeightDesc(C.Structure):
+    _fields_ = [("q", vp), ("scale", vp), ("zero", vp), ("sum", vp), ("N", C.c_int32), ("K", C.c_int32), ("group", C.c_int32)]
+
+
+_W4 = C.POINTER(W4WeightDesc)
 _SIGS = {
     "qc_last_error": (C.c_char_p, []),
     "qc_arena_bytes": (i32, [C.POINTER(ModelDesc), i32, C.POINTER(sz)]),
@@ -85,6 +94,12 @@ _SIGS = {
     "qc_tap_cluster": (i32, [vp, vp, i32, i32, vp, i32, i32, f32, i32, i32, i32, vp, vp, i32, vp, vp, vp, sz, vp]),
     "qc_tap_profile_begin": (i32, []),
     "qc_tap_profile_end": (i32, [C.POINTER(f32), C.POINTER(i32)]),
+    "qc_w4_quantize": (i32, [vp, i32, i64, _W4, vp]),
+    "qc_w4_expand": (i32, [_W4, vp, i32, i64, vp]),
+    "qc_w4_linear": (i32, [vp, i32, i64, f32, i32, _W4, vp, i32, vp, i64, vp]),
+    "qc_w4_gated": (i32, [vp, i32, i64, f32, i32, _W4, _W4, vp, vp, i32, i32, vp, i64, vp]),
+    "qc_w4_linear_grad": (i32, [vp, i32, i64, _W4, vp, i64, _W4, i32, vp, i64, vp]),
+    "qc_w4_gated_grad": (i32, [vp, i32, i64, _W4, _W4, vp, vp, i32, vp, i64, i32, vp, vp, i64, vp]),
     "qc_profile_begin": (i32, [vp]),
     "qc_profile_end": (i32, [vp, i32, C.POINTER(C.c_int32), C.POINTER(f32), vp]),
 }
@@ -208,6 +223,128 @@ def qc_tap_profile_end():
     ms, n = f32(0), i32(0)
     _chk(lib.qc_tap_profile_end(C.byref(ms), C.byref(n)))
     return ms.value, n.value
+
+
+# ------------------------------------------------ 4-bit weights with a scale per group (include/qc_w4.h)
+class W4Weight:
+    """A quantised weight [N, K]: q uint8 [N, K/2], scale float32 [N, G], zero uint8 [N, G] or None, sum float32 [N] or None
+    (G = ceil(K / group)), all contiguous CUDA tensors.  Keeps them and the structure that the calls take."""
+
+    def __init__(self, q, scale, group, zero=None, sum=None):  # noqa: A002
+        import torch
+        N, K = q.shape[0], 2 * q.shape[1]
+        G = -(-K // group) if group > 0 else 0
+        for t, dtype, shape in ((q, torch.uint8, (N, K // 2)), (scale, torch.float32, (N, G)), (zero, torch.uint8, (N, G)),
+                                (sum, torch.float32, (N,))):
+            if t is not None and (t.dtype is not dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != q.device):
+                raise QCError(-2, "W4Weight: a tensor of type %s and shape %s is needed" % (dtype, shape))
+        self.q, self.scale, self.zero, self.sum = q, scale, zero, sum
+        self.N, self.K, self.group, self.device = N, K, group, q.device
+        self.desc = W4WeightDesc(_p(q), _p(scale), _p(zero), _p(sum), N, K, group)
+        self.ref = C.pointer(self.desc)
+
+    @classmethod
+    def empty(cls, N, K, group, asymmetric=False, device="cuda"):
+        """Buffers for qc_w4_quantize."""
+        import torch
+        G = -(-K // group)
+        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
+        return cls(new(N, K // 2, dtype=torch.uint8), new(N, G), group, new(N, G, dtype=torch.uint8) if asymmetric else None, new(N))
+
+
+_w4_types = {}
+
+
+def _w4_type(t):
+    if not _w4_types:
+        import torch
+        _w4_types.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 3})
+    code = _w4_types.get(t.dtype)
+    if code is None:
+        raise QCError(-7, "tensors of type %s are not supported" % t.dtype)
+    return code
+
+
+def _w4_rows(t, rows, cols, dtype, device, name):
+    """Leading dimension of a [rows, cols] tensor whose rows are contiguous."""
+    if t.dtype is not dtype or t.device != device:
+        raise QCError(-2, "%s: %s on %s, not %s on %s" % (name, t.dtype, t.device, dtype, device))
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (t.stride(1) != 1 and cols > 1):
+        raise QCError(-2, "%s: shape %s, strides %s; [%d, %d] with contiguous rows is needed" % (name, tuple(t.shape), t.stride(), rows, cols))
+    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+
+def _w4_bias(b, w):
+    if b is not None and (b.dtype is not w.scale.dtype or b.shape != (w.N,) or not b.is_contiguous() or b.device != w.device):
+        raise QCError(-2, "a bias is a contiguous float32 vector of %d elements on the weight's device" % w.N)
+    return _p(b)
+
+
+def _w4_stream(w):
+    import torch
+    dev = torch.cuda.current_device() if w.device.type == "cuda" else -1
+    if w.device.index != dev:
+        raise QCError(-2, "the weight lies on %s, which is not the current GPU" % w.device)
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def qc_w4_quantize(w, out):
+    """w [N, K] float32 / float16 / bfloat16 into the buffers of `out` (W4Weight.empty)."""
+    ld = _w4_rows(w, out.N, out.K, w.dtype, out.device, "w")
+    _chk(lib.qc_w4_quantize(_p(w), _w4_type(w), ld, out.ref, _w4_stream(out)))
+
+
+def qc_w4_expand(w, out):
+    ld = _w4_rows(out, w.N, w.K, out.dtype, w.device, "out")
+    _chk(lib.qc_w4_expand(w.ref, _p(out), _w4_type(out), ld, _w4_stream(w)))
+
+
+def qc_w4_linear(x, w, y, bias=None, x_scale=1.0, x_zp=128):
+    """y = x w^T + bias; x [M, K] float32 / float16 / bfloat16, or int8 codes with x_scale and x_zp (y float32)."""
+    t = _w4_type(x)
+    M = x.shape[0]
+    ldx = _w4_rows(x, M, w.K, x.dtype, w.device, "x")
+    ldy = _w4_rows(y, M, w.N, x.dtype if t != 3 else w.scale.dtype, w.device, "y")
+    _chk(lib.qc_w4_linear(_p(x), t, ldx, x_scale, x_zp, w.ref, _w4_bias(bias, w), M, _p(y), ldy, _w4_stream(w)))
+
+
+def qc_w4_gated(x, gate, up, h, act=QC_ACT_SILU, gate_bias=None, up_bias=None, x_scale=1.0, x_zp=128):
+    """h = act(x gate^T + gate_bias) * (x up^T + up_bias)."""
+    t = _w4_type(x)
+    M = x.shape[0]
+    ldx = _w4_rows(x, M, gate.K, x.dtype, gate.device, "x")
+    ldh = _w4_rows(h, M, gate.N, x.dtype if t != 3 else gate.scale.dtype, gate.device, "h")
+    if up.device != gate.device:
+        raise QCError(-2, "the weights lie on different devices")
+    _chk(lib.qc_w4_gated(_p(x), t, ldx, x_scale, x_zp, gate.ref, up.ref, _w4_bias(gate_bias, gate), _w4_bias(up_bias, up), act, M,
+                         _p(h), ldh, _w4_stream(gate)))
+
+
+def qc_w4_linear_grad(dy, w, dx, dy2=None, w2=None):
+    """dx = dy w (+ dy2 w2)."""
+    M = dy.shape[0]
+    ld = _w4_rows(dy, M, w.N, dy.dtype, w.device, "dy")
+    if (dy2 is None) != (w2 is None):
+        raise QCError(-1, "dy2 and w2 belong together")
+    ld2 = 0 if w2 is None else _w4_rows(dy2, M, w2.N, dy.dtype, w.device, "dy2")
+    if w2 is not None and w2.device != w.device:
+        raise QCError(-2, "the weights lie on different devices")
+    lddx = _w4_rows(dx, M, w.K, dy.dtype, w.device, "dx")
+    _chk(lib.qc_w4_linear_grad(_p(dy), _w4_type(dy), ld, w.ref, _p(dy2), ld2, None if w2 is None else w2.ref, M, _p(dx), lddx, _w4_stream(w)))
+
+
+def qc_w4_gated_grad(x, gate, up, dh, dgate, dup, act=QC_ACT_SILU, gate_bias=None, up_bias=None):
+    """dgate, dup: gradients of x gate^T + gate_bias and x up^T + up_bias, from dh."""
+    M = x.shape[0]
+    ldx = _w4_rows(x, M, gate.K, x.dtype, gate.device, "x")
+    lddh = _w4_rows(dh, M, gate.N, x.dtype, gate.device, "dh")
+    ldd = _w4_rows(dgate, M, gate.N, x.dtype, gate.device, "dgate")
+    if _w4_rows(dup, M, gate.N, x.dtype, gate.device, "dup") != ldd:
+        raise QCError(-2, "dgate and dup have different row strides")
+    if up.device != gate.device:
+        raise QCError(-2, "the weights lie on different devices")
+    _chk(lib.qc_w4_gated_grad(_p(x), _w4_type(x), ldx, gate.ref, up.ref, _w4_bias(gate_bias, gate), _w4_bias(up_bias, up), act, _p(dh), lddh, M,
+                              _p(dgate), _p(dup), ldd, _w4_stream(gate)))
 
 
 def qc_ddim_schedule(steps: int):

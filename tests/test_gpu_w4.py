@@ -1,0 +1,449 @@
+"""Operators on 4-bit weights with a scale per group (include/qc_w4.h) against the float64 oracle.
+
+Tolerances, derived from the arithmetic (e = 2^-24, half a float32 step; h = half a step of the result's type, absolute below its
+normal numbers):
+  a product sum of K terms: codes are exact in every type; sums run over at most 128 products of a group, then over the
+      groups (K / 32 at most), wavefronts and slices (32 at most), each addition and scaling off by e of a magnitude that the sum
+      of |x| |w| bounds:  (200 + K / 16) e S,  S = sum |x| |w| + |b|;  codes: S = x_scale (sum |c| |w| + |zp| |sum w|) + |b|
+  float16 and bfloat16 gradients of inputs: every weight rounded to the type, hw sum |dy| (half a step of float16's subnormal
+      numbers, 2^-25, for each weight besides), and sums of N terms as above with N / 4 in the place of K / 16
+  the gated block: with dv, du those of its two sums, |act'| <= 1.13, |act''| <= 1, the activation and its derivative evaluated
+      to 16 e of their largest intermediate (1 + |v|)."""
+import numpy as np
+import pytest
+
+from oracle import w4 as O
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+HALF = {"f32": E, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 0.0, "f16": 2.0 ** -25, "bf16": 0.0}
+
+
+@pytest.fixture(scope="module")
+def qc():
+    import paper_2503_02508_amd as m
+    return m
+
+
+def _type(name):
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "i8": torch.int8}[name]
+
+
+def _out(name):
+    return "f32" if name == "i8" else name
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+class Weight:
+    """Random quantised weights: the oracle's matrix and the framework's handle."""
+
+    def __init__(self, qc, rng, N, K, group, asym, scale=1.0):
+        import torch
+        w = (rng.standard_normal((N, K)) * scale / np.sqrt(K) * rng.uniform(0.5, 1.5, (N, 1))).astype(np.float32)
+        u, s, z = O.group_quant(w, group, asym)
+        self.v = O.values(u, s, z, group)
+        dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+        self.sum = self.v.sum(1).astype(np.float32)
+        self.h = qc.W4Weight(dev(O.pack(u)), dev(s), group, dev(z.astype(np.uint8)) if asym else None, dev(self.sum))
+
+
+def _strided(rows, cols, dtype, pad, fill=None, offset=0):
+    """[rows, cols] inside a larger buffer of known contents, and that buffer."""
+    import torch
+    buf = torch.full((rows + 2, cols + pad), 77 if dtype == torch.int8 else 777.0, dtype=dtype, device="cuda")
+    t = buf[1:1 + rows, offset:offset + cols]
+    if fill is not None:
+        t.copy_(fill)
+    return t, buf
+
+
+def _untouched(t, buf):
+    """Everything of the buffer but the tensor's own rows and columns."""
+    b = buf.clone()
+    r, c = t.shape
+    o = (t.data_ptr() - buf.data_ptr()) // t.element_size() - buf.stride(0)
+    b[1:1 + r, o:o + c] = 777.0
+    return bool((b == 777.0).all())
+
+
+def _inputs(rng, M, K, dtype, xpad):
+    import torch
+    if dtype == "i8":
+        x = torch.from_numpy(rng.integers(-128, 128, (M, K)).astype(np.int8)).cuda()
+        xs, zp = np.float32(0.0173), 117
+        xt, _ = _strided(M, K, torch.int8, 16 * xpad, x)
+        c = _np(x)
+        return xt, float(xs), zp, (c + 128 - zp) * np.float64(xs), np.abs(c) * np.float64(xs), abs(zp - 128) * np.float64(xs)
+    x = torch.from_numpy(rng.standard_normal((M, K)).astype(np.float32)).cuda().to(_type(dtype))
+    xt, _ = _strided(M, K, _type(dtype), 16 * xpad, x)
+    return xt, 1.0, 128, _np(x), np.abs(_np(x)), 0.0
+
+
+def _sum_tol(w, b, mag, zmag, K):
+    """Bound of the error of x W^T + b before it is rounded to the result's type."""
+    S = mag @ np.abs(w.v).T + zmag * np.abs(w.v.sum(1)) + (0 if b is None else np.abs(b))
+    return (200 + K / 16) * E * S
+
+
+def _check(got, want, tol, t, what):
+    got = _np(got)
+    lim = tol + HALF[t] * (np.abs(want) + tol) + TINY[t]
+    bad = ~(np.abs(got - want) <= lim)
+    assert not bad.any(), "%s: %d of %d, worst %g of its limit" % (what, bad.sum(), bad.size, np.nanmax(np.abs(got - want) / lim))
+
+
+# M, N, K: a single value; odd everything; a row; the last chunk and the last group cut; many rows
+SHAPES = [(1, 1, 16), (1, 17, 48), (2, 33, 144), (5, 100, 1168), (1, 700, 4608), (16, 48, 384), (17, 64, 272), (33, 31, 656), (64, 130, 1152),
+          (77, 257, 1040), (128, 128, 128), (129, 200, 912), (300, 384, 1152), (515, 261, 400), (1, 40, 14336)]
+
+
+# ---------------------------------------------------------------- quantiser
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("asym", [False, True])
+@pytest.mark.parametrize("N,K,group", [(1, 16, 32), (7, 48, 64), (37, 144, 32), (5, 272, 128), (64, 1152, 128), (9, 2064, 64), (3, 14336, 32)])
+def test_quantize_and_expand_bit_exact(qc, N, K, group, asym, dtype):
+    import torch
+    rng = np.random.default_rng(N + K + group)
+    w = rng.standard_normal((N, K)) * np.exp(rng.uniform(-8, 3, (N, 1)))
+    w[N // 2, : K // 2] = 0
+    w[:, -3:] *= 3
+    w[0, :16] = np.array([7, -3.5, 0.5, 1.5, 2.5, -0.5, -1.5, 6.5, -6.5, 5.5, 0, -0.0, 3.5, 4.5, -2.5, -7]) / 8       # halves
+    wt, _ = _strided(N, K, _type(dtype), 16, torch.from_numpy(w).to(_type(dtype)))
+    W = qc.W4Weight.empty(N, K, group, asym)
+    qc.qc_w4_quantize(wt, W)
+    u, s, z = O.group_quant(_np(wt), group, asym)
+    assert np.array_equal(O.unpack(W.q.cpu().numpy()), u)
+    assert np.array_equal(W.scale.cpu().numpy(), s)
+    if asym:
+        assert np.array_equal(W.zero.cpu().numpy(), z)
+    v = O.values(u, s, z, group)
+    # float64 sums of K terms, rounded once
+    assert (np.abs(_np(W.sum) - v.sum(1)) <= E * np.abs(v.sum(1)) + K * 2.0 ** -52 * np.abs(v).sum(1)).all()
+    for t in ("f32", "f16", "bf16"):
+        for pad in (0, 16, 3):
+            out, buf = _strided(N, K, _type(t), pad)
+            qc.qc_w4_expand(W, out)
+            # the product of a float32 scale and a small number, rounded to float32 and then to the type
+            want = torch.from_numpy(v).float().to(_type(t))
+            assert torch.equal(out.cpu(), want) and _untouched(out, buf)
+
+
+def test_quantize_extreme_groups(qc):
+    """A group too small for its step, one at the top of float32, one of equal values, and one of a single sign."""
+    import torch
+    w = np.zeros((5, 64), np.float32)
+    w[0, :3] = [1e-45, -1e-45, 0]
+    w[1, :4] = [3e38, -3e38, 1e38, 1e-30]
+    w[2] = -0.25
+    w[3] = np.linspace(0.5, 1.0, 64)
+    w[4] = -np.linspace(0.5, 1.0, 64)
+    for asym in (False, True):
+        if asym:
+            w[1] *= 0.4                    # h - l stays finite
+        W = qc.W4Weight.empty(5, 64, 32, asym)
+        qc.qc_w4_quantize(torch.from_numpy(w).cuda(), W)
+        u, s, z = O.group_quant(w, 32, asym)
+        assert np.array_equal(O.unpack(W.q.cpu().numpy()), u) and np.array_equal(W.scale.cpu().numpy(), s)
+
+
+# ---------------------------------------------------------------- linear
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16", "i8"])
+@pytest.mark.parametrize("group,asym", [(32, True), (64, False), (128, True), (128, False)])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_linear(qc, M, N, K, group, asym, dtype):
+    import torch
+    rng = np.random.default_rng(M * 7 + N * 3 + K + group + asym)
+    w = Weight(qc, rng, N, K, group, asym)
+    b = rng.standard_normal(N).astype(np.float32) if (M + N) % 3 else None
+    x, xs, zp, xv, mag, zmag = _inputs(rng, M, K, dtype, 1)
+    t = _out(dtype)
+    y, buf = _strided(M, N, _type(t), 5, offset=2)
+    qc.qc_w4_linear(x, w.h, y, bias=None if b is None else torch.from_numpy(b).cuda(), x_scale=xs, x_zp=zp)
+    _check(y, O.linear(xv, w.v, b), _sum_tol(w, b, mag, zmag, K), t, "y")
+    assert _untouched(y, buf)
+
+
+# ---------------------------------------------------------------- gated block
+def _gated_terms(x, xs, zp, xv, mag, zmag, g, u, bg, bu, K, act):
+    v, p = O.linear(xv, g.v, bg), O.linear(xv, u.v, bu)
+    a, d = O.act(act, v)
+    dv, dp = _sum_tol(g, bg, mag, zmag, K), _sum_tol(u, bu, mag, zmag, K)
+    da = 1.13 * dv + 16 * E * (1 + np.abs(v)) * np.abs(v)
+    dd = 1.0 * dv + 16 * E * (1 + np.abs(v))
+    return v, p, a, d, dv, dp, da, dd
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16", "i8"])
+@pytest.mark.parametrize("group,asym,act", [(32, False, "silu"), (64, True, "gelu"), (128, False, "gelu"), (128, True, "silu")])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_gated(qc, M, N, K, group, asym, act, dtype):
+    import torch
+    rng = np.random.default_rng(M * 5 + N * 11 + K + group)
+    g, u = Weight(qc, rng, N, K, group, asym, 2.0), Weight(qc, rng, N, K, group, asym)
+    bg, bu = rng.standard_normal(N).astype(np.float32), (rng.standard_normal(N).astype(np.float32) if N % 2 else None)
+    x, xs, zp, xv, mag, zmag = _inputs(rng, M, K, dtype, 0)
+    t = _out(dtype)
+    h, buf = _strided(M, N, _type(t), 3, offset=1)
+    dev = lambda v: None if v is None else torch.from_numpy(v).cuda()  # noqa: E731
+    qc.qc_w4_gated(x, g.h, u.h, h, {"silu": qc.QC_ACT_SILU, "gelu": qc.QC_ACT_GELU}[act], gate_bias=dev(bg), up_bias=dev(bu), x_scale=xs, x_zp=zp)
+    v, p, a, d, dv, dp, da, dd = _gated_terms(x, xs, zp, xv, mag, zmag, g, u, bg, bu, K, act)
+    _check(h, a * p, da * (np.abs(p) + dp) + np.abs(a) * dp + 4 * E * np.abs(a * p), t, "h")
+    assert _untouched(h, buf)
+
+
+# ---------------------------------------------------------------- gradients
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("group,asym,act", [(32, True, "gelu"), (64, False, "silu"), (128, True, "silu")])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_gated_grad(qc, M, N, K, group, asym, act, dtype):
+    import torch
+    rng = np.random.default_rng(M * 3 + N * 5 + K + group)
+    g, u = Weight(qc, rng, N, K, group, asym, 2.0), Weight(qc, rng, N, K, group, asym)
+    bg, bu = (rng.standard_normal(N).astype(np.float32) for _ in range(2))
+    x, xs, zp, xv, mag, zmag = _inputs(rng, M, K, dtype, 1)
+    dh, _ = _strided(M, N, _type(dtype), 7, torch.from_numpy(rng.standard_normal((M, N))).to(_type(dtype)), offset=3)
+    both, buf = _strided(M, 2 * N, _type(dtype), 5, offset=1)             # the two results side by side
+    dg, du = both[:, :N], both[:, N:]
+    qc.qc_w4_gated_grad(x, g.h, u.h, dh, dg, du, {"silu": 0, "gelu": 1}[act], gate_bias=torch.from_numpy(bg).cuda(), up_bias=torch.from_numpy(bu).cuda())
+    v, p, a, d, dv, dp, da, dd = _gated_terms(x, xs, zp, xv, mag, zmag, g, u, bg, bu, K, act)
+    z = np.abs(_np(dh))
+    _check(dg, _np(dh) * p * d, z * (dp * (np.abs(d) + dd) + np.abs(p) * dd + 4 * E * np.abs(p * d)), dtype, "dgate")
+    _check(du, _np(dh) * a, z * (da + 4 * E * np.abs(a)), dtype, "dup")
+    assert _untouched(both, buf)
+
+
+def _grad_tol(dy, w, t):
+    S = np.abs(dy) @ np.abs(w)
+    tol = (200 + w.shape[0] / 4) * E * S
+    if t != "f32":
+        tol = tol + HALF[t] * S * (1 + 2 * E) + TINY[t] * np.abs(dy).sum(1)[:, None]
+    return tol
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("group,asym", [(32, True), (64, False), (128, True), (128, False)])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_linear_grad(qc, M, N, K, group, asym, dtype):
+    import torch
+    rng = np.random.default_rng(M + N * 13 + K + group)
+    w = Weight(qc, rng, N, K, group, asym)
+    pair = (M + K // 16) % 2 == 0
+    dy, _ = _strided(M, N, _type(dtype), 3, torch.from_numpy(rng.standard_normal((M, N))).to(_type(dtype)), offset=1)
+    dx, buf = _strided(M, K, _type(dtype), 5, offset=3)
+    want, tol, kw = _np(dy) @ w.v, _grad_tol(_np(dy), w.v, dtype), {}
+    if pair:
+        N2 = 2 * N + 1
+        w2 = Weight(qc, rng, N2, K, group, asym)
+        dy2 = torch.from_numpy(rng.standard_normal((M, N2))).cuda().to(_type(dtype))
+        want, tol, kw = want + _np(dy2) @ w2.v, tol + _grad_tol(_np(dy2), w2.v, dtype), dict(dy2=dy2, w2=w2.h)
+    qc.qc_w4_linear_grad(dy, w.h, dx, **kw)
+    _check(dx, want, tol, dtype, "dx")
+    assert _untouched(dx, buf)
+
+
+def test_gradient_of_no_outputs_is_zero_and_empty_calls(qc):
+    import torch
+    W = qc.W4Weight.empty(0, 64, 32)
+    dx = torch.full((3, 64), 5.0, device="cuda")
+    qc.qc_w4_linear_grad(torch.empty((3, 0), device="cuda"), W, dx)
+    assert (dx == 0).all()
+    V = Weight(qc, np.random.default_rng(0), 8, 64, 32, False).h
+    for x, y in ((torch.empty((0, 64), device="cuda"), torch.empty((0, 8), device="cuda")),):
+        qc.qc_w4_linear(x, V, y)
+        qc.qc_w4_gated(x, V, V, y)
+        qc.qc_w4_linear_grad(y, V, x)
+        qc.qc_w4_gated_grad(x, V, V, y, y, torch.empty_like(y))
+    qc.qc_w4_linear(torch.ones((2, 64), device="cuda"), W, torch.empty((2, 0), device="cuda"))
+    qc.qc_w4_quantize(torch.empty((0, 64), device="cuda"), W)
+    qc.qc_w4_expand(W, torch.empty((0, 64), device="cuda"))
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M", [1, 20, 200])
+def test_rows_do_not_meet(qc, M, dtype):
+    """NaN and infinities in one row stay in that row, and in the columns of a weight row with an infinite scale."""
+    import torch
+    rng = np.random.default_rng(M)
+    w = Weight(qc, rng, 70, 272, 64, True)
+    x = torch.from_numpy(rng.standard_normal((M, 272)).astype(np.float32)).cuda().to(_type(dtype))
+    y = [torch.empty((M, 70), dtype=x.dtype, device="cuda") for _ in range(2)]
+    qc.qc_w4_linear(x, w.h, y[0])
+    r = M // 2
+    x[r, 5], x[r, 100] = float("nan"), float("inf")
+    qc.qc_w4_linear(x, w.h, y[1])
+    keep = torch.arange(M, device="cuda") != r
+    assert torch.isnan(y[1][r]).all() and torch.equal(y[0][keep], y[1][keep])
+    dx = [torch.empty((M, 272), dtype=x.dtype, device="cuda") for _ in range(2)]
+    qc.qc_w4_linear_grad(y[0], w.h, dx[0])
+    y[0][r, 3] = float("nan")
+    qc.qc_w4_linear_grad(y[0], w.h, dx[1])
+    assert torch.isnan(dx[1][r]).all() and torch.equal(dx[0][keep], dx[1][keep])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_values_and_single_terms(qc, dtype):
+    """One input of a row set: y is that weight times it, exactly rounded, over the whole exponent range; an infinite one gives signed infinities."""
+    import torch
+    rng = np.random.default_rng(5)
+    w = Weight(qc, rng, 64, 160, 32, False)
+    x = torch.zeros((40, 160), device="cuda")
+    val = np.concatenate([2.0 ** np.arange(-100, 100, 5.3)[:38], [np.inf, -np.inf]])
+    x[torch.arange(40), torch.arange(40) * 4] = torch.from_numpy(val).float().cuda()
+    x = x.to(_type(dtype))
+    y = torch.empty((40, 64), dtype=x.dtype, device="cuda")
+    qc.qc_w4_linear(x, w.h, y)
+    xv = _np(x)
+    for m in range(38):
+        want = xv[m, 4 * m] * w.v[:, 4 * m]
+        assert (np.abs(_np(y)[m] - want) <= (4 * E + HALF[dtype]) * np.abs(want)).all(), m
+    for m, s in ((38, 1), (39, -1)):
+        c = w.v[:, 4 * m]
+        got = _np(y)[m]
+        assert np.array_equal(got[c != 0], s * np.sign(c[c != 0]) * np.inf) and np.isnan(got[c == 0]).all()
+
+
+# ---------------------------------------------------------------- together
+def _block(qc, rng, D, H, group, asym):
+    return [Weight(qc, rng, H, D, group, asym), Weight(qc, rng, H, D, group, asym), Weight(qc, rng, D, H, group, asym)]
+
+
+def _feed_forward(qc, x, ws, bs, h, y):
+    qc.qc_w4_gated(x, ws[0].h, ws[1].h, h, qc.QC_ACT_SILU, gate_bias=bs[0], up_bias=bs[1])
+    qc.qc_w4_linear(h, ws[2].h, y, bias=bs[2])
+
+
+def _backward(qc, x, ws, bs, dy, dh, dg, du, dx):
+    qc.qc_w4_linear_grad(dy, ws[2].h, dh)
+    qc.qc_w4_gated_grad(x, ws[0].h, ws[1].h, dh, dg, du, qc.QC_ACT_SILU, gate_bias=bs[0], up_bias=bs[1])
+    qc.qc_w4_linear_grad(dg, ws[0].h, dx, dy2=du, w2=ws[1].h)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [1, 37, 256])
+def test_feed_forward_block_and_its_gradient(qc, M, dtype):
+    """Weights quantised on the GPU, the block forward and backward: against the oracle's chain, and the gradient in float32 against
+    differences of the block itself along random directions."""
+    import torch
+    D, H, group = 384, 1056, 64
+    rng = np.random.default_rng(M)
+    ws, bs = _block(qc, rng, D, H, group, True), [torch.from_numpy(0.1 * rng.standard_normal(n)).float().cuda() for n in (H, H, D)]
+    x = torch.from_numpy(rng.standard_normal((M, D))).cuda().to(_type(dtype))
+    new = lambda c: torch.empty((M, c), dtype=x.dtype, device="cuda")  # noqa: E731
+    h, y, dh, dg, du, dx = new(H), new(D), new(H), new(H), new(H), new(D)
+    dy = torch.from_numpy(rng.standard_normal((M, D))).cuda().to(x.dtype)
+    _feed_forward(qc, x, ws, bs, h, y)
+    _backward(qc, x, ws, bs, dy, dh, dg, du, dx)
+    b = [_np(v) for v in bs]
+    hv = O.gated(_np(x), ws[0].v, ws[1].v, b[0], b[1], "silu")
+    want_y = O.linear(hv, ws[2].v, b[2])
+    gg, gu = O.gated_grad(_np(x), ws[0].v, ws[1].v, b[0], b[1], "silu", _np(dy) @ ws[2].v)
+    want_dx = gg @ ws[0].v + gu @ ws[1].v
+    # relative to the norm: h, dh, dg, du and dx rounded to the type (independently: their relative errors of at most half a step add
+    # as norms do), the gradients' weights too; float32: sums of 1056 terms
+    for got, want, n in ((y, want_y, 3), (dx, want_dx, 8)):
+        err = np.linalg.norm(_np(got) - want) / np.linalg.norm(want)
+        assert err <= n * max(HALF[dtype], (200 + 1056 / 4) * E), err
+    if dtype == "f32":
+        for _ in range(3):
+            d = torch.from_numpy(rng.standard_normal((M, D))).float().cuda()
+            # central differences of the oracle's block (its own rounding is 2^-52): error t^2 / 6 of the third derivative
+            t = 1e-3
+            f = [(O.linear(O.gated(_np(x) + s * t * _np(d), ws[0].v, ws[1].v, b[0], b[1], "silu"), ws[2].v, b[2]) * _np(dy)).sum() for s in (1, -1)]
+            num, ana = (f[0] - f[1]) / (2 * t), (_np(dx) * _np(d)).sum()
+            assert abs(num - ana) <= 1e-4 * np.sqrt((_np(dx) ** 2).sum() * (_np(d) ** 2).sum())
+
+
+def test_codes_through_the_activation_quantiser(qc):
+    """x -> codes (qc_quantize_act) -> gated block -> codes -> linear, as a 4-bit-weight, 8-bit-activation block runs."""
+    import torch
+    rng = np.random.default_rng(3)
+    D, H, M = 384, 1536, 50
+    ws = _block(qc, rng, D, H, 128, False)
+    x = torch.from_numpy(rng.standard_normal((M, D))).float().cuda()
+    q, h, qh, y = (torch.empty(s, dtype=t, device="cuda") for s, t in (((M, D), torch.int8), ((M, H), torch.float32), ((M, H), torch.int8),
+                                                                     ((M, D), torch.float32)))
+    qc.qc_quantize_act(x, q, 0.03, 120)
+    qc.qc_w4_gated(q, ws[0].h, ws[1].h, h, x_scale=0.03, x_zp=120)
+    qc.qc_quantize_act(h, qh, 0.01, 100)
+    qc.qc_w4_linear(qh, ws[2].h, y, x_scale=0.01, x_zp=100)
+    xs, hs = np.float64(np.float32(0.03)), np.float64(np.float32(0.01))
+    xv = (_np(q) + 8) * xs
+    assert np.max(np.abs(_np(h) - O.gated(xv, ws[0].v, ws[1].v, None, None, "silu"))) <= 1e-4 * np.abs(_np(h)).max()
+    hv = (_np(qh) + 28) * hs
+    _check(y, O.linear(hv, ws[2].v), _sum_tol(ws[2], None, np.abs(_np(qh)) * hs, 28 * hs, H), "f32", "y")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16", "i8"])
+def test_row_of_a_channel_wise_weight_equals_the_row_quantised_linear(qc, dtype):
+    """One group a row and symmetric: the matrix of qc_quantize_weight with 4 bits."""
+    import torch
+    rng = np.random.default_rng(9)
+    N, K, M = 200, 128, 40
+    w = torch.from_numpy((rng.standard_normal((N, K)) * 0.05).astype(np.float32)).cuda()
+    qw, sc, ws = torch.empty((N, K // 2), dtype=torch.uint8, device="cuda"), torch.empty(N, device="cuda"), torch.empty(N, dtype=torch.int32, device="cuda")
+    qc.qc_quantize_weight(w, 4, qw, sc, ws)
+    W = qc.W4Weight.empty(N, K, 128)
+    qc.qc_w4_quantize(w, W)
+    assert torch.equal(W.q, qw) and torch.equal(W.scale[:, 0], sc)
+    if dtype == "i8":
+        x = torch.from_numpy(rng.integers(-128, 128, (M, K)).astype(np.int8)).cuda()
+        y = [torch.empty((M, N), device="cuda") for _ in range(2)]
+        qc.qc_w8a8_linear(x, qw, ws, sc, None, 0.02, 90, 4, y[0])
+        qc.qc_w4_linear(x, W, y[1], x_scale=0.02, x_zp=90)
+        assert (y[0] - y[1]).abs().max() <= 1e-5 * y[0].abs().max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "i8"])
+@pytest.mark.parametrize("M", [1, 40, 400])
+def test_streams_graphs_and_repeats(qc, M, dtype):
+    """Two calls at once on two streams, and a captured chain replayed with other work between: every result equals the eager one."""
+    import torch
+    rng = np.random.default_rng(M)
+    w, w2 = Weight(qc, rng, 320, 656, 64, True), Weight(qc, rng, 320, 656, 64, True)
+    x, xs, zp, *_ = _inputs(rng, M, 656, dtype, 0)
+    x = x.contiguous()
+    ot = _type(_out(dtype))
+
+    def chain(y, h, dx, dg, du):
+        qc.qc_w4_linear(x, w.h, y, x_scale=xs, x_zp=zp)
+        qc.qc_w4_gated(x, w.h, w2.h, h, x_scale=xs, x_zp=zp)
+        if dtype != "i8":
+            qc.qc_w4_gated_grad(x, w.h, w2.h, y, dg, du)
+            qc.qc_w4_linear_grad(dg, w.h, dx, dy2=du, w2=w2.h)
+
+    def buffers():
+        return [torch.full((M, c), 3.0, dtype=ot, device="cuda") for c in (320, 320, 656, 320, 320)]
+
+    eager = buffers()
+    chain(*eager)
+    torch.cuda.synchronize()
+    s = [torch.cuda.Stream() for _ in range(2)]
+    outs = [buffers() for _ in range(2)]
+    torch.cuda.synchronize()
+    for st, o in zip(s, outs):
+        with torch.cuda.stream(st):
+            chain(*o)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(a, b) for a, b in zip(o, eager))
+    got = buffers()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        chain(*got)
+    for i in range(4):
+        for t in got:
+            t.fill_(float(i))
+        if i % 2:
+            chain(*buffers())
+            torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        want = eager if dtype != "i8" else eager[:2]
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
