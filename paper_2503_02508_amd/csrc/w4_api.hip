@@ -94,6 +94,11 @@ W4Args args(const void *x, int type, int64_t ldx, float x_scale, int x_zp, const
   return a;
 }
 
+hipError_t launch(const W4Args &a, int type, int op, void *stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return w4_tile_pays(a, type, op) ? launch_w4_tile(a, type, op, st) : launch_w4_rows(a, type, op, st);
+}
+
 int result_type(int type) { return type == QC_TYPE_I8 ? QC_TYPE_F32 : type; }
 
 }  // namespace
@@ -128,7 +133,7 @@ int qc_w4_linear(const void *x, int type, int64_t ldx, float x_scale, int x_zp, 
   QC_TRY(check_rows(y, "y", ldy, M, w->N, result_type(type), bytes_of(result_type(type))));
   QC_TRY(check_bias(bias));
   if (M == 0 || w->N == 0) return QC_OK;
-  QC_HIP(launch_w4_rows(args(x, type, ldx, x_scale, x_zp, w, bias, M, y, ldy), type, W4_LINEAR, static_cast<hipStream_t>(stream)));
+  QC_HIP(launch(args(x, type, ldx, x_scale, x_zp, w, bias, M, y, ldy), type, W4_LINEAR, stream));
   return QC_OK;
 }
 
@@ -150,7 +155,7 @@ int qc_w4_gated(const void *x, int type, int64_t ldx, float x_scale, int x_zp, c
   W4Args a = args(x, type, ldx, x_scale, x_zp, gate, gate_bias, M, h, ldh);
   a.w[1] = mat(up, up_bias);
   a.act = act;
-  QC_HIP(launch_w4_rows(a, type, W4_GATED, static_cast<hipStream_t>(stream)));
+  QC_HIP(launch(a, type, W4_GATED, stream));
   return QC_OK;
 }
 
@@ -199,7 +204,7 @@ int qc_w4_gated_grad(const void *x, int type, int64_t ldx, const qc_w4_weight *g
   a.w[1] = mat(up, up_bias);
   a.act = act;
   a.dh = dh; a.lddh = lddh; a.y2 = dup;
-  QC_HIP(launch_w4_rows(a, type, W4_GATED_GRAD, static_cast<hipStream_t>(stream)));
+  QC_HIP(launch(a, type, W4_GATED_GRAD, stream));
   return QC_OK;
 }
 

@@ -54,6 +54,9 @@ struct W4GradArgs {
 // launchers (every argument checked by the host layer)
 hipError_t launch_w4_quantize(const void *w, int type, int64_t ld, const qc_w4_weight &out, hipStream_t st);
 hipError_t launch_w4_expand(const qc_w4_weight &w, void *out, int type, int64_t ld, hipStream_t st);
+// many rows: whether it pays, and the launch
+bool w4_tile_pays(const W4Args &a, int type, int op);
+hipError_t launch_w4_tile(const W4Args &a, int type, int op, hipStream_t st);
 hipError_t launch_w4_rows(const W4Args &a, int type, int op, hipStream_t st);
 hipError_t launch_w4_grad(const W4GradArgs &a, int type, hipStream_t st);
 
@@ -84,10 +87,137 @@ struct W4Mem<QC_TYPE_I8> : W4Mem<QC_TYPE_F32> {};
 // ---- codes.  The nibble at bits 0-3 as a signed number over 16; one instruction (v_cvt_off_f32_i4), exact.  The scales are
 // multiplied by 16 to match.
 __device__ __forceinline__ float w4_nibble(unsigned w) { return __builtin_amdgcn_cvt_off_f32_i4((int)w); }
+// all 8 of a word: the instruction reads any byte of a register, so that the odd ones cost one shift for all four
+__device__ __forceinline__ void w4_nibbles(unsigned w, float v[8]) {
+  unsigned odd = w >> 4;
+  asm("" : "+v"(odd));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = w4_nibble((w >> (8 * i)) & 0xFF);
+    v[2 * i + 1] = w4_nibble((odd >> (8 * i)) & 0xFF);
+  }
+}
 
 // the upper halves of two float32 words: exact for numbers of at most 8 significant bits
 __device__ __forceinline__ unsigned w4_pack_bf16(float lo, float hi) {
   return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, hi), __builtin_bit_cast(unsigned, lo), 0x07060302u);
+}
+
+// One type's operands of a product of 16 x 32 by 32 x 16: lane l holds 8 inputs 8 (l / 16) .. of row (column) l % 16, the result's
+// column l % 16 and rows 4 (l / 16) ..
+template <int TYPE>
+struct Frag;
+
+template <>
+struct Frag<QC_TYPE_BF16> {
+  using X = w4_bf8;
+  using W = w4_bf8;
+  using Acc = w4_f4;
+  template <bool ASYM>
+  static __device__ __forceinline__ W weights(unsigned w, float z16, unsigned) {
+    float v[8];
+    w4_nibbles(w, v);
+    w4_u4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = ASYM ? w4_pack_bf16(v[2 * i] - z16, v[2 * i + 1] - z16) : w4_pack_bf16(v[2 * i], v[2 * i + 1]);
+    return __builtin_bit_cast(W, r);
+  }
+  static __device__ __forceinline__ Acc mma(X x, W w, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w, c, 0, 0, 0); }
+};
+
+template <>
+struct Frag<QC_TYPE_F16> {
+  using X = w4_h8;
+  using W = w4_h8;
+  using Acc = w4_f4;
+  template <bool ASYM>
+  static __device__ __forceinline__ W weights(unsigned w, float z16, unsigned) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    const _Float16 z = (_Float16)z16;
+    float v[8];
+    w4_nibbles(w, v);
+    w4_u4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h2 p = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(v[2 * i], v[2 * i + 1]));
+      if (ASYM) p -= h2{z, z};
+      r[i] = __builtin_bit_cast(unsigned, p);
+    }
+    return __builtin_bit_cast(W, r);
+  }
+  static __device__ __forceinline__ Acc mma(X x, W w, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w, c, 0, 0, 0); }
+};
+
+template <>
+struct Frag<QC_TYPE_F32> {
+  using X = w4_f8;
+  using W = w4_f8;
+  using Acc = w4_f4;
+  template <bool ASYM>
+  static __device__ __forceinline__ W weights(unsigned w, float z16, unsigned) {
+    float v[8];
+    w4_nibbles(w, v);
+    W r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = ASYM ? v[i] - z16 : v[i];
+    return r;
+  }
+  // eight products of four inputs: i, i + 8, i + 16 and i + 24 of the 32
+  static __device__ __forceinline__ Acc mma(X x, W w, Acc c) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], w[i], c, 0, 0, 0);
+    return c;
+  }
+};
+
+template <>
+struct Frag<QC_TYPE_I8> {
+  using X = w4_u2;
+  using W = w4_u2;
+  using Acc = w4_i4;
+  // u - z in bytes: (u + 128) - z never borrows from its neighbour
+  template <bool ASYM>
+  static __device__ __forceinline__ W weights(unsigned w, float, unsigned zb) {
+    if (!ASYM) zb = 0x08080808u;
+    const unsigned even = (((w & 0x0F0F0F0Fu) ^ 0x88888888u) - zb) ^ 0x80808080u;
+    const unsigned odd = ((((w >> 4) & 0x0F0F0F0Fu) ^ 0x88888888u) - zb) ^ 0x80808080u;
+    W r;
+    r[0] = __builtin_amdgcn_perm(odd, even, 0x05010400u);
+    r[1] = __builtin_amdgcn_perm(odd, even, 0x07030602u);
+    return r;
+  }
+  static __device__ __forceinline__ Acc mma(X x, W w, Acc c) {
+    return __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, x), __builtin_bit_cast(long, w), c, 0, 0, 0);
+  }
+};
+
+// words of four lanes 16 apart: word j of row i of the wavefront (16 lanes) changes places with word i of row j
+__device__ __forceinline__ void w4_transpose(w4_u4 &v) {
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  u2 a = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+  u2 b = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+  u2 c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+  u2 d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+  v[0] = c[0];
+  v[1] = c[1];
+  v[2] = d[0];
+  v[3] = d[1];
+}
+
+// the first half of it: words 0 and 1 of the upper 32 lanes change places with words 2 and 3 of the lower
+__device__ __forceinline__ void w4_swap32(w4_u4 &v) {
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  const u2 a = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+  const u2 b = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+  v = w4_u4{a[0], b[0], a[1], b[1]};
+}
+
+// 16 bytes of a row of KB bytes at `at`; beyond the row's end: anything of the row (the inputs there count as zero)
+__device__ __forceinline__ w4_u4 w4_load16(const uint8_t *row, int at, int KB) {
+  if (at + 16 <= KB) return *(const w4_u4_a8 *)(row + at);
+  const int p = at + 8 <= KB ? at : KB - 8;
+  const w4_u2 v = *(const w4_u2 *)(row + p);
+  return w4_u4{v[0], v[1], v[0], v[1]};
 }
 
 // ---- activation and derivative of the gated block, in float32

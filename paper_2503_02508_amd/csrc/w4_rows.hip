@@ -9,99 +9,6 @@
 
 namespace qc {
 
-// One type's operands of a product of 16 x 32 by 32 x 16: lane l holds 8 inputs 8 (l / 16) .. of row (column) l % 16, the result's
-// column l % 16 and rows 4 (l / 16) ..
-template <int TYPE>
-struct Frag;
-
-template <>
-struct Frag<QC_TYPE_BF16> {
-  using X = w4_bf8;
-  using W = w4_bf8;
-  using Acc = w4_f4;
-  static __device__ __forceinline__ W weights(unsigned w, float z16, unsigned) {
-    w4_u4 r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = w4_pack_bf16(w4_nibble(w >> (8 * i)) - z16, w4_nibble(w >> (8 * i + 4)) - z16);
-    return __builtin_bit_cast(W, r);
-  }
-  static __device__ __forceinline__ Acc mma(X x, W w, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w, c, 0, 0, 0); }
-};
-
-template <>
-struct Frag<QC_TYPE_F16> {
-  using X = w4_h8;
-  using W = w4_h8;
-  using Acc = w4_f4;
-  static __device__ __forceinline__ W weights(unsigned w, float z16, unsigned) {
-    w4_u4 r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      r[i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(w4_nibble(w >> (8 * i)) - z16, w4_nibble(w >> (8 * i + 4)) - z16));
-    return __builtin_bit_cast(W, r);
-  }
-  static __device__ __forceinline__ Acc mma(X x, W w, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w, c, 0, 0, 0); }
-};
-
-template <>
-struct Frag<QC_TYPE_F32> {
-  using X = w4_f8;
-  using W = w4_f8;
-  using Acc = w4_f4;
-  static __device__ __forceinline__ W weights(unsigned w, float z16, unsigned) {
-    W r;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = w4_nibble(w >> (4 * i)) - z16;
-    return r;
-  }
-  // eight products of four inputs: i, i + 8, i + 16 and i + 24 of the 32
-  static __device__ __forceinline__ Acc mma(X x, W w, Acc c) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], w[i], c, 0, 0, 0);
-    return c;
-  }
-};
-
-template <>
-struct Frag<QC_TYPE_I8> {
-  using X = w4_u2;
-  using W = w4_u2;
-  using Acc = w4_i4;
-  // u - z in bytes: (u + 128) - z never borrows from its neighbour
-  static __device__ __forceinline__ W weights(unsigned w, float, unsigned zb) {
-    const unsigned even = (((w & 0x0F0F0F0Fu) ^ 0x88888888u) - zb) ^ 0x80808080u;
-    const unsigned odd = ((((w >> 4) & 0x0F0F0F0Fu) ^ 0x88888888u) - zb) ^ 0x80808080u;
-    W r;
-    r[0] = __builtin_amdgcn_perm(odd, even, 0x05010400u);
-    r[1] = __builtin_amdgcn_perm(odd, even, 0x07030602u);
-    return r;
-  }
-  static __device__ __forceinline__ Acc mma(X x, W w, Acc c) {
-    return __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, x), __builtin_bit_cast(long, w), c, 0, 0, 0);
-  }
-};
-
-// words of four lanes 16 apart: word j of row i of the wavefront (16 lanes) changes places with word i of row j
-__device__ __forceinline__ void w4_transpose(w4_u4 &v) {
-  typedef unsigned u2 __attribute__((ext_vector_type(2)));
-  u2 a = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
-  u2 b = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
-  u2 c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
-  u2 d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-  v[0] = c[0];
-  v[1] = c[1];
-  v[2] = d[0];
-  v[3] = d[1];
-}
-
-// 16 bytes of a row of KB bytes at `at`; beyond the row's end: anything of the row (the inputs there count as zero)
-__device__ __forceinline__ w4_u4 w4_load16(const uint8_t *row, int at, int KB) {
-  if (at + 16 <= KB) return *(const w4_u4_a8 *)(row + at);
-  const int p = at + 8 <= KB ? at : KB - 8;
-  const w4_u2 v = *(const w4_u2 *)(row + p);
-  return w4_u4{v[0], v[1], v[0], v[1]};
-}
-
 // GC: groups in a chunk of 128 inputs; MT: tiles of 16 rows
 template <int TYPE, int GC, int MT, int OP>
 __global__ __launch_bounds__(MT > 1 ? 512 : 1024) void w4_rows_kernel(W4Args a) {
@@ -159,7 +66,7 @@ __global__ __launch_bounds__(MT > 1 ? 512 : 1024) void w4_rows_kernel(W4Args a) 
         }
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          const typename F::W wf = F::weights(q[w][j], z16[w], zb[w]);
+          const typename F::W wf = F::template weights<true>(q[w][j], z16[w], zb[w]);
 #pragma unroll
           for (int i = 0; i < MT; ++i) acc[w][i] = F::mma(x[i], wf, acc[w][i]);
         }
