@@ -16,6 +16,9 @@ typedef unsigned w4_u4 __attribute__((ext_vector_type(4)));
 typedef unsigned w4_u2 __attribute__((ext_vector_type(2)));
 // rows of packed codes start at multiples of 8 bytes (K % 16 == 0)
 typedef w4_u4 w4_u4_a8 __attribute__((aligned(8)));
+// rows of gradients start at any element
+typedef w4_u4 w4_u4_a4 __attribute__((aligned(4)));
+typedef w4_u4 w4_u4_a2 __attribute__((aligned(2)));
 
 struct W4Mat {
   const uint8_t *q;
@@ -58,6 +61,8 @@ hipError_t launch_w4_expand(const qc_w4_weight &w, void *out, int type, int64_t 
 bool w4_tile_pays(const W4Args &a, int type, int op);
 hipError_t launch_w4_tile(const W4Args &a, int type, int op, hipStream_t st);
 hipError_t launch_w4_rows(const W4Args &a, int type, int op, hipStream_t st);
+bool w4_grad_tile_pays(const W4GradArgs &a, int type);
+hipError_t launch_w4_grad_tile(const W4GradArgs &a, int type, hipStream_t st);
 hipError_t launch_w4_grad(const W4GradArgs &a, int type, hipStream_t st);
 
 // ---- element types in memory
@@ -218,6 +223,27 @@ __device__ __forceinline__ w4_u4 w4_load16(const uint8_t *row, int at, int KB) {
   const int p = at + 8 <= KB ? at : KB - 8;
   const w4_u2 v = *(const w4_u2 *)(row + p);
   return w4_u4{v[0], v[1], v[0], v[1]};
+}
+
+// float32 as three bfloat16 numbers whose sum it is exactly: truncation leaves 8 bits of the 24 each time.  What does not
+// change when its upper half is taken away (infinities) leaves nothing.
+__device__ __forceinline__ void tile_split(float v, float p[3]) {
+  const float h = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v) & 0xFFFF0000u);
+  const float r = h == v ? 0.0f : v - h;
+  const float m = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, r) & 0xFFFF0000u);
+  p[0] = h;
+  p[1] = m;
+  p[2] = r - m;
+}
+
+// position of a launch's workgroup: the workgroups of one XCD (every eighth) take neighbouring tiles, groups of GM tile rows column by column
+__device__ __forceinline__ void tile_at(int id, int total, int tm, int tn, int GM, int &mi, int &ni) {
+  const int x = id & 7, q = total >> 3, r = total & 7;
+  int t = x * q + min(x, r) + (id >> 3);
+  const int per = GM * tn, g = t / per, rows = min(GM, tm - g * GM);
+  t -= g * per;
+  mi = g * GM + t % rows;
+  ni = t / rows;
 }
 
 // ---- activation and derivative of the gated block, in float32

@@ -21,17 +21,6 @@ __device__ __forceinline__ int tile_slot(int r, int u) {
   return TYPE == QC_TYPE_I8 ? r * 128 + ((u ^ ((r >> 1) & 7)) << 4) : r * 256 + ((u ^ (r & 15)) << 4);
 }
 
-// float32 as three bfloat16 numbers whose sum it is exactly: truncation leaves 8 bits of the 24 each time.  What does not
-// change when its upper half is taken away (infinities) leaves nothing.
-__device__ __forceinline__ void tile_split(float v, float p[3]) {
-  const float h = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v) & 0xFFFF0000u);
-  const float r = h == v ? 0.0f : v - h;
-  const float m = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, r) & 0xFFFF0000u);
-  p[0] = h;
-  p[1] = m;
-  p[2] = r - m;
-}
-
 // The matrix products' operands of float32 activations: bfloat16, three a product
 template <int TYPE>
 using TileFrag = Frag<TYPE == QC_TYPE_F32 ? QC_TYPE_BF16 : TYPE>;
@@ -86,16 +75,6 @@ template <int TYPE, int MI>
 constexpr int tile_buffer = 16 * MI * tile_row<TYPE> * tile_planes<TYPE>;
 template <int TYPE, int MI>
 constexpr int tile_lds = 2 * tile_buffer<TYPE, MI> > 4 * 16 * 68 * 4 ? 2 * tile_buffer<TYPE, MI> : 4 * 16 * 68 * 4;
-
-// position of a launch's workgroup: the workgroups of one XCD (every eighth) take neighbouring tiles, groups of GM tile rows column by column
-__device__ __forceinline__ void tile_at(int id, int total, int tm, int tn, int GM, int &mi, int &ni) {
-  const int x = id & 7, q = total >> 3, r = total & 7;
-  int t = x * q + min(x, r) + (id >> 3);
-  const int per = GM * tn, g = t / per, rows = min(GM, tm - g * GM);
-  t -= g * per;
-  mi = g * GM + t % rows;
-  ni = t / rows;
-}
 
 // UK: inputs whose weights a wavefront holds expanded, a group or half of one
 template <int TYPE, int GC, int MI, int OP, bool ASYM, int UK>
