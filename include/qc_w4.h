@@ -34,8 +34,9 @@
  * number of columns.  x rows, packed codes and the matrices given to
  * qc_w4_quantize start at multiples of 16 bytes (QC_ERR_ALIGN); results,
  * gradients of results and vectors need only the alignment of their elements.
- * Limits: M, N and K below 2^24, N * ceil(K / 32) below 2^31; M = 0 and N = 0
- * are valid and do nothing (the gradients of N = 0 outputs are zero).
+ * Limits: M below 2^24, N, K and leading dimensions below 2^22, M times a
+ * result's columns and N * ceil(K / 32) below 2^31; M = 0 and N = 0 are valid
+ * and do nothing (the gradients of N = 0 outputs are zero).
  */
 #ifndef QC_W4_H_
 #define QC_W4_H_

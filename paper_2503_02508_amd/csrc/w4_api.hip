@@ -25,7 +25,7 @@ using namespace qc;
 
 namespace {
 
-constexpr int LIMIT = 1 << 24;
+constexpr int LIMIT_M = 1 << 24, LIMIT = 1 << 22;     // rows; features and leading dimensions (32-bit offsets inside 128 rows)
 
 int bytes_of(int type) { return type == QC_TYPE_F32 ? 4 : type == QC_TYPE_I8 ? 1 : 2; }
 bool off_by(const void *p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes != 0; }
@@ -58,13 +58,13 @@ int check_pair(const qc_w4_weight *a, const qc_w4_weight *b, bool rows) {
 int check_rows(const void *p, const char *name, int64_t ld, int64_t rows, int64_t cols, int type, int align) {
   if (rows == 0 || cols == 0) return QC_OK;
   if (!p) QC_FAIL(QC_ERR_NULL, "%s is NULL", name);
-  if (ld < cols || ld >= (1ll << 40)) QC_FAIL(QC_ERR_SHAPE, "%s: leading dimension %lld of %lld columns", name, (long long)ld, (long long)cols);
+  if (ld < cols || ld >= LIMIT) QC_FAIL(QC_ERR_SHAPE, "%s: leading dimension %lld of %lld columns", name, (long long)ld, (long long)cols);
   if (off_by(p, align) || ld * bytes_of(type) % align) QC_FAIL(QC_ERR_ALIGN, "%s: rows must start at multiples of %d bytes", name, align);
   return QC_OK;
 }
 
 int check_rows_of_call(int M, int64_t cols) {
-  if (M < 0 || M >= LIMIT) QC_FAIL(QC_ERR_SHAPE, "M (%d) out of range", M);
+  if (M < 0 || M >= LIMIT_M) QC_FAIL(QC_ERR_SHAPE, "M (%d) out of range", M);
   if (M * cols >= (1ll << 31)) QC_FAIL(QC_ERR_UNSUPPORTED, "a result of %d x %lld is too large", M, (long long)cols);
   return QC_OK;
 }

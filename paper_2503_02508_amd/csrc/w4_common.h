@@ -59,6 +59,7 @@ hipError_t launch_w4_quantize(const void *w, int type, int64_t ld, const qc_w4_w
 hipError_t launch_w4_expand(const qc_w4_weight &w, void *out, int type, int64_t ld, hipStream_t st);
 // many rows: whether it pays, and the launch
 bool w4_tile_pays(const W4Args &a, int type, int op);
+int w4_tile_rows(const W4Args &a, int type);
 hipError_t launch_w4_tile(const W4Args &a, int type, int op, hipStream_t st);
 hipError_t launch_w4_rows(const W4Args &a, int type, int op, hipStream_t st);
 bool w4_grad_tile_pays(const W4GradArgs &a, int type);
@@ -154,28 +155,6 @@ struct Frag<QC_TYPE_F16> {
 };
 
 template <>
-struct Frag<QC_TYPE_F32> {
-  using X = w4_f8;
-  using W = w4_f8;
-  using Acc = w4_f4;
-  template <bool ASYM>
-  static __device__ __forceinline__ W weights(unsigned w, float z16, unsigned) {
-    float v[8];
-    w4_nibbles(w, v);
-    W r;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = ASYM ? v[i] - z16 : v[i];
-    return r;
-  }
-  // eight products of four inputs: i, i + 8, i + 16 and i + 24 of the 32
-  static __device__ __forceinline__ Acc mma(X x, W w, Acc c) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], w[i], c, 0, 0, 0);
-    return c;
-  }
-};
-
-template <>
 struct Frag<QC_TYPE_I8> {
   using X = w4_u2;
   using W = w4_u2;
@@ -227,7 +206,7 @@ __device__ __forceinline__ w4_u4 w4_load16(const uint8_t *row, int at, int KB) {
 
 // float32 as three bfloat16 numbers whose sum it is exactly: truncation leaves 8 bits of the 24 each time.  What does not
 // change when its upper half is taken away (infinities) leaves nothing.
-__device__ __forceinline__ void tile_split(float v, float p[3]) {
+__device__ __forceinline__ void w4_split(float v, float p[3]) {
   const float h = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v) & 0xFFFF0000u);
   const float r = h == v ? 0.0f : v - h;
   const float m = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, r) & 0xFFFF0000u);
@@ -235,6 +214,10 @@ __device__ __forceinline__ void tile_split(float v, float p[3]) {
   p[1] = m;
   p[2] = r - m;
 }
+
+// The matrix products' operands of float32 activations: bfloat16, three products for one
+template <int TYPE>
+using FragOf = Frag<TYPE == QC_TYPE_F32 ? QC_TYPE_BF16 : TYPE>;
 
 // position of a launch's workgroup: the workgroups of one XCD (every eighth) take neighbouring tiles, groups of GM tile rows column by column
 __device__ __forceinline__ void tile_at(int id, int total, int tm, int tn, int GM, int &mi, int &ni) {
@@ -246,18 +229,33 @@ __device__ __forceinline__ void tile_at(int id, int total, int tm, int tn, int G
   ni = t / rows;
 }
 
-// ---- activation and derivative of the gated block, in float32
+// ---- Loads through a buffer descriptor: `bytes` from p on; what lies beyond reads as zero, without a branch.  Offsets are 32 bits, so p is
+// the first byte of a workgroup's own rows.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t w4_buffer(const void *p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)min(max(bytes, (int64_t)0), (int64_t)0x7FFFFFFF), 0x00027000);
+}
+constexpr unsigned W4_NOWHERE = 0x80000000u;      // an offset beyond every buffer
+
+// ---- A wavefront's 16 weight rows, 64 bytes of each.  Sixteen neighbouring lanes are looked up together, a cache line a clock: loads
+// therefore give 4 neighbouring lanes one row's 64 bytes (4 lines for 16 lanes, not 16), and lanes then fetch what is theirs
+// from each other: lane l holds piece l / 16 of row l % 16 afterwards.
+__device__ __forceinline__ unsigned w4_pull(unsigned v, int from4) { return (unsigned)__builtin_amdgcn_ds_bpermute(from4, (int)v); }
+__device__ __forceinline__ int w4_from(int lane) { return ((lane & 15) * 4 + (lane >> 4)) * 4; }
+
+// ---- activation and derivative of the gated block, in float32.  Both are v times a logistic function, 1 / (1 + exp(-t)), from the
+// hardware's exponential and reciprocal: off by a few units in the last place, and exp2's argument by |t| of them.
+__device__ __forceinline__ float w4_logistic(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t * -1.4426950408889634f)); }
 __device__ __forceinline__ float w4_act(int act, float v, float &d) {
   if (act == QC_ACT_SILU) {
-    const float e = 1.0f / (1.0f + expf(-v));
+    const float e = w4_logistic(v);
     d = e * (1.0f + v * (1.0f - e));
     return v * e;
   }
-  // (1 + tanh(y)) / 2 as 1 / (1 + exp(-2 y)), which keeps its digits where it is small; |v| > 30 is 0 or 1 already
-  const float c0 = 0.7978845608028654f, c1 = 0.044715f;
+  // (1 + tanh(y)) / 2 = logistic(2 y), which keeps its digits where it is small; |v| > 30 is 0 or 1 already
+  const float c0 = 1.5957691216057308f, c1 = 0.044715f;
   const float b = fminf(fmaxf(v, -30.0f), 30.0f), b2 = b * b;
-  const float e = 1.0f / (1.0f + expf(-2.0f * c0 * (b + c1 * b * b2)));
-  d = e + 2.0f * c0 * b * (1.0f + 3.0f * c1 * b2) * (e * (1.0f - e));
+  const float e = w4_logistic(c0 * b * (1.0f + c1 * b2));
+  d = e + c0 * b * (1.0f + 3.0f * c1 * b2) * (e * (1.0f - e));
   return v * e;
 }
 

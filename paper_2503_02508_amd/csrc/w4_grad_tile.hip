@@ -1,7 +1,7 @@
 // Gradient of a linear layer's input through fixed 4-bit weights of groups, many rows: dx = dy W (+ dy2 W2).
 //
-// A workgroup makes 16 MI rows by 256 columns of dx, its four wavefronts side by side along the columns, 64 rows of W a step.  The step's
-// gradients, packed codes and scales go through LDS.  A lane expands, of 8 neighbouring rows of W, the 4 neighbouring columns it will hold
+// A workgroup makes 16 MI rows by 256 columns of dx.  Its two halves take every second step, 64 rows of W, and add their sums at the end; a
+// half's four wavefronts stand side by side along the columns.  A step's gradients, packed codes and scales go through LDS.  A lane expands, of 8 neighbouring rows of W, the 4 neighbouring columns it will hold
 // results of (nibble t of its two bytes belongs to product t); the scales vary along the summed axis, so a weight is scaled before it
 // enters a product.  float16 and bfloat16: it is rounded to the type.  float32: gradients and scaled weights are each the sum of
 // three bfloat16 numbers, and six of the nine products are formed (the others are below 2^-22 of the largest).
@@ -19,6 +19,8 @@ struct GradTile {
   static constexpr int W = GT_N * GT_WROW;
   static constexpr int S = 8 * GT_N * 8;                                 // (scale, offset) of up to 8 groups of columns
   static constexpr int BUF = DY + W + S;
+  // two halves with two buffers each; afterwards half of the sums of each half, on their way to the other
+  static constexpr int LDS = 4 * BUF > MI / 2 * 4 * 512 * 16 ? 4 * BUF : MI / 2 * 4 * 512 * 16;
   static constexpr int UR = GT_N * ES / 16, NU = 16 * MI * UR / 256;
 };
 
@@ -26,13 +28,14 @@ struct GradTile {
 __device__ __forceinline__ int gt_slot(int r, int u) { return r * 128 + ((u ^ ((r >> 1) & 7)) << 4); }
 
 template <int TYPE, int MI, bool ASYM>
-__global__ __launch_bounds__(256, 2) void w4_grad_tile_kernel(W4GradArgs a, int tm, int tk) {
+__global__ __launch_bounds__(512, 2) void w4_grad_tile_kernel(W4GradArgs a, int tm, int tk) {
   using T = typename W4Mem<TYPE>::T;
   using F = Frag<TYPE == QC_TYPE_F32 ? QC_TYPE_BF16 : TYPE>;
   using G = GradTile<TYPE, MI>;
   constexpr int P = G::P;
   extern __shared__ __align__(16) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, kb = lane >> 4;
+  const int half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, kb = lane >> 4;
   int mi, ki;
   tile_at(blockIdx.x, gridDim.x, tm, tk, 8, mi, ki);
   const int m0 = mi * 16 * MI, k0 = ki * 256, KB = a.K / 2;
@@ -44,7 +47,7 @@ __global__ __launch_bounds__(256, 2) void w4_grad_tile_kernel(W4GradArgs a, int 
   float sv[2];
   int zv[2];
   const auto fetch = [&](int step) {
-    const int i = step >= steps0, n0 = (step - (i ? steps0 : 0)) * GT_N, N = a.N[i];
+    const int i = step >= steps0 && a.nw > 1, n0 = (step - (i ? steps0 : 0)) * GT_N, N = a.N[i];
     const T *dy = (const T *)a.dy[i] + (int64_t)m0 * a.lddy[i];
     const W4Mat &w = a.w[i];
     const int ld = (int)a.lddy[i];
@@ -84,7 +87,7 @@ __global__ __launch_bounds__(256, 2) void w4_grad_tile_kernel(W4GradArgs a, int 
       if constexpr (TYPE == QC_TYPE_F32) {
         float p[4][3];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) tile_split(__builtin_bit_cast(w4_f4, dyv[v])[e], p[e]);
+        for (int e = 0; e < 4; ++e) w4_split(__builtin_bit_cast(w4_f4, dyv[v])[e], p[e]);
 #pragma unroll
         for (int s = 0; s < 3; ++s)
           *(w4_u2 *)(buf + s * 16 * MI * 128 + gt_slot(r, u >> 1) + (u & 1) * 8) = w4_u2{w4_pack_bf16(p[0][s], p[1][s]), w4_pack_bf16(p[2][s], p[3][s])};
@@ -111,14 +114,16 @@ __global__ __launch_bounds__(256, 2) void w4_grad_tile_kernel(W4GradArgs a, int 
   };
 
   w4_f4 acc[MI][4] = {};
-  if (steps) {
-    fetch(0);
-    put(lds);
+  char *mybuf = lds + half * (2 * G::BUF);
+  const int turns = (steps + 1) / 2;                                     // of both halves: the last step of one may lie beyond the rows
+  if (turns) {
+    fetch(half);
+    put(mybuf);
   }
   __syncthreads();
-  for (int step = 0; step < steps; ++step) {
-    const char *cur = lds + (step & 1) * G::BUF;
-    if (step + 1 < steps) fetch(step + 1);
+  for (int turn = 0; turn < turns; ++turn) {
+    const char *cur = mybuf + (turn & 1) * G::BUF;
+    if (turn + 1 < turns) fetch(2 * (turn + 1) + half);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       unsigned short q[8];
@@ -150,8 +155,8 @@ __global__ __launch_bounds__(256, 2) void w4_grad_tile_kernel(W4GradArgs a, int 
         for (int t = 0; t < 4; ++t) {
           if constexpr (TYPE == QC_TYPE_F32) {
             float p0[3], p1[3];
-            tile_split(v[0][t], p0);
-            tile_split(v[1][t], p1);
+            w4_split(v[0][t], p0);
+            w4_split(v[1][t], p1);
 #pragma unroll
             for (int p = 0; p < 3; ++p) wf[p][t][i] = w4_pack_bf16(p0[p], p1[p]);
           } else {
@@ -174,23 +179,36 @@ __global__ __launch_bounds__(256, 2) void w4_grad_tile_kernel(W4GradArgs a, int 
         }
       }
     }
-    if (step + 1 < steps) put(lds + ((step + 1) & 1) * G::BUF);
+    if (turn + 1 < turns) put(mybuf + ((turn + 1) & 1) * G::BUF);
     __syncthreads();
   }
 
+  // the first half of the workgroup finishes the tile's upper rows, the second the lower ones
+  w4_f4 *there = (w4_f4 *)lds;
+#pragma unroll
+  for (int i = 0; i < MI / 2; ++i)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) there[(i * 4 + t) * 512 + threadIdx.x] = half ? acc[i][t] : acc[i + MI / 2][t];
+  __syncthreads();
   const int k = k0 + wave * 64 + r16 * 4;
   if (k >= a.K) return;
 #pragma unroll
-  for (int i = 0; i < MI; ++i)
+  for (int i = 0; i < MI / 2; ++i) {
+    w4_f4 sum[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const w4_f4 o = there[(i * 4 + t) * 512 + (threadIdx.x ^ 256)];
+      sum[t] = half ? o + acc[i + MI / 2][t] : acc[i][t] + o;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int r = 16 * i + kb * 4 + e;
+      const int r = 16 * (i + half * (MI / 2)) + kb * 4 + e;
       if (r > last) continue;
       T *o = (T *)a.dx + (int64_t)(m0 + r) * a.lddx + k;
       typedef T T4 __attribute__((ext_vector_type(4)));
       T4 v;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) v[t] = W4Mem<TYPE>::put(acc[i][t][e]);
+      for (int t = 0; t < 4; ++t) v[t] = W4Mem<TYPE>::put(sum[t][e]);
       if ((uintptr_t)o % sizeof(T4) == 0) {
         *(T4 *)o = v;
       } else {
@@ -198,11 +216,12 @@ __global__ __launch_bounds__(256, 2) void w4_grad_tile_kernel(W4GradArgs a, int 
         for (int t = 0; t < 4; ++t) o[t] = v[t];
       }
     }
+  }
 }
 
 template <int TYPE, int MI, bool ASYM>
 static hipError_t launch(const W4GradArgs &a, hipStream_t st) {
-  constexpr int lds = 2 * GradTile<TYPE, MI>::BUF;
+  constexpr int lds = GradTile<TYPE, MI>::LDS;
   const int tm = (a.M + 16 * MI - 1) / (16 * MI), tk = (a.K + 255) / 256;
   static std::atomic<unsigned long long> done{0};
   auto kern = w4_grad_tile_kernel<TYPE, MI, ASYM>;
@@ -210,21 +229,35 @@ static hipError_t launch(const W4GradArgs &a, hipStream_t st) {
     hipError_t e = allow_lds((const void *)kern, lds, done);
     if (e != hipSuccess) return e;
   }
-  kern<<<tm * tk, 256, lds, st>>>(a, tm, tk);
+  kern<<<tm * tk, 512, lds, st>>>(a, tm, tk);
   return hipGetLastError();
 }
+
+// us of a step of both halves of a workgroup (128 rows of W), by row blocks of a tile: measured with bfloat16 at 4608 x 1152, 9216 x 1152
+// and 4608 x 4608, 64 - 4096 rows.  A compute unit runs one workgroup at a time, two of the smallest.
+static float step_time(int MI) { return MI == 8 ? 2.9f : MI == 6 ? 2.75f : MI == 4 ? 2.3f : 2.1f; }
 
 template <int TYPE, bool ASYM>
 static hipError_t rows(const W4GradArgs &a, hipStream_t st) {
   const int64_t tk = (a.K + 255) / 256;
-  if constexpr (TYPE != QC_TYPE_F32)
-    if ((a.M + 127) / 128 * tk >= 256) return launch<TYPE, 8, ASYM>(a, st);
-  if ((a.M + 63) / 64 * tk >= 256) return launch<TYPE, 4, ASYM>(a, st);
-  return launch<TYPE, 2, ASYM>(a, st);
+  int best = 2;
+  float time = 0.0f;
+  for (int MI = 2; MI <= (TYPE == QC_TYPE_F32 ? 4 : 8); MI += 2) {       // float32: three planes of 64 rows fill LDS
+    const int64_t groups = (a.M + 16 * MI - 1) / (16 * MI) * tk, slots = MI == 2 ? 512 : 256;
+    const float t = step_time(MI) * (float)((groups + slots - 1) / slots);
+    if (MI == 2 || t < time) {
+      best = MI;
+      time = t;
+    }
+  }
+  if constexpr (TYPE != QC_TYPE_F32) {
+    if (best == 8) return launch<TYPE, 8, ASYM>(a, st);
+    if (best == 6) return launch<TYPE, 6, ASYM>(a, st);
+  }
+  return best == 4 ? launch<TYPE, 4, ASYM>(a, st) : launch<TYPE, 2, ASYM>(a, st);
 }
 
-// 32-bit offsets inside a tile's rows
-bool w4_grad_tile_pays(const W4GradArgs &a, int) { return a.M > 16 && a.lddy[0] < (1 << 22) && a.lddy[1] < (1 << 22); }
+bool w4_grad_tile_pays(const W4GradArgs &a, int) { return a.M > 16; }
 
 hipError_t launch_w4_grad_tile(const W4GradArgs &a, int type, hipStream_t st) {
   const bool z = a.w[0].zero != nullptr;

@@ -9,66 +9,141 @@
 
 namespace qc {
 
-// GC: groups in a chunk of 128 inputs; MT: tiles of 16 rows
-template <int TYPE, int GC, int MT, int OP>
-__global__ __launch_bounds__(MT > 1 ? 512 : 1024) void w4_rows_kernel(W4Args a) {
-  using F = Frag<TYPE>;
+template <int TYPE>
+struct RowsX {                                                           // a lane's 8 inputs of a product
+  using X = typename std::conditional<TYPE == QC_TYPE_F32, w4_f8, typename FragOf<TYPE>::X>::type;
+  static constexpr int ES = TYPE == QC_TYPE_F32 ? 4 : TYPE == QC_TYPE_I8 ? 1 : 2;
+  static __device__ __forceinline__ X load(__amdgpu_buffer_rsrc_t buf, unsigned at, int chunk) {
+    if constexpr (TYPE == QC_TYPE_I8) {
+      return __builtin_bit_cast(w4_u2, __builtin_amdgcn_raw_buffer_load_b64(buf, at, chunk, 0));
+    } else if constexpr (TYPE == QC_TYPE_F32) {
+      const w4_f4 a = __builtin_bit_cast(w4_f4, __builtin_amdgcn_raw_buffer_load_b128(buf, at, chunk, 0));
+      const w4_f4 b = __builtin_bit_cast(w4_f4, __builtin_amdgcn_raw_buffer_load_b128(buf, at + 16, chunk, 0));
+      return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      return __builtin_bit_cast(X, __builtin_amdgcn_raw_buffer_load_b128(buf, at, chunk, 0));
+    }
+  }
+};
+
+// GC: groups in a chunk of 128 inputs; MT: tiles of 16 rows; NT: of 16 columns (of each matrix)
+// PULL: inputs are loaded like weight rows, four lanes a row, and pulled into place (a few rows cost less as they are)
+template <int TYPE, int GC, int MT, int NT, int OP, bool ASYM, bool PULL>
+__global__ __launch_bounds__(MT * NT > 2 ? 512 : 1024) void w4_rows_kernel(W4Args a) {
+  using F = FragOf<TYPE>;
   using T = typename W4Mem<TYPE>::T;
-  using XT = typename std::conditional<TYPE == QC_TYPE_I8, int8_t, T>::type;
-  constexpr int NW = OP == W4_LINEAR ? 1 : 2;
+  constexpr int P = TYPE == QC_TYPE_F32 ? 3 : 1, ES = RowsX<TYPE>::ES, MATS = OP == W4_LINEAR ? 1 : 2, NW = MATS * NT;
+  constexpr int AHEAD = MT == 1 ? 2 : 1;         // chunks whose inputs are asked for before they are needed
   extern __shared__ float red[];                 // [wavefronts][NW][MT][64][4]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int r16 = lane & 15, kb = lane >> 4;
-  const int ntn = (a.N + 15) / 16, n0 = (int)(blockIdx.x % ntn) * 16, m0 = (int)(blockIdx.x / ntn) * (16 * MT);
-  const size_t n = min(n0 + r16, a.N - 1);
-  const XT *xr[MT];
+  const int ntn = (a.N + 16 * NT - 1) / (16 * NT), n0 = (int)(blockIdx.x % ntn) * (16 * NT), m0 = (int)(blockIdx.x / ntn) * (16 * MT);
+  const int KB = a.K / 2, chunks = (a.K + 127) / 128, rest = a.N - n0;
+  const __amdgpu_buffer_rsrc_t xb = w4_buffer((const char *)a.x + (int64_t)m0 * a.ldx * ES, ((int64_t)(a.M - 1 - m0) * a.ldx + a.K) * ES);
+  __amdgpu_buffer_rsrc_t qb[MATS], sb[MATS], zb[MATS];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) xr[i] = (const XT *)a.x + (int64_t)min(m0 + 16 * i + r16, a.M - 1) * a.ldx;
-  const int KB = a.K / 2, chunks = (a.K + 127) / 128;
-  w4_f4 y[NW][MT];
+  for (int w = 0; w < MATS; ++w) {
+    qb[w] = w4_buffer(a.w[w].q + (size_t)n0 * KB, (int64_t)rest * KB);
+    sb[w] = w4_buffer(a.w[w].scale + (size_t)n0 * a.G, (int64_t)rest * a.G * 4);
+    if (ASYM) zb[w] = w4_buffer(a.w[w].zero + (size_t)n0 * a.G, (int64_t)rest * a.G);
+  }
+  // offsets of the lane; a chunk's own offset is uniform
+  unsigned xat[MT], qat[NT], gat[NT];
 #pragma unroll
-  for (int w = 0; w < NW; ++w)
+  for (int i = 0; i < MT; ++i) xat[i] = (unsigned)(16 * i + (PULL ? lane >> 2 : r16)) * (unsigned)a.ldx * ES + (PULL ? lane & 3 : kb) * 8 * ES;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) y[w][i] = w4_f4{};
-  for (int c = wave; c < chunks; c += waves) {
+  for (int w = 0; w < NT; ++w) {
+    qat[w] = (unsigned)((16 * w + (lane >> 2)) * KB + (lane & 3) * 16);
+    gat[w] = (unsigned)((16 * w + (lane >> 2)) * a.G + (lane & 3));
+  }
+  const int from = w4_from(lane), fromg = r16 * 16;                     // four groups of a row lie in four neighbouring lanes
+
+  struct Slot {
     w4_u4 q[NW];
+    typename RowsX<TYPE>::X x[MT][4];
+  } slot[AHEAD];
+  constexpr int PER = 4 / GC;                    // chunks to four groups
+  unsigned s4[NW], z4[NW];
+  w4_f4 y[NW][MT] = {};
+  const auto fetch = [&](Slot &f, int c) {
+#pragma unroll
+    for (int w = 0; w < NW; ++w) f.q[w] = __builtin_bit_cast(w4_u4, __builtin_amdgcn_raw_buffer_load_b128(qb[w / NT], qat[w % NT], c * 64, 0));
+    if ((c + 1) * 128 <= a.K) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) f.x[i][j] = RowsX<TYPE>::load(xb, xat[i] + j * 32 * ES, c * 128 * ES);
+    } else {                                     // a row's end is not the buffer's
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          f.x[i][j] = RowsX<TYPE>::load(xb, c * 128 + j * 32 + (PULL ? lane & 3 : kb) * 8 < a.K ? xat[i] + j * 32 * ES : W4_NOWHERE, c * 128 * ES);
+    }
+  };
+  const auto fetch4 = [&](int c) {               // scales and zero points of the four groups that chunk c's are among
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      q[w] = w4_load16(a.w[w].q + n * KB, c * 64 + kb * 16, KB);
-      w4_transpose(q[w]);
+      s4[w] = __builtin_amdgcn_raw_buffer_load_b32(sb[w / NT], gat[w % NT] * 4, (c & -PER) * GC * 4, 0);
+      if (ASYM) z4[w] = __builtin_amdgcn_raw_buffer_load_b8(zb[w / NT], gat[w % NT], (c & -PER) * GC, 0);
+    }
+  };
+  const auto use = [&](Slot &f, int c) {
+    float sc[NW][GC];
+    int z[NW][GC];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f.q[w][e] = w4_pull(f.q[w][e], from);
+#pragma unroll
+      for (int g = 0; g < GC; ++g) {
+        const int at = fromg + ((c & (PER - 1)) * GC + g) * 4;
+        const float s = __builtin_bit_cast(float, w4_pull(s4[w], at));
+        // beyond the last group nothing is added, whatever was read there
+        sc[w][g] = c * GC + g < a.G ? s * (TYPE == QC_TYPE_I8 ? 1.0f : 16.0f) : 0.0f;
+        z[w][g] = ASYM ? (int)w4_pull(z4[w], at) : 8;
+      }
+      w4_transpose(f.q[w]);
     }
 #pragma unroll
-    for (int gi = 0; gi < GC; ++gi) {
-      const size_t g = n * a.G + min(c * GC + gi, a.G - 1);
-      typename F::Acc acc[NW][MT];
-#pragma unroll
-      for (int w = 0; w < NW; ++w)
-#pragma unroll
-        for (int i = 0; i < MT; ++i) acc[w][i] = typename F::Acc{};
-      float s[NW], z16[NW];
-      unsigned zb[NW];
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        s[w] = a.w[w].scale[g] * (TYPE == QC_TYPE_I8 ? 1.0f : 16.0f);
-        const int z = a.w[w].zero ? a.w[w].zero[g] : 8;
-        z16[w] = (float)(z - 8) * 0.0625f;
-        zb[w] = (unsigned)z * 0x01010101u;
-      }
+    for (int g = 0; g < GC; ++g) {
+      typename F::Acc acc[NW][MT] = {};
 #pragma unroll
       for (int t = 0; t < 4 / GC; ++t) {
-        const int j = gi * (4 / GC) + t;
-        const int k = c * 128 + j * 32 + kb * 8;
-        typename F::X x[MT];
+        const int j = g * (4 / GC) + t;
+        if (PULL) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            typedef unsigned XU __attribute__((ext_vector_type(2 * ES)));
+            XU v = __builtin_bit_cast(XU, f.x[i][j]);
+#pragma unroll
+            for (int e = 0; e < 2 * ES; ++e) v[e] = w4_pull(v[e], from);
+            f.x[i][j] = __builtin_bit_cast(typename RowsX<TYPE>::X, v);
+          }
+        }
+        typename F::X xf[MT][P];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          x[i] = typename F::X{};
-          if (k < a.K) x[i] = *(const typename F::X *)(xr[i] + k);
+          if constexpr (TYPE == QC_TYPE_F32) {
+            float p[8][3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w4_split(f.x[i][j][e], p[e]);
+#pragma unroll
+            for (int s = 0; s < 3; ++s)
+              xf[i][s] = __builtin_bit_cast(w4_bf8, w4_u4{w4_pack_bf16(p[0][s], p[1][s]), w4_pack_bf16(p[2][s], p[3][s]),
+                                                          w4_pack_bf16(p[4][s], p[5][s]), w4_pack_bf16(p[6][s], p[7][s])});
+          } else {
+            xf[i][0] = f.x[i][j];
+          }
         }
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          const typename F::W wf = F::template weights<true>(q[w][j], z16[w], zb[w]);
+          const float z16 = ASYM ? (float)(z[w][g] - 8) * 0.0625f : 0.0f;
+          const typename F::W wf = F::template weights<ASYM>(f.q[w][j], z16, ASYM ? (unsigned)z[w][g] * 0x01010101u : 0u);
 #pragma unroll
-          for (int i = 0; i < MT; ++i) acc[w][i] = F::mma(x[i], wf, acc[w][i]);
+          for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) acc[w][i] = F::mma(xf[i][p], wf, acc[w][i]);
         }
       }
 #pragma unroll
@@ -76,7 +151,32 @@ __global__ __launch_bounds__(MT > 1 ? 512 : 1024) void w4_rows_kernel(W4Args a) 
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[w][i][e] += s[w] * (float)acc[w][i][e];
+          for (int e = 0; e < 4; ++e) y[w][i][e] += sc[w][g] * (float)acc[w][i][e];
+    }
+  };
+  // Wavefronts take pairs of chunks, 128 bytes of every weight row: whole cache lines
+  if constexpr (AHEAD == 2) {
+    // four groups serve the pair, or (groups of 32) each chunk its own four
+    const int step = 2 * waves;
+    int c = 2 * wave;
+    if (c < chunks) {
+      fetch4(c);
+      fetch(slot[0], c);
+    }
+    if (c + 1 < chunks) fetch(slot[1], c + 1);
+    for (; c < chunks; c += step) {
+      use(slot[0], c);
+      if (GC == 4 && c + 1 < chunks) fetch4(c + 1);
+      if (c + step < chunks) fetch(slot[0], c + step);
+      if (c + 1 < chunks) use(slot[1], c + 1);
+      if (c + step < chunks) fetch4(c + step);
+      if (c + 1 + step < chunks) fetch(slot[1], c + 1 + step);
+    }
+  } else {
+    for (int c = wave; c < chunks; c += waves) {
+      fetch4(c);
+      fetch(slot[0], c);
+      use(slot[0], c);
     }
   }
   constexpr int TILE = MT * 256;
@@ -87,14 +187,15 @@ __global__ __launch_bounds__(MT > 1 ? 512 : 1024) void w4_rows_kernel(W4Args a) 
 #pragma unroll
       for (int e = 0; e < 4; ++e) red[(wave * NW + w) * TILE + (i * 16 + kb * 4 + e) * 16 + r16] = y[w][i][e];
   __syncthreads();
-  for (int o = threadIdx.x; o < TILE; o += blockDim.x) {
-    const int m = m0 + o / 16, col = n0 + o % 16;
+  for (int o = threadIdx.x; o < TILE * NT; o += blockDim.x) {
+    const int nt = o / TILE, in = o % TILE, m = m0 + in / 16, col = n0 + nt * 16 + in % 16;
     if (m >= a.M || col >= a.N) continue;
-    float v[NW];
+    float v[MATS];
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      float t = red[w * TILE + o];
-      for (int p = 1; p < waves; ++p) t += red[(p * NW + w) * TILE + o];
+    for (int w = 0; w < MATS; ++w) {
+      const float *r = red + (w * NT + nt) * TILE + in;
+      float t = r[0];
+      for (int p = 1; p < waves; ++p) t += r[p * NW * TILE];
       if (TYPE == QC_TYPE_I8) t = a.xs * (t - (float)a.zp * a.w[w].sum[col]);
       v[w] = t + (a.w[w].bias ? a.w[w].bias[col] : 0.0f);
     }
@@ -115,25 +216,77 @@ __global__ __launch_bounds__(MT > 1 ? 512 : 1024) void w4_rows_kernel(W4Args a) 
   }
 }
 
-template <int TYPE, int GC, int MT, int OP>
+// wavefronts of a workgroup: up to 16 (8 of the larger tiles), no more than chunks (pairs of chunks) and than fill the chip
+static int rows_waves(const W4Args &a, int MT, int NW, int groups) {
+  const int chunks = (a.K + 127) / 128, turns = MT == 1 ? (chunks + 1) / 2 : chunks, most = MT * NW > 2 ? 8 : 16;
+  int waves = 1;
+  while (waves < most && waves < turns && groups * waves < 4096) waves *= 2;
+  return waves;
+}
+
+template <int TYPE, int GC, int MT, int NW, int OP, bool PULL>
 static hipError_t rows_launch(const W4Args &a, hipStream_t st) {
-  const int waves = std::min((a.K + 127) / 128, MT > 1 ? 8 : 16);
-  const int lds = waves * (OP == W4_LINEAR ? 1 : 2) * MT * 1024;
-  const unsigned grid = (unsigned)((a.N + 15) / 16) * (unsigned)((a.M + 16 * MT - 1) / (16 * MT));
-  static std::atomic<unsigned long long> done{0};
-  auto kern = w4_rows_kernel<TYPE, GC, MT, OP>;
+  constexpr int NT = NW / (OP == W4_LINEAR ? 1 : 2);
+  const int ntn = (a.N + 16 * NT - 1) / (16 * NT), ntm = (a.M + 16 * MT - 1) / (16 * MT), waves = rows_waves(a, MT, NW, ntn * ntm);
+  const int lds = waves * NW * MT * 1024;
+  static std::atomic<unsigned long long> done[2];
+  auto kern = a.w[0].zero ? w4_rows_kernel<TYPE, GC, MT, NT, OP, true, PULL> : w4_rows_kernel<TYPE, GC, MT, NT, OP, false, PULL>;
   if (lds > 65536) {
-    hipError_t e = allow_lds((const void *)kern, lds, done);
+    hipError_t e = allow_lds((const void *)kern, lds, done[a.w[0].zero != nullptr]);
     if (e != hipSuccess) return e;
   }
-  kern<<<grid, waves * 64, lds, st>>>(a);
+  kern<<<(unsigned)ntn * (unsigned)ntm, waves * 64, lds, st>>>(a);
   return hipGetLastError();
+}
+
+// Tiles of this kernel, MT row blocks by NW column blocks of both matrices, and what a step (a chunk of every wavefront of a workgroup)
+// of theirs takes in us, measured with bfloat16 and groups of 128 at 4608 x 1152, 1152 x 4608, 8192 x 8192 and 2000 x 1040, 1 - 512
+// rows: alone, and for each 16 (8 of the larger tiles) wavefronts a compute unit has to run.  A launch takes the tile whose steps
+// come to least; against the best of all tiles that loses 18 % at most and mostly nothing.
+struct RowsTile {
+  int MT, NW;
+  float alone, full;
+};
+static constexpr RowsTile ROWS_TILES[] = {{1, 1, 0.7f, 1.2f}, {1, 2, 0.9f, 2.0f}, {2, 2, 1.9f, 1.4f}, {4, 2, 2.3f, 2.6f}, {4, 4, 3.7f, 4.0f}};
+
+static float rows_time(const W4Args &a, int op, const RowsTile &t) {
+  const int cols = 16 * t.NW / (op == W4_LINEAR ? 1 : 2), groups = ((a.N + cols - 1) / cols) * ((a.M + 16 * t.MT - 1) / (16 * t.MT));
+  const int waves = rows_waves(a, t.MT, t.NW, groups), chunks = (a.K + 127) / 128, steps = (chunks + waves - 1) / waves;
+  return steps * std::max(t.alone, t.full * groups * waves / (256.0f * (t.MT * t.NW > 2 ? 8 : 16)));
+}
+
+static int rows_tile(const W4Args &a, int op, float &time) {
+  int best = -1;
+  for (int i = op == W4_LINEAR ? 0 : 1; i < 5; ++i) {
+    const float t = rows_time(a, op, ROWS_TILES[i]);
+    if (best < 0 || t < time) {
+      best = i;
+      time = t;
+    }
+  }
+  return best;
+}
+
+// The kernel of large tiles (w4_tile.hip) takes 2 us a chunk while a compute unit has one of its workgroups, and 2.8 for two.
+bool w4_tile_pays(const W4Args &a, int type, int op) {
+  float rows;
+  rows_tile(a, op, rows);
+  const int tr = w4_tile_rows(a, type), tc = op == W4_LINEAR ? 256 : 128;
+  const float tiles = (float)((a.M + tr - 1) / tr) * (float)((a.N + tc - 1) / tc);
+  return (a.K + 127) / 128 * std::max(2.0f, 2.8f * tiles / 512.0f) < rows;
 }
 
 template <int TYPE, int GC, int OP>
 static hipError_t rows_mt(const W4Args &a, hipStream_t st) {
-  if (a.M <= 16) return rows_launch<TYPE, GC, 1, OP>(a, st);
-  return rows_launch<TYPE, GC, 4, OP>(a, st);
+  float time;
+  const int i = rows_tile(a, OP, time);
+  const bool pull = a.M > 4;       // 8192 x 8192, bfloat16: 11.7 us without and 12.1 with at 4 rows, 12.8 and 12.6 at 8
+  if constexpr (OP == W4_LINEAR)
+    if (i == 0) return pull ? rows_launch<TYPE, GC, 1, 1, OP, true>(a, st) : rows_launch<TYPE, GC, 1, 1, OP, false>(a, st);
+  if (i == 1) return pull ? rows_launch<TYPE, GC, 1, 2, OP, true>(a, st) : rows_launch<TYPE, GC, 1, 2, OP, false>(a, st);
+  if (i == 2) return rows_launch<TYPE, GC, 2, 2, OP, true>(a, st);
+  if (i == 3) return rows_launch<TYPE, GC, 4, 2, OP, true>(a, st);
+  return rows_launch<TYPE, GC, 4, 4, OP, true>(a, st);
 }
 
 template <int TYPE, int OP>

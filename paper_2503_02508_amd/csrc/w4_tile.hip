@@ -21,10 +21,6 @@ __device__ __forceinline__ int tile_slot(int r, int u) {
   return TYPE == QC_TYPE_I8 ? r * 128 + ((u ^ ((r >> 1) & 7)) << 4) : r * 256 + ((u ^ (r & 15)) << 4);
 }
 
-// The matrix products' operands of float32 activations: bfloat16, three a product
-template <int TYPE>
-using TileFrag = Frag<TYPE == QC_TYPE_F32 ? QC_TYPE_BF16 : TYPE>;
-
 // Activations of one chunk on their way from memory to LDS, in units of 16 bytes.  float32 goes through registers, where it is split;
 // the other types go to LDS directly: a wavefront's load fills 1024 bytes in the order of its lanes, so the lane that fills a slot
 // asks for the unit that belongs there.
@@ -33,10 +29,12 @@ struct TileLoad {
   static constexpr int ES = TYPE == QC_TYPE_F32 ? 4 : TYPE == QC_TYPE_I8 ? 1 : 2;
   static constexpr int UR = TILE_K * ES / 16;                            // units a row
   static constexpr int NU = 16 * MI * UR / 256;
+  static_assert(16 * MI * UR % 256 == 0, "whole loads");
   w4_u4 v[TYPE == QC_TYPE_F32 ? NU : 1];
   // x: the tile's first row; `last`: the last row of it that exists.  The offsets are formed again each time, not kept.
   __device__ __forceinline__ void load(const char *x, int row_bytes, int last, int k0, int K, char *lds) {
     asm volatile("" : "+s"(last));
+    const bool whole = k0 + TILE_K <= K;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
       const int t = threadIdx.x + 256 * i, r = t / UR;
@@ -44,11 +42,15 @@ struct TileLoad {
       const int k = k0 + u * (16 / ES);
       const char *from = x + (unsigned)(min(r, last) * row_bytes + k * ES);
       if constexpr (TYPE == QC_TYPE_F32) {
-        v[i] = w4_u4{};
-        if (k < K) v[i] = *(const w4_u4 *)from;
+        if (whole) {
+          v[i] = *(const w4_u4 *)from;
+        } else {
+          v[i] = w4_u4{};
+          if (k < K) v[i] = *(const w4_u4 *)from;
+        }
       } else {
         char *to = lds + (threadIdx.x >> 6) * 1024 + i * 4096;
-        if (k < K)
+        if (whole || k < K)
           __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
         else
           *(w4_u4 *)(to + (threadIdx.x & 63) * 16) = w4_u4{};
@@ -62,7 +64,7 @@ struct TileLoad {
         const int t = threadIdx.x + 256 * i, r = t / UR, u = t % UR;
         float p[4][3];                                                   // four values: half a unit of each plane
 #pragma unroll
-        for (int e = 0; e < 4; ++e) tile_split(__builtin_bit_cast(w4_f4, v[i])[e], p[e]);
+        for (int e = 0; e < 4; ++e) w4_split(__builtin_bit_cast(w4_f4, v[i])[e], p[e]);
 #pragma unroll
         for (int s = 0; s < 3; ++s)
           *(w4_u2 *)(lds + s * 16 * MI * 256 + tile_slot<TYPE>(r, u >> 1) + (u & 1) * 8) = w4_u2{w4_pack_bf16(p[0][s], p[1][s]), w4_pack_bf16(p[2][s], p[3][s])};
@@ -79,7 +81,7 @@ constexpr int tile_lds = 2 * tile_buffer<TYPE, MI> > 4 * 16 * 68 * 4 ? 2 * tile_
 // UK: inputs whose weights a wavefront holds expanded, a group or half of one
 template <int TYPE, int GC, int MI, int OP, bool ASYM, int UK>
 __global__ __launch_bounds__(256, 2) void w4_tile_kernel(W4Args a, int tm, int tn) {
-  using F = TileFrag<TYPE>;
+  using F = FragOf<TYPE>;
   using T = typename W4Mem<TYPE>::T;
   constexpr int BUF = tile_buffer<TYPE, MI>, P = tile_planes<TYPE>;
   constexpr bool TWO = OP != W4_LINEAR;
@@ -96,28 +98,36 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(W4Args a, int tm, int t
   const int row_bytes = (int)a.ldx * TileLoad<TYPE, MI>::ES, last = a.M - 1 - m0;
   const char *x0 = (const char *)a.x + (int64_t)m0 * row_bytes;
 
-  // block j of a wavefront: its matrix and its column in this lane
-  int nj[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) nj[j] = min(n0 + (TWO ? j & 1 : j) * 16 + r16, a.N - 1);
+  // block j of a wavefront: its matrix and its column in this lane.  Rows beyond the last read as zero.
   const auto wj = [&](int j) -> const W4Mat & { return a.w[TWO ? j >> 1 : 0]; };
+  constexpr int MATS = TWO ? 2 : 1;
+  __amdgpu_buffer_rsrc_t qb[MATS], sb[MATS], zb_[MATS];
+  const int first = ni * LN, rest = a.N - first;
+#pragma unroll
+  for (int w = 0; w < MATS; ++w) {
+    qb[w] = w4_buffer(a.w[w].q + (size_t)first * KB, (int64_t)rest * KB);
+    sb[w] = w4_buffer(a.w[w].scale + (size_t)first * a.G, (int64_t)rest * a.G * 4);
+    if (ASYM) zb_[w] = w4_buffer(a.w[w].zero + (size_t)first * a.G, (int64_t)rest * a.G);
+  }
+  const int nl = wave * WN + (lane >> 2), from = w4_from(lane), fromg = r16 * 16;
 
   w4_f4 y[MI][4] = {};
   TileLoad<TYPE, MI> next;
   w4_u4 q[4];
-  float s[4][GC];
-  int z[4][GC];
+  unsigned s4[4], z4[4];                                                 // of four groups, in four neighbouring lanes
+  constexpr int PER = 4 / GC;                                            // chunks to four groups
   const auto fetch = [&](int c) {
+    int n = nl;
+    asm volatile("" : "+v"(n));                                          // offsets are formed again each time, not kept
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      int n = nj[j];
-      asm volatile("" : "+v"(n));                                        // addresses are formed again each time, not kept
-      q[j] = w4_load16(wj(j).q + (size_t)n * KB, c * 64 + kb * 16, KB);
+    for (int j = 0; j < 4; ++j)
+      q[j] = __builtin_bit_cast(w4_u4, __builtin_amdgcn_raw_buffer_load_b128(qb[TWO ? j >> 1 : 0], (n + (TWO ? j & 1 : j) * 16) * KB + (lane & 3) * 16, c * 64, 0));
+    if (c % PER == 0) {
 #pragma unroll
-      for (int g = 0; g < GC; ++g) {
-        const size_t at = (size_t)((unsigned)n * (unsigned)a.G + (unsigned)min(c * GC + g, a.G - 1));
-        s[j][g] = wj(j).scale[at];
-        if (ASYM) z[j][g] = wj(j).zero[at];
+      for (int j = 0; j < 4; ++j) {
+        const int at = (n + (TWO ? j & 1 : j) * 16) * a.G + (lane & 3);
+        s4[j] = __builtin_amdgcn_raw_buffer_load_b32(sb[TWO ? j >> 1 : 0], at * 4, c * GC * 4, 0);
+        if (ASYM) z4[j] = __builtin_amdgcn_raw_buffer_load_b8(zb_[TWO ? j >> 1 : 0], at, c * GC, 0);
       }
     }
   };
@@ -131,13 +141,19 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(W4Args a, int tm, int t
     unsigned zb[4][GC];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[j][e] = w4_pull(q[j][e], from);
       if (!K64) w4_transpose(q[j]);
       else if (GC == 2) w4_swap32(q[j]);
 #pragma unroll
       for (int g = 0; g < GC; ++g) {
-        sc[j][g] = s[j][g] * (TYPE == QC_TYPE_I8 ? 1.0f : 16.0f);
-        z16[j][g] = ASYM ? (float)(z[j][g] - 8) * 0.0625f : 0.0f;
-        zb[j][g] = ASYM ? (unsigned)z[j][g] * 0x01010101u : 0u;
+        const int at = fromg + (c % PER * GC + g) * 4;
+        const float s = __builtin_bit_cast(float, w4_pull(s4[j], at));
+        // beyond the last group nothing is added, whatever was read there
+        sc[j][g] = c * GC + g < a.G ? s * (TYPE == QC_TYPE_I8 ? 1.0f : 16.0f) : 0.0f;
+        const int z = ASYM ? (int)w4_pull(z4[j], at) : 8;
+        z16[j][g] = (float)(z - 8) * 0.0625f;
+        zb[j][g] = (unsigned)z * 0x01010101u;
       }
     }
     if (c + 1 < chunks) next.load(x0, row_bytes, last, (c + 1) * 128, a.K, lds + ((c + 1) & 1) * BUF);
@@ -164,8 +180,20 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(W4Args a, int tm, int t
         }
       // the next chunk's codes, now that this one's are expanded
       if (un == U - 1 && c + 1 < chunks) fetch(c + 1);
-      // the products of one row block run while those of the one before are scaled
+      // The products of one row block run while those of the one before are scaled; operands are read RING - 1 products ahead
+      typedef typename std::conditional<K64, w4_i4, typename F::X>::type XF;
+      constexpr int RING = TYPE == QC_TYPE_I8 ? 2 : 3;
+      XF xf[RING][P];
+      const auto read = [&](int step) {
+        const int i = step / UJ, jj = un * UJ + step % UJ;
+        const int u = !K64 ? (TYPE == QC_TYPE_I8 ? jj * 2 + (kb >> 1) : jj * 4 + kb) : GC == 1 ? kb * 2 + jj : jj * 4 + ((kb & 1) << 1 | kb >> 1);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          xf[step % RING][p] = *(const XF *)(cur + p * 16 * MI * 256 + tile_slot<TYPE>(16 * i + r16, u) + (TYPE == QC_TYPE_I8 && !K64 ? (kb & 1) * 8 : 0));
+      };
       typename F::Acc acc[2][4];
+#pragma unroll
+      for (int t = 0; t + 1 < RING; ++t) read(t);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i <= MI; ++i) {
@@ -174,26 +202,18 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(W4Args a, int tm, int t
           for (int j = 0; j < 4; ++j) acc[i & 1][j] = typename F::Acc{};
 #pragma unroll
           for (int t = 0; t < UJ; ++t) {
-            const int jj = un * UJ + t;
-            if constexpr (K64) {
-              const int u = GC == 1 ? kb * 2 + jj : jj * 4 + ((kb & 1) << 1 | kb >> 1);
-              const w4_i4 xf = *(const w4_i4 *)(cur + tile_slot<TYPE>(16 * i + r16, u));
+            const int step = i * UJ + t;
+            if (step + RING - 1 < MI * UJ) read(step + RING - 1);
 #pragma unroll
-              for (int j = 0; j < 4; ++j)
-                acc[i & 1][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xf, __builtin_bit_cast(w4_i4, wf[t][j]), acc[i & 1][j], 0, 0, 0);
-            } else {
+            for (int p = 0; p < P; ++p)
 #pragma unroll
-              for (int p = 0; p < P; ++p) {
-                const char *at = cur + p * 16 * MI * 256 + (TYPE == QC_TYPE_I8 ? tile_slot<TYPE>(16 * i + r16, jj * 2 + (kb >> 1)) + (kb & 1) * 8
-                                                                               : tile_slot<TYPE>(16 * i + r16, jj * 4 + kb));
-                const typename F::X xf = *(const typename F::X *)at;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  if constexpr (TYPE == QC_TYPE_I8) acc[i & 1][j] = F::mma(xf, w4_u2{wf[t][j][0], wf[t][j][1]}, acc[i & 1][j]);
-                  else acc[i & 1][j] = F::mma(xf, __builtin_bit_cast(typename F::W, wf[t][j]), acc[i & 1][j]);
-                }
+              for (int j = 0; j < 4; ++j) {
+                const XF x = xf[step % RING][p];
+                typename F::Acc &to = acc[i & 1][j];
+                if constexpr (K64) to = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, __builtin_bit_cast(w4_i4, wf[t][j]), to, 0, 0, 0);
+                else if constexpr (TYPE == QC_TYPE_I8) to = F::mma(x, w4_u2{wf[t][j][0], wf[t][j][1]}, to);
+                else to = F::mma(x, __builtin_bit_cast(typename F::W, wf[t][j]), to);
               }
-            }
           }
         }
         if (i > 0) {
@@ -215,6 +235,9 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(W4Args a, int tm, int t
   constexpr int SR = WN + 4, LR = WN / 4;                                // floats a staged row; lanes that store a row
   float *stage = (float *)lds + wave * (16 * 68);
   float bias[4], sum[4];
+  int nj[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) nj[j] = min(n0 + (TWO ? j & 1 : j) * 16 + r16, a.N - 1);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     bias[j] = wj(j).bias ? wj(j).bias[nj[j]] : 0.0f;
@@ -246,42 +269,53 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(W4Args a, int tm, int t
   };
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
+    constexpr int OUTS = OP == W4_GATED_GRAD ? 2 : 1;
+    w4_f4 v[OUTS][WN / 16];
 #pragma unroll
-    for (int pass = 0; pass < (OP == W4_GATED_GRAD ? 2 : 1); ++pass) {
+    for (int j = 0; j < WN / 16; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[0][j][e] = value(i, j, e);
+        if constexpr (TWO) {
+          float d;
+          const float act = w4_act(a.act, v[0][j][e], d), up = value(i, j + 2, e);
+          v[0][j][e] = OP == W4_GATED ? act * up : up * d;
+          if constexpr (OP == W4_GATED_GRAD) v[1][j][e] = act;
+        }
+      }
+#pragma unroll
+    for (int o = 0; o < OUTS; ++o) {
 #pragma unroll
       for (int j = 0; j < WN / 16; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = value(i, j, e);
-          if constexpr (TWO) {
-            float d;
-            const float act = w4_act(a.act, v, d), up = value(i, j + 2, e);
-            v = OP == W4_GATED ? act * up : pass ? act : up * d;
-          }
-          stage[(kb * 4 + e) * SR + j * 16 + r16] = v;
-        }
+        for (int e = 0; e < 4; ++e) stage[(kb * 4 + e) * SR + j * 16 + r16] = v[o][j][e];
       turn();
 #pragma unroll
       for (int rr = 0; rr < 16 * LR / 64; ++rr) {
         const int r = rr * (64 / LR) + lane / LR, row = m0 + i * 16 + r;
-        w4_f4 v = *(const w4_f4 *)(stage + r * SR + lane % LR * 4);
+        w4_f4 t = *(const w4_f4 *)(stage + r * SR + lane % LR * 4);
         if (row < a.M) {
           if constexpr (OP == W4_GATED_GRAD) {
             const T *dh = (const T *)a.dh + (int64_t)row * a.lddh + col;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] *= col + e < a.N ? W4Mem<TYPE>::get(dh[e]) : 0.0f;
+            for (int e = 0; e < 4; ++e) t[e] *= col + e < a.N ? W4Mem<TYPE>::get(dh[e]) : 0.0f;
           }
-          put4(pass ? a.y2 : a.y, a.ldy, row, v);
+          put4(o ? a.y2 : a.y, a.ldy, row, t);
         }
       }
       turn();
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
+// row blocks of a tile: as many as 256 registers hold without spilling
+static constexpr int tile_mi_of(int type, int group) { return type == QC_TYPE_F32 ? 4 : type == QC_TYPE_I8 ? 8 : group == 128 ? 5 : 6; }
+int w4_tile_rows(const W4Args &a, int type) { return 16 * tile_mi_of(type, a.group); }
+
 template <int TYPE, int GC, int MI, int OP, bool ASYM>
 static hipError_t tile_launch(const W4Args &a, hipStream_t st) {
-  constexpr int lds = tile_lds<TYPE, MI>, UK = TYPE == QC_TYPE_I8 ? 128 / GC : std::min(128 / GC, 64);
+  constexpr int lds = tile_lds<TYPE, MI>, UK = TYPE == QC_TYPE_F32 ? std::min(128 / GC, 64) : 128 / GC;
   const int tm = (a.M + 16 * MI - 1) / (16 * MI), tn = (a.N + (OP == W4_LINEAR ? 255 : 127)) / (OP == W4_LINEAR ? 256 : 128);
   static std::atomic<unsigned long long> done{0};
   auto kern = w4_tile_kernel<TYPE, GC, MI, OP, ASYM, UK>;
@@ -295,7 +329,7 @@ static hipError_t tile_launch(const W4Args &a, hipStream_t st) {
 
 template <int TYPE, int GC, int OP>
 static hipError_t tile_mi(const W4Args &a, hipStream_t st) {
-  constexpr int MI = TYPE == QC_TYPE_F32 ? 4 : 8;
+  constexpr int MI = tile_mi_of(TYPE, 128 / GC);
   return a.w[0].zero ? tile_launch<TYPE, GC, MI, OP, true>(a, st) : tile_launch<TYPE, GC, MI, OP, false>(a, st);
 }
 
@@ -313,9 +347,6 @@ static hipError_t tile_op(const W4Args &a, int op, hipStream_t st) {
   if constexpr (TYPE == QC_TYPE_I8) return hipErrorInvalidValue;
   else return tile_gc<TYPE, W4_GATED_GRAD>(a, st);
 }
-
-// 32-bit offsets inside a tile's rows
-bool w4_tile_pays(const W4Args &a, int, int) { return a.M > 64 && a.ldx < (1 << 22); }
 
 hipError_t launch_w4_tile(const W4Args &a, int type, int op, hipStream_t st) {
   if (type == QC_TYPE_F32) return tile_op<QC_TYPE_F32>(a, op, st);

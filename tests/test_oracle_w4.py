@@ -75,14 +75,14 @@ def _desc(qc, N=8, K=64, group=32, q=P, scale=P, zero=None, sum=P):  # noqa: A00
 
 
 BAD_WEIGHTS = [(dict(q=None), -1), (dict(scale=None), -1), (dict(N=-1), -2), (dict(K=0), -2), (dict(K=24), -2), (dict(K=-16), -2),
-               (dict(N=1 << 24), -2), (dict(K=1 << 24), -2), (dict(group=0), -7), (dict(group=16), -7), (dict(group=96), -7), (dict(group=-32), -7),
-               (dict(N=(1 << 24) - 1, K=1 << 16), -7), (dict(q=P + 8), -3), (dict(scale=P + 2), -3), (dict(sum=P + 1), -3)]
+               (dict(N=1 << 22), -2), (dict(K=1 << 22), -2), (dict(group=0), -7), (dict(group=16), -7), (dict(group=96), -7), (dict(group=-32), -7),
+               (dict(N=(1 << 22) - 1, K=1 << 15), -7), (dict(q=P + 8), -3), (dict(scale=P + 2), -3), (dict(sum=P + 1), -3)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_WEIGHTS)
 def test_every_call_refuses_a_bad_weight(qc, kw, code):
     L, bad, ok = qc.lib, C.byref(_desc(qc, **kw)), C.byref(_desc(qc))
-    far = 1 << 30
+    far = (1 << 22) - 16
     assert L.qc_w4_quantize(P, 0, far, bad, None) == code and qc.last_error()
     assert L.qc_w4_expand(bad, P, 0, far, None) == code
     assert L.qc_w4_linear(P, 0, far, 1.0, 128, bad, None, 1, P, far, None) == code
@@ -99,7 +99,7 @@ def test_refusals_of_the_other_arguments(qc):
     nosum, zeros, wide, short = (C.byref(_desc(qc, **kw)) for kw in (dict(sum=None), dict(zero=P), dict(K=128), dict(N=7)))
     for args, code in [((P, 3, 64, w, None), -7), ((P, 4, 64, w, None), -7), ((P, -1, 64, w, None), -7), ((None, 0, 64, w, None), -1),
                        ((P, 0, 63, w, None), -2), ((P, 0, 66, w, None), -3), ((P + 4, 0, 64, w, None), -3), ((P, 1, 68, w, None), -3),
-                       ((P, 0, 1 << 40, w, None), -2), ((P, 0, 64, None, None), -1)]:
+                       ((P, 0, 1 << 22, w, None), -2), ((P, 0, 64, None, None), -1)]:
         assert L.qc_w4_quantize(*args) == code, args
     for args, code in [((w, P, 3, 64, None), -7), ((w, None, 0, 64, None), -1), ((w, P, 0, 60, None), -2), ((w, P + 2, 0, 64, None), -3),
                        ((w, P + 1, 2, 64, None), -3), ((None, P, 0, 64, None), -1)]:
