@@ -181,8 +181,7 @@ int qc_w4_linear_grad(const void *dy, int type, int64_t lddy, const qc_w4_weight
   }
   a.M = M; a.K = w->K; a.group = w->group; a.G = (w->K + w->group - 1) / w->group;
   a.dx = dx; a.lddx = lddx;
-  QC_HIP(w4_grad_tile_pays(a, type) ? launch_w4_grad_tile(a, type, static_cast<hipStream_t>(stream))
-                                    : launch_w4_grad(a, type, static_cast<hipStream_t>(stream)));
+  QC_HIP(launch_w4_grad(a, type, static_cast<hipStream_t>(stream)));
   return QC_OK;
 }
 

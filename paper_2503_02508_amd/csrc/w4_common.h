@@ -62,8 +62,6 @@ bool w4_tile_pays(const W4Args &a, int type, int op);
 int w4_tile_rows(const W4Args &a, int type);
 hipError_t launch_w4_tile(const W4Args &a, int type, int op, hipStream_t st);
 hipError_t launch_w4_rows(const W4Args &a, int type, int op, hipStream_t st);
-bool w4_grad_tile_pays(const W4GradArgs &a, int type);
-hipError_t launch_w4_grad_tile(const W4GradArgs &a, int type, hipStream_t st);
 hipError_t launch_w4_grad(const W4GradArgs &a, int type, hipStream_t st);
 
 // ---- element types in memory
@@ -206,9 +204,10 @@ __device__ __forceinline__ w4_u4 w4_load16(const uint8_t *row, int at, int KB) {
 
 // float32 as three bfloat16 numbers whose sum it is exactly: truncation leaves 8 bits of the 24 each time.  What does not
 // change when its upper half is taken away (infinities) leaves nothing.
+template <bool FINITE = false>
 __device__ __forceinline__ void w4_split(float v, float p[3]) {
   const float h = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v) & 0xFFFF0000u);
-  const float r = h == v ? 0.0f : v - h;
+  const float r = !FINITE && h == v ? 0.0f : v - h;
   const float m = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, r) & 0xFFFF0000u);
   p[0] = h;
   p[1] = m;

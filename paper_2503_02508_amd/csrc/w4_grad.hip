@@ -1,67 +1,366 @@
 // Gradient of a linear layer's input through fixed 4-bit weights of groups: dx = dy W (+ dy2 W2).
 //
-// The summed axis is the rows of W, and the scales vary along it, so every weight is scaled before it enters a product.  A lane reads
-// 4 bytes of a weight row, 8 neighbouring inputs, and nibble t is its operand of product t: after the sum over all rows it
-// holds 8 neighbouring results of each of its rows of dx.
+// The summed axis is the rows of W.  A workgroup makes 16 MI rows by 64 CW columns of dx; its eight wavefronts are 8 / CW parties that take
+// the steps, 64 rows of W, in turn and add their sums at the end, so that a narrow dx still has every wavefront at work.  A step's
+// gradients, packed codes and scales go through LDS.  A lane expands, of 8 neighbouring rows of W, the 4 neighbouring columns it will hold
+// results of (nibble t of its two bytes belongs to product t).  The scales vary along the summed axis, so a weight is scaled before it
+// enters a product.  float16 and bfloat16: it is rounded to the type, half a step like every stored value; two products for one
+// would keep it whole and cost twice the time.  float32: gradients and scaled weights are each the sum of three bfloat16 numbers, and six of
+// the nine products are formed (the others are below 2^-22 of the largest).
 #include "w4_common.h"
 
 namespace qc {
 
-// 16 rows of dx by 128 columns; the workgroup's four wavefronts take the weight rows in turn, four at a time
-template <int TYPE>
-__global__ __launch_bounds__(256) void w4_grad_kernel(W4GradArgs a) {
+constexpr int GT_N = 64;                       // rows of W a step
+
+// MI: blocks of 16 rows; CW: wavefronts side by side, 64 columns each; the workgroup's eight wavefronts are 8 / CW such parties
+template <int TYPE, int MI, int CW, bool PRE>
+struct GradTile {
+  static constexpr int P = TYPE == QC_TYPE_F32 ? 3 : 1;
+  static constexpr int ES = TYPE == QC_TYPE_F32 ? 4 : 2;
+  static constexpr int S = 8 / CW, TH = 64 * CW;                         // parties, threads of one
+  static constexpr int WROW = 32 * CW + 8;                               // bytes between rows of packed codes in LDS: four rows 8 apart share no bank
+  static constexpr int GR = CW < 2 ? 2 : 2 * CW;                         // groups of up to 64 CW columns
+  static constexpr int DY = 16 * MI * 128 * P;                           // bytes: planes of 16 MI rows of 64 gradients
+  static constexpr int W = GT_N * WROW;
+  static constexpr int BUF = DY + W + (PRE ? 0 : GR * GT_N * 8);         // and (scale, offset) of every row and group
+  // two buffers a party; afterwards the sums, of two parties only the half that the other finishes
+  static constexpr int SUMS = (S == 2 ? MI / 2 : MI) * 4 * 512 * 16;
+  static constexpr int TABLES = PRE ? S * 3 * 2 * GT_N * 4 : 0;
+  static constexpr int LDS = 2 * S * BUF + TABLES > SUMS ? 2 * S * BUF + TABLES : SUMS;
+  static constexpr int UR = GT_N * ES / 16, NU = 16 * MI * UR / TH;
+  static constexpr int WU = 2 * CW, NW = GT_N * WU / TH;                 // units of a row of codes, a thread's
+  static constexpr int NS = GR * GT_N / TH;
+  static_assert(16 * MI * UR % TH == 0 && (S > 2 || MI % 2 == 0), "whole loads");
+};
+
+// 16-byte unit u of row r of a plane: 16 rows of one unit lie in 16 different slots of 256 bytes
+__device__ __forceinline__ int gt_slot(int r, int u) { return r * 128 + ((u ^ ((r >> 1) & 7)) << 4); }
+
+// PRE (float32): the tile's columns lie in one group, so that the scale of a weight row multiplies the gradients as they go to LDS, and the
+// weights are exact codes: three products for six, and nothing of the weights to split
+template <int TYPE, int MI, int CW, bool ASYM, bool PRE>
+__global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, int tk) {
   using T = typename W4Mem<TYPE>::T;
-  __shared__ float red[3][16 * 128];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kb = lane >> 4;
-  const int ntk = (a.K + 127) / 128, k0 = (int)(blockIdx.x % ntk) * 128, m0 = (int)(blockIdx.x / ntk) * 16;
-  const int k = min(k0 + r16 * 8, a.K - 8), g = k / a.group, KB = a.K / 2;
-  const int64_t m = min(m0 + r16, a.M - 1);
-  w4_f4 acc[8] = {};
-  for (int i = 0; i < a.nw; ++i) {
-    const T *dy = (const T *)a.dy[i] + m * a.lddy[i];
+  using F = Frag<TYPE == QC_TYPE_F32 ? QC_TYPE_BF16 : TYPE>;
+  using G = GradTile<TYPE, MI, CW, PRE>;
+  constexpr int P = G::P;
+  extern __shared__ __align__(16) char lds[];
+  const int party = __builtin_amdgcn_readfirstlane(threadIdx.x / G::TH), tid = threadIdx.x % G::TH;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, kb = lane >> 4;
+  int mi, ki;
+  tile_at(blockIdx.x, gridDim.x, tm, tk, 8, mi, ki);
+  const int m0 = mi * 16 * MI, k0 = ki * (64 * CW), KB = a.K / 2;
+  const int last = a.M - 1 - m0, ncol = (64 * CW + a.group - 1) / a.group;  // groups of the tile's columns
+  const int g0 = k0 / a.group, mine = (k0 + wave * 64 + r16 * 4) / a.group - g0;   // the lane's own
+  const int steps0 = (a.N[0] + GT_N - 1) / GT_N, steps = steps0 + (a.nw > 1 ? (a.N[1] + GT_N - 1) / GT_N : 0);
+
+  w4_u4 dyv[G::NU], wv[G::NW];
+  float sv[G::NS];
+  int zv[G::NS];
+  // scales and zero points of a step
+  const auto fetch_scales = [&](int step) {
+    const int i = step >= steps0 && a.nw > 1, n0 = (step - (i ? steps0 : 0)) * GT_N, N = a.N[i];
     const W4Mat &w = a.w[i];
-    const int N = a.N[i];
-    for (int n = wave * 4; n < N; n += 16) {
-      const size_t row = min(n + kb, N - 1);
-      const float x = n + kb < N ? W4Mem<TYPE>::get(dy[n + kb]) : 0.0f;
-      const unsigned q = *(const unsigned *)(w.q + row * KB + k / 2);
-      const float s = w.scale[row * a.G + g] * 16.0f;
-      const float z16 = w.zero ? (float)((int)w.zero[row * a.G + g] - 8) * 0.0625f : 0.0f;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, s * (w4_nibble(q >> (4 * t)) - z16), acc[t], 0, 0, 0);
+    for (int v = 0; v < G::NS; ++v) {
+      const int t = tid + G::TH * v, g = g0 + t / GT_N;                  // entries [group][row]
+      if (t < ncol * GT_N) {
+        const size_t at = (size_t)min(n0 + t % GT_N, N - 1) * a.G + min(g, a.G - 1);
+        sv[v] = w.scale[at];
+        if (ASYM) zv[v] = w.zero[at];
+      }
     }
-  }
-  if (wave) {
+  };
+  const auto put_scales = [&](float *s) {
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
+    for (int v = 0; v < G::NS; ++v) {
+      const int t = tid + G::TH * v;
+      if (t < ncol * GT_N) {
+        if (PRE) {                                                       // [row] scales, then [row] offsets
+          s[t] = sv[v] * 16.0f;
+          if (ASYM) s[GT_N + t] = (float)(zv[v] - 8) * 0.0625f;
+        } else if (ASYM) {
+          s[2 * t] = sv[v] * 16.0f;
+          s[2 * t + 1] = -(float)(zv[v] - 8) * sv[v];
+        } else {
+          s[t] = sv[v] * 16.0f;
+        }
+      }
+    }
+  };
+  const auto fetch = [&](int step) {
+    const int i = step >= steps0 && a.nw > 1, n0 = (step - (i ? steps0 : 0)) * GT_N, N = a.N[i];
+    const T *dy = (const T *)a.dy[i] + (int64_t)m0 * a.lddy[i];
+    const W4Mat &w = a.w[i];
+    const int ld = (int)a.lddy[i];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) red[wave - 1][(kb * 4 + e) * 128 + r16 * 8 + t] = acc[t][e];
+    for (int v = 0; v < G::NU; ++v) {
+      const int t = tid + G::TH * v, r = t / G::UR, n = n0 + t % G::UR * (16 / G::ES);
+      const T *p = dy + (size_t)min(r, last) * ld + n;
+      dyv[v] = w4_u4{};
+      if (n + 16 / G::ES <= N) {
+        dyv[v] = *(const typename std::conditional<G::ES == 4, w4_u4_a4, w4_u4_a2>::type *)p;
+      } else if (n < N) {
+        T e[16 / G::ES];
+#pragma unroll
+        for (int x = 0; x < 16 / G::ES; ++x) {
+          e[x] = (T)0.0f;
+          if (n + x < N) e[x] = p[x];
+        }
+        dyv[v] = __builtin_bit_cast(w4_u4, e);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < G::NW; ++v) {
+      const int t = tid + G::TH * v;
+      wv[v] = w4_load16(w.q + (size_t)min(n0 + t / G::WU, N - 1) * KB, k0 / 2 + t % G::WU * 16, KB);
+    }
+    if (!PRE) fetch_scales(step);
+  };
+  const auto put = [&](char *buf, const float *scales) {
+#pragma unroll
+    for (int v = 0; v < G::NU; ++v) {
+      const int t = tid + G::TH * v, r = t / G::UR, u = t % G::UR;
+      if constexpr (TYPE == QC_TYPE_F32) {
+        float p[4][3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w4_split(__builtin_bit_cast(w4_f4, dyv[v])[e] * (PRE ? scales[u * 4 + e] : 1.0f), p[e]);
+#pragma unroll
+        for (int s = 0; s < 3; ++s)
+          *(w4_u2 *)(buf + s * 16 * MI * 128 + gt_slot(r, u >> 1) + (u & 1) * 8) = w4_u2{w4_pack_bf16(p[0][s], p[1][s]), w4_pack_bf16(p[2][s], p[3][s])};
+      } else {
+        *(w4_u4 *)(buf + gt_slot(r, u)) = dyv[v];
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < G::NW; ++v) {
+      const int t = tid + G::TH * v;
+      char *at = buf + G::DY + t / G::WU * G::WROW + t % G::WU * 16;
+      *(w4_u2 *)at = w4_u2{wv[v][0], wv[v][1]};
+      *(w4_u2 *)(at + 8) = w4_u2{wv[v][2], wv[v][3]};
+    }
+    if (!PRE) put_scales((float *)(buf + G::DY + G::W));
+  };
+
+  w4_f4 acc[MI][4] = {};
+  char *mybuf = lds + party * (2 * G::BUF);
+  const int turns = (steps + G::S - 1) / G::S;                           // of every party: the last step of one may lie beyond the rows
+  // PRE: three tables of scales, since a step's are needed when its gradients are stored, a step before its weights are used
+  float *tables = (float *)(lds + 2 * G::S * G::BUF) + party * (3 * 2 * GT_N);
+  if (turns) {
+    if (PRE) {
+      fetch_scales(party);
+      put_scales(tables);
+      fetch_scales(G::S + party);
+      put_scales(tables + 2 * GT_N);
+      __syncthreads();
+    }
+    fetch(party);
+    put(mybuf, tables);
   }
   __syncthreads();
-  if (wave || k0 + r16 * 8 >= a.K) return;
+  int table = 0;                                                         // of the present step
+  for (int turn = 0; turn < turns; ++turn) {
+    const char *cur = mybuf + (turn & 1) * G::BUF;
+    const float *now = tables + table * (2 * GT_N);
+    if (turn + 1 < turns) fetch(G::S * (turn + 1) + party);
+    if (PRE && turn + 2 < turns) fetch_scales(G::S * (turn + 2) + party);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int row = m0 + kb * 4 + e;
-    if (row >= a.M) break;
-    T *o = (T *)a.dx + (int64_t)row * a.lddx + k;
+    for (int h = 0; h < 2; ++h) {
+      unsigned short q[8];
+      float s[8], o[8];
+      const char *wq = cur + G::DY + (h * 32 + kb * 8) * G::WROW + wave * 32 + r16 * 2;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const int at = (kb * 4 + e) * 128 + r16 * 8 + t;
-      o[t] = W4Mem<TYPE>::put(((acc[t][e] + red[0][at]) + red[1][at]) + red[2][at]);
+      for (int i = 0; i < 8; ++i) q[i] = *(const unsigned short *)(wq + i * G::WROW);
+      const float *sp = PRE ? now + GT_N + h * 32 + kb * 8 : (const float *)(cur + G::DY + G::W) + (mine * GT_N + h * 32 + kb * 8) * (ASYM ? 2 : 1);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        s[i] = PRE ? 1.0f : sp[ASYM ? 2 * i : i];
+        o[i] = !ASYM ? 0.0f : PRE ? -sp[i] : sp[2 * i + 1];
+      }
+      w4_u4 wf[PRE ? 1 : P][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {                                      // rows 2 i and 2 i + 1
+        float v[2][4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          unsigned even = q[2 * i + b], odd = even >> 4;
+          asm("" : "+v"(odd));
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const float c = w4_nibble(((t & 1 ? odd : even) >> (t & 2 ? 8 : 0)) & 0xFF);
+            v[b][t] = PRE ? (ASYM ? c + o[2 * i + b] : c) : ASYM ? fmaf(c, s[2 * i + b], o[2 * i + b]) : c * s[2 * i + b];
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          if constexpr (PRE) {
+            wf[0][t][i] = w4_pack_bf16(v[0][t], v[1][t]);
+          } else if constexpr (TYPE == QC_TYPE_F32) {
+            float p0[3], p1[3];
+            w4_split<true>(v[0][t], p0);
+            w4_split<true>(v[1][t], p1);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) wf[p][t][i] = w4_pack_bf16(p0[p], p1[p]);
+          } else {
+            typedef T T2 __attribute__((ext_vector_type(2)));
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            asm("" : "+v"(v[0][t]), "+v"(v[1][t]));                      // rounded to float32 before it is rounded to the type
+            wf[0][t][i] = __builtin_bit_cast(unsigned, __builtin_convertvector((f2{v[0][t], v[1][t]}), T2));
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const typename F::X x = *(const typename F::X *)(cur + p * 16 * MI * 128 + gt_slot(16 * i + r16, h * 4 + kb));
+#pragma unroll
+          for (int pw = 0; pw < (PRE ? 1 : P - p); ++pw)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[i][t] = F::mma(x, __builtin_bit_cast(typename F::W, wf[pw][t]), acc[i][t]);
+        }
+      }
+    }
+    const int after = table == 2 ? 0 : table + 1;
+    if (turn + 1 < turns) put(mybuf + ((turn + 1) & 1) * G::BUF, tables + after * (2 * GT_N));
+    if (PRE && turn + 2 < turns) put_scales(tables + (after == 2 ? 0 : after + 1) * (2 * GT_N));
+    table = after;
+    __syncthreads();
+  }
+
+  w4_f4 *there = (w4_f4 *)lds;
+  const auto store = [&](int row0, int k, const w4_f4 sum[4]) {
+    if (k >= a.K) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = row0 + e;
+      if (r > last) continue;
+      T *o = (T *)a.dx + (int64_t)(m0 + r) * a.lddx + k;
+      typedef T T4 __attribute__((ext_vector_type(4)));
+      T4 v;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[t] = W4Mem<TYPE>::put(sum[t][e]);
+      if ((uintptr_t)o % sizeof(T4) == 0) {
+        *(T4 *)o = v;
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) o[t] = v[t];
+      }
+    }
+  };
+  if constexpr (G::S == 2) {                     // the first party finishes the tile's upper rows, the second the lower ones
+#pragma unroll
+    for (int i = 0; i < MI / 2; ++i)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) there[(i * 4 + t) * 512 + threadIdx.x] = party ? acc[i][t] : acc[i + MI / 2][t];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MI / 2; ++i) {
+      w4_f4 sum[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const w4_f4 o = there[(i * 4 + t) * 512 + (threadIdx.x ^ 256)];
+        sum[t] = party ? o + acc[i + MI / 2][t] : acc[i][t] + o;
+      }
+      store(16 * (i + party * (MI / 2)) + kb * 4, k0 + wave * 64 + r16 * 4, sum);
+    }
+  } else {                                       // all parties' sums, in their order
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) there[(i * 4 + t) * 512 + threadIdx.x] = acc[i][t];
+    __syncthreads();
+    for (int o = threadIdx.x; o < MI * G::TH; o += 512) {
+      const int i = o / G::TH, th = o % G::TH;
+      w4_f4 sum[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        sum[t] = there[(i * 4 + t) * 512 + th];
+#pragma unroll
+        for (int p = 1; p < G::S; ++p) sum[t] += there[(i * 4 + t) * 512 + p * G::TH + th];
+      }
+      store(16 * i + (th >> 4 & 3) * 4, k0 + (th >> 6) * 64 + (th & 15) * 4, sum);
     }
   }
 }
 
-template <int TYPE>
-static void grad(const W4GradArgs &a, hipStream_t st) {
-  w4_grad_kernel<TYPE><<<(unsigned)((a.K + 127) / 128) * (unsigned)((a.M + 15) / 16), 256, 0, st>>>(a);
+template <int TYPE, int MI, int CW, bool ASYM, bool PRE>
+static hipError_t launch(const W4GradArgs &a, hipStream_t st) {
+  constexpr int lds = GradTile<TYPE, MI, CW, PRE>::LDS;
+  static_assert(lds <= 163840, "LDS of a compute unit");
+  const int64_t tm = (a.M + 16 * MI - 1) / (16 * MI), tk = (a.K + 64 * CW - 1) / (64 * CW);
+  static std::atomic<unsigned long long> done{0};
+  auto kern = w4_grad_kernel<TYPE, MI, CW, ASYM, PRE>;
+  if (lds > 65536) {
+    hipError_t e = allow_lds((const void *)kern, lds, done);
+    if (e != hipSuccess) return e;
+  }
+  kern<<<(unsigned)(tm * tk), 512, lds, st>>>(a, (int)tm, (int)tk);
+  return hipGetLastError();
+}
+
+// Tiles: row blocks, wavefronts side by side, and us of a step of all parties of a workgroup, 8 / CW * 64 rows of W (a compute unit runs one
+// workgroup at a time).  Measured at 4608 x 1152, 1152 x 4608, 8192 x 8192 and 1000 x 400, 1 - 2048 rows; the tile whose steps come to
+// least is within 20 % of the best of all there.  Few rows want many parties and narrow tiles (1 row of 4608 x 1152, bfloat16: 16.8 us;
+// tiles of 128 columns 32, of 256 columns 72), many rows tall and wide ones (2048 rows of 8192 x 8192: 300 us, 376 with 96 rows a tile).
+struct GradShape {
+  int MI, CW, group;       // group: the smallest the tile takes
+  float step;
+};
+static constexpr GradShape SHAPES_16[] = {{1, 1, 32, 1.5f}, {2, 1, 32, 1.8f}, {2, 2, 32, 1.55f}, {4, 2, 32, 1.95f}, {4, 4, 32, 2.2f}, {6, 4, 32, 2.55f}, {8, 4, 32, 2.8f}};
+// the first two with the scale in the gradients (PRE)
+static constexpr GradShape SHAPES_F32[] = {{1, 1, 64, 2.7f}, {2, 2, 128, 2.9f}, {1, 1, 32, 3.6f}, {2, 2, 32, 4.1f}, {2, 4, 32, 4.1f}, {4, 4, 32, 5.5f}};
+
+template <int N>
+static int shape(const W4GradArgs &a, const GradShape (&shapes)[N]) {
+  const int steps = (a.N[0] + GT_N - 1) / GT_N + (a.nw > 1 ? (a.N[1] + GT_N - 1) / GT_N : 0);
+  int best = -1;
+  float least = 0.0f;
+  for (int i = 0; i < N; ++i) {
+    const GradShape &s = shapes[i];
+    if (a.group < s.group) continue;
+    const int parties = 8 / s.CW;
+    const int64_t groups = (int64_t)((a.M + 16 * s.MI - 1) / (16 * s.MI)) * ((a.K + 64 * s.CW - 1) / (64 * s.CW));
+    const float t = s.step * ((steps + parties - 1) / parties) * (float)((groups + 255) / 256);
+    if (best < 0 || t < least) {
+      best = i;
+      least = t;
+    }
+  }
+  return best;
+}
+
+template <int TYPE, bool ASYM>
+static hipError_t rows(const W4GradArgs &a, hipStream_t st) {
+  if constexpr (TYPE == QC_TYPE_F32) {
+    switch (shape(a, SHAPES_F32)) {
+      case 0: return launch<TYPE, 1, 1, ASYM, true>(a, st);
+      case 1: return launch<TYPE, 2, 2, ASYM, true>(a, st);
+      case 2: return launch<TYPE, 1, 1, ASYM, false>(a, st);
+      case 3: return launch<TYPE, 2, 2, ASYM, false>(a, st);
+      case 4: return launch<TYPE, 2, 4, ASYM, false>(a, st);
+      default: return launch<TYPE, 4, 4, ASYM, false>(a, st);
+    }
+  } else {
+    switch (shape(a, SHAPES_16)) {
+      case 0: return launch<TYPE, 1, 1, ASYM, false>(a, st);
+      case 1: return launch<TYPE, 2, 1, ASYM, false>(a, st);
+      case 2: return launch<TYPE, 2, 2, ASYM, false>(a, st);
+      case 3: return launch<TYPE, 4, 2, ASYM, false>(a, st);
+      case 4: return launch<TYPE, 4, 4, ASYM, false>(a, st);
+      case 5: return launch<TYPE, 6, 4, ASYM, false>(a, st);
+      default: return launch<TYPE, 8, 4, ASYM, false>(a, st);
+    }
+  }
 }
 
 hipError_t launch_w4_grad(const W4GradArgs &a, int type, hipStream_t st) {
-  if (type == QC_TYPE_F32) grad<QC_TYPE_F32>(a, st);
-  else if (type == QC_TYPE_F16) grad<QC_TYPE_F16>(a, st);
-  else grad<QC_TYPE_BF16>(a, st);
-  return hipGetLastError();
+  const bool z = a.w[0].zero != nullptr;
+  if (type == QC_TYPE_F32) return z ? rows<QC_TYPE_F32, true>(a, st) : rows<QC_TYPE_F32, false>(a, st);
+  if (type == QC_TYPE_F16) return z ? rows<QC_TYPE_F16, true>(a, st) : rows<QC_TYPE_F16, false>(a, st);
+  return z ? rows<QC_TYPE_BF16, true>(a, st) : rows<QC_TYPE_BF16, false>(a, st);
 }
 
 }  // namespace qc
