@@ -240,6 +240,7 @@ class W4Weight:
                 raise QCError(-2, "W4Weight: a tensor of type %s and shape %s is needed" % (dtype, shape))
         self.q, self.scale, self.zero, self.sum = q, scale, zero, sum
         self.N, self.K, self.group, self.device = N, K, group, q.device
+        self.index = q.device.index if q.device.type == "cuda" else -1
         self.desc = W4WeightDesc(_p(q), _p(scale), _p(zero), _p(sum), N, K, group)
         self.ref = C.pointer(self.desc)
 
@@ -252,13 +253,16 @@ class W4Weight:
         return cls(new(N, K // 2, dtype=torch.uint8), new(N, G), group, new(N, G, dtype=torch.uint8) if asymmetric else None, new(N))
 
 
+_w4_torch = None
 _w4_types = {}
 
 
 def _w4_type(t):
-    if not _w4_types:
+    global _w4_torch
+    if _w4_torch is None:
         import torch
         _w4_types.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 3})
+        _w4_torch = torch
     code = _w4_types.get(t.dtype)
     if code is None:
         raise QCError(-7, "tensors of type %s are not supported" % t.dtype)
@@ -267,36 +271,41 @@ def _w4_type(t):
 
 def _w4_rows(t, rows, cols, dtype, device, name):
     """Leading dimension of a [rows, cols] tensor whose rows are contiguous."""
-    if t.dtype is not dtype or t.device != device:
-        raise QCError(-2, "%s: %s on %s, not %s on %s" % (name, t.dtype, t.device, dtype, device))
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (t.stride(1) != 1 and cols > 1):
-        raise QCError(-2, "%s: shape %s, strides %s; [%d, %d] with contiguous rows is needed" % (name, tuple(t.shape), t.stride(), rows, cols))
-    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    if t.dtype is dtype and t.device == device and t.shape == (rows, cols):
+        ld, one = t.stride()
+        if one == 1 or cols <= 1:
+            return ld if rows > 1 else cols
+    raise QCError(-2, "%s: %s %s with strides %s on %s; %s [%d, %d] with contiguous rows on %s is needed" % (
+        name, t.dtype, tuple(t.shape), t.stride(), t.device, dtype, rows, cols, device))
 
 
 def _w4_bias(b, w):
-    if b is not None and (b.dtype is not w.scale.dtype or b.shape != (w.N,) or not b.is_contiguous() or b.device != w.device):
+    if b is None:
+        return None
+    if b.dtype is not w.scale.dtype or b.shape != (w.N,) or not b.is_contiguous() or b.device != w.device:
         raise QCError(-2, "a bias is a contiguous float32 vector of %d elements on the weight's device" % w.N)
-    return _p(b)
+    return b.data_ptr()
 
 
 def _w4_stream(w):
-    import torch
-    dev = torch.cuda.current_device() if w.device.type == "cuda" else -1
-    if w.device.index != dev:
+    # (private functions of torch 2.10, as in _stream)
+    dev = _w4_torch.cuda.current_device() if w.index >= 0 else -2
+    if w.index != dev:
         raise QCError(-2, "the weight lies on %s, which is not the current GPU" % w.device)
-    return torch._C._cuda_getCurrentRawStream(dev)
+    return _w4_torch._C._cuda_getCurrentRawStream(dev)
 
 
 def qc_w4_quantize(w, out):
     """w [N, K] float32 / float16 / bfloat16 into the buffers of `out` (W4Weight.empty)."""
+    t = _w4_type(w)
     ld = _w4_rows(w, out.N, out.K, w.dtype, out.device, "w")
-    _chk(lib.qc_w4_quantize(_p(w), _w4_type(w), ld, out.ref, _w4_stream(out)))
+    _chk(lib.qc_w4_quantize(w.data_ptr(), t, ld, out.ref, _w4_stream(out)))
 
 
 def qc_w4_expand(w, out):
+    t = _w4_type(out)
     ld = _w4_rows(out, w.N, w.K, out.dtype, w.device, "out")
-    _chk(lib.qc_w4_expand(w.ref, _p(out), _w4_type(out), ld, _w4_stream(w)))
+    _chk(lib.qc_w4_expand(w.ref, out.data_ptr(), t, ld, _w4_stream(w)))
 
 
 def qc_w4_linear(x, w, y, bias=None, x_scale=1.0, x_zp=128):
@@ -305,7 +314,7 @@ def qc_w4_linear(x, w, y, bias=None, x_scale=1.0, x_zp=128):
     M = x.shape[0]
     ldx = _w4_rows(x, M, w.K, x.dtype, w.device, "x")
     ldy = _w4_rows(y, M, w.N, x.dtype if t != 3 else w.scale.dtype, w.device, "y")
-    _chk(lib.qc_w4_linear(_p(x), t, ldx, x_scale, x_zp, w.ref, _w4_bias(bias, w), M, _p(y), ldy, _w4_stream(w)))
+    _chk(lib.qc_w4_linear(x.data_ptr(), t, ldx, x_scale, x_zp, w.ref, _w4_bias(bias, w), M, y.data_ptr(), ldy, _w4_stream(w)))
 
 
 def qc_w4_gated(x, gate, up, h, act=QC_ACT_SILU, gate_bias=None, up_bias=None, x_scale=1.0, x_zp=128):
@@ -316,12 +325,13 @@ def qc_w4_gated(x, gate, up, h, act=QC_ACT_SILU, gate_bias=None, up_bias=None, x
     ldh = _w4_rows(h, M, gate.N, x.dtype if t != 3 else gate.scale.dtype, gate.device, "h")
     if up.device != gate.device:
         raise QCError(-2, "the weights lie on different devices")
-    _chk(lib.qc_w4_gated(_p(x), t, ldx, x_scale, x_zp, gate.ref, up.ref, _w4_bias(gate_bias, gate), _w4_bias(up_bias, up), act, M,
-                         _p(h), ldh, _w4_stream(gate)))
+    _chk(lib.qc_w4_gated(x.data_ptr(), t, ldx, x_scale, x_zp, gate.ref, up.ref, _w4_bias(gate_bias, gate), _w4_bias(up_bias, up), act, M,
+                         h.data_ptr(), ldh, _w4_stream(gate)))
 
 
 def qc_w4_linear_grad(dy, w, dx, dy2=None, w2=None):
     """dx = dy w (+ dy2 w2)."""
+    t = _w4_type(dy)
     M = dy.shape[0]
     ld = _w4_rows(dy, M, w.N, dy.dtype, w.device, "dy")
     if (dy2 is None) != (w2 is None):
@@ -330,11 +340,12 @@ def qc_w4_linear_grad(dy, w, dx, dy2=None, w2=None):
     if w2 is not None and w2.device != w.device:
         raise QCError(-2, "the weights lie on different devices")
     lddx = _w4_rows(dx, M, w.K, dy.dtype, w.device, "dx")
-    _chk(lib.qc_w4_linear_grad(_p(dy), _w4_type(dy), ld, w.ref, _p(dy2), ld2, None if w2 is None else w2.ref, M, _p(dx), lddx, _w4_stream(w)))
+    _chk(lib.qc_w4_linear_grad(dy.data_ptr(), t, ld, w.ref, _p(dy2), ld2, None if w2 is None else w2.ref, M, dx.data_ptr(), lddx, _w4_stream(w)))
 
 
 def qc_w4_gated_grad(x, gate, up, dh, dgate, dup, act=QC_ACT_SILU, gate_bias=None, up_bias=None):
     """dgate, dup: gradients of x gate^T + gate_bias and x up^T + up_bias, from dh."""
+    t = _w4_type(x)
     M = x.shape[0]
     ldx = _w4_rows(x, M, gate.K, x.dtype, gate.device, "x")
     lddh = _w4_rows(dh, M, gate.N, x.dtype, gate.device, "dh")
@@ -343,8 +354,8 @@ def qc_w4_gated_grad(x, gate, up, dh, dgate, dup, act=QC_ACT_SILU, gate_bias=Non
         raise QCError(-2, "dgate and dup have different row strides")
     if up.device != gate.device:
         raise QCError(-2, "the weights lie on different devices")
-    _chk(lib.qc_w4_gated_grad(_p(x), _w4_type(x), ldx, gate.ref, up.ref, _w4_bias(gate_bias, gate), _w4_bias(up_bias, up), act, _p(dh), lddh, M,
-                              _p(dgate), _p(dup), ldd, _w4_stream(gate)))
+    _chk(lib.qc_w4_gated_grad(x.data_ptr(), t, ldx, gate.ref, up.ref, _w4_bias(gate_bias, gate), _w4_bias(up_bias, up), act,
+                              dh.data_ptr(), lddh, M, dgate.data_ptr(), dup.data_ptr(), ldd, _w4_stream(gate)))
 
 
 def qc_ddim_schedule(steps: int):

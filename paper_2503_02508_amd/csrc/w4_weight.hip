@@ -55,15 +55,30 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const typename W4Mem<T
       s = fmaxf(hi, -lo) / 7.0f;
       if (s == 0.0f) s = 1.0f;
     }
+    // w / s by way of 1 / s, off by less than 3e-6 for |w / s| <= 15.5: only next to a half does it take the division to decide
+    const float inv = 1.0f / s;
+    float r[8];
+    bool near = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float t = v[i] * inv;
+      r[i] = rintf(t);
+      near |= !(fabsf(t - r[i]) <= 0.49999f);                            // or 1 / s is infinite
+    }
+    if (near) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = rintf(v[i] / s);
+    }
     unsigned code = 0;
     int isum = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float u = fminf(fmaxf(rintf(v[i] / s) + z, low), 15.0f);
-      const int c = (int)u;
-      isum += c - (int)z;
-      code |= (unsigned)((c - 8) & 15) << (4 * i);
+      const int c = (int)__builtin_amdgcn_fmed3f(r[i] + z, low, 15.0f);
+      isum += c;
+      code |= (unsigned)c << (4 * i);
     }
+    code ^= 0x88888888u;                                                 // u - 8 in two's complement
+    isum -= 8 * (int)z;
     if (in) {
       *(unsigned *)(q + n * (K / 2) + k / 2) = code;
       if (k % group == 0) {
@@ -83,31 +98,33 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const typename W4Mem<T
   }
 }
 
-// VEC: rows of the result start at multiples of 16 bytes
+// VEC: rows of the result start at multiples of 16 bytes, which is what a lane stores
 template <int TYPE, bool VEC>
 __global__ __launch_bounds__(256) void w4_expand_kernel(const uint8_t *q, const float *scale, const uint8_t *zero, int K, int group, int G,
                                                         typename W4Mem<TYPE>::T *out, int64_t ld) {
   using T = typename W4Mem<TYPE>::T;
-  typedef T T8 __attribute__((ext_vector_type(8)));
+  constexpr int E = 16 / sizeof(T);
+  typedef T TE __attribute__((ext_vector_type(E)));
+  typedef typename std::conditional<E == 8, unsigned, unsigned short>::type Code;
   const size_t n = blockIdx.x;
-  for (int k = threadIdx.x * 8; k < K; k += blockDim.x * 8) {
-    const unsigned code = *(const unsigned *)(q + n * (K / 2) + k / 2);
+  for (int k = threadIdx.x * E; k < K; k += blockDim.x * E) {
+    const unsigned code = *(const Code *)(q + n * (K / 2) + k / 2);
     const size_t g = n * G + k / group;
     const float s = scale[g];
     const int z = zero ? (int)zero[g] - 8 : 0;
-    T8 t;
+    TE t;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < E; ++i) {
       float v = s * (float)(((int)(code << (28 - 4 * i)) >> 28) - z);
       asm("" : "+v"(v));          // rounded to float32, then to the type: not a product that is rounded to float16 directly
       t[i] = W4Mem<TYPE>::put(v);
     }
     T *o = out + n * ld + k;
     if (VEC) {
-      *(T8 *)o = t;
+      *(TE *)o = t;
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = t[i];
+      for (int i = 0; i < E; ++i) o[i] = t[i];
     }
   }
 }
