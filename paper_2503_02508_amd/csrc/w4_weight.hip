@@ -8,35 +8,41 @@
 namespace qc {
 
 template <int TYPE>
-__device__ __forceinline__ void w4_load8(const typename W4Mem<TYPE>::T *p, float v[8]) {
-  using T = typename W4Mem<TYPE>::T;
-  typedef T T8 __attribute__((ext_vector_type(8)));
-  const T8 t = *(const T8 *)p;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = W4Mem<TYPE>::get(t[i]);
-}
+using W4Eight = typename W4Mem<TYPE>::T __attribute__((ext_vector_type(8)));
 
+// a value of the other lanes of a group, by data-parallel primitives: the neighbour, the pair beside, the quad beside, the eight beside
+template <int CTRL>
+__device__ __forceinline__ float w4_beside(float v) {
+  const int b = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, CTRL, 0xF, 0xF, false));
+}
 // minimum / maximum over 4, 8 or 16 neighbouring lanes, in each of them
 template <bool MAX>
 __device__ __forceinline__ float w4_group_reduce(float v, int lanes) {
-  for (int m = 1; m < lanes; m <<= 1) {
-    const float o = __shfl_xor(v, m);
-    v = MAX ? fmaxf(v, o) : fminf(v, o);
-  }
+  const auto with = [&](float o) { v = MAX ? fmaxf(v, o) : fminf(v, o); };
+  with(w4_beside<0xB1>(v));      // quad_perm [1, 0, 3, 2]
+  with(w4_beside<0x4E>(v));      // quad_perm [2, 3, 0, 1]
+  if (lanes > 4) with(w4_beside<0x141>(v));      // row_half_mirror
+  if (lanes > 8) with(w4_beside<0x140>(v));      // row_mirror
   return v;
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(256) void w4_quantize_kernel(const typename W4Mem<TYPE>::T *w, int64_t ld, int K, int group, int G, uint8_t *q,
+__global__ __launch_bounds__(256) void w4_quantize_kernel(const typename W4Mem<TYPE>::T *w, int64_t ld, int K, int group, int shift, int G, uint8_t *q,
                                                           float *scale, uint8_t *zero, float *sum) {
   __shared__ double part[4];
   const size_t n = blockIdx.x;
   const int lanes = group / 8, KR = (K + 127) / 128 * 128;       // whole groups, so that all lanes of one take part
   double total = 0.0;
+  W4Eight<TYPE> next = {};
+  if ((int)threadIdx.x * 8 < K) next = *(const W4Eight<TYPE> *)(w + n * ld + threadIdx.x * 8);
   for (int k = threadIdx.x * 8; k < KR; k += blockDim.x * 8) {
-    float v[8] = {};
     const bool in = k < K;
-    if (in) w4_load8<TYPE>(w + n * ld + k, v);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = in ? W4Mem<TYPE>::get(next[i]) : 0.0f;
+    const int kn = k + blockDim.x * 8;
+    if (kn < K) next = *(const W4Eight<TYPE> *)(w + n * ld + kn);
     float lo = fminf(v[0], 0.0f), hi = fmaxf(v[0], 0.0f);
 #pragma unroll
     for (int i = 1; i < 8; ++i) {
@@ -45,46 +51,43 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const typename W4Mem<T
     }
     lo = w4_group_reduce<false>(lo, lanes);
     hi = w4_group_reduce<true>(hi, lanes);
-    float s, z = 8.0f, low = 1.0f;
-    if (zero) {
-      s = (hi - lo) / 15.0f;
-      if (s == 0.0f) s = 1.0f;
-      z = fminf(fmaxf(rintf(-lo / s), 0.0f), 15.0f);
-      low = 0.0f;
-    } else {
-      s = fmaxf(hi, -lo) / 7.0f;
-      if (s == 0.0f) s = 1.0f;
-    }
-    // w / s by way of 1 / s, off by less than 3e-6 for |w / s| <= 15.5: only next to a half does it take the division to decide
-    const float inv = 1.0f / s;
-    float r[8];
-    bool near = false;
+    // w / s by way of 1 / s, off by less than 4e-6 for |w / s| <= 15.5: only next to a half (or where 1 / s is infinite) does it take
+    // the division to decide
+    float s = zero ? (hi - lo) / 15.0f : fmaxf(hi, -lo) / 7.0f;
+    if (s == 0.0f) s = 1.0f;
+    const float inv = __builtin_amdgcn_rcpf(s);
+    float r[8], z = 8.0f, off = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float t = v[i] * inv;
       r[i] = rintf(t);
-      near |= !(fabsf(t - r[i]) <= 0.49999f);                            // or 1 / s is infinite
+      off = fmaxf(off, fabsf(t - r[i]));
     }
-    if (near) {
+    if (zero) {
+      const float t = -lo * inv;
+      z = rintf(t);
+      off = fmaxf(off, fabsf(t - z));
+    }
+    if (off > 0.49999f || !(inv < 3.0e38f)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) r[i] = rintf(v[i] / s);
+      if (zero) z = rintf(-lo / s);
     }
-    unsigned code = 0;
-    int isum = 0;
+    z = fminf(fmaxf(z, 0.0f), 15.0f);
+    const float low = (zero ? 0.0f : 1.0f) - z, high = 15.0f - z;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = (int)__builtin_amdgcn_fmed3f(r[i] + z, low, 15.0f);
-      isum += c;
-      code |= (unsigned)c << (4 * i);
-    }
-    code ^= 0x88888888u;                                                 // u - 8 in two's complement
-    isum -= 8 * (int)z;
+    for (int i = 0; i < 8; ++i) r[i] = __builtin_amdgcn_fmed3f(r[i], low, high);
+    // four codes as one number below 65536, exact in float32; their sum is at most 60
+    const auto four = [&](const float *c) { return (unsigned)fmaf(fmaf(fmaf(c[3], 16.0f, c[2]), 16.0f, c[1]), 16.0f, fmaf(z, 4369.0f, c[0])); };
+    const unsigned code = (four(r) | four(r + 4) << 16) ^ 0x88888888u;   // u - 8 in two's complement
     if (in) {
       *(unsigned *)(q + n * (K / 2) + k / 2) = code;
-      if (k % group == 0) {
-        scale[n * G + k / group] = s;
-        if (zero) zero[n * G + k / group] = (uint8_t)z;
+      if ((k & (group - 1)) == 0) {
+        const size_t at = n * G + (k >> shift);
+        scale[at] = s;
+        if (zero) zero[at] = (uint8_t)z;
       }
+      const float isum = ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7]));
       total += (double)s * (double)isum;
     }
   }
@@ -100,7 +103,7 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const typename W4Mem<T
 
 // VEC: rows of the result start at multiples of 16 bytes, which is what a lane stores
 template <int TYPE, bool VEC>
-__global__ __launch_bounds__(256) void w4_expand_kernel(const uint8_t *q, const float *scale, const uint8_t *zero, int K, int group, int G,
+__global__ __launch_bounds__(256) void w4_expand_kernel(const uint8_t *q, const float *scale, const uint8_t *zero, int K, int shift, int G,
                                                         typename W4Mem<TYPE>::T *out, int64_t ld) {
   using T = typename W4Mem<TYPE>::T;
   constexpr int E = 16 / sizeof(T);
@@ -109,7 +112,7 @@ __global__ __launch_bounds__(256) void w4_expand_kernel(const uint8_t *q, const 
   const size_t n = blockIdx.x;
   for (int k = threadIdx.x * E; k < K; k += blockDim.x * E) {
     const unsigned code = *(const Code *)(q + n * (K / 2) + k / 2);
-    const size_t g = n * G + k / group;
+    const size_t g = n * G + (k >> shift);
     const float s = scale[g];
     const int z = zero ? (int)zero[g] - 8 : 0;
     TE t;
@@ -134,7 +137,7 @@ static int row_threads(int K) { return std::min(256, ((K + 127) / 128 * 16 + 63)
 template <int TYPE>
 static void quantize(const void *w, int64_t ld, const qc_w4_weight &o, hipStream_t st) {
   const int G = (o.K + o.group - 1) / o.group;
-  w4_quantize_kernel<TYPE><<<o.N, row_threads(o.K), 0, st>>>((const typename W4Mem<TYPE>::T *)w, ld, o.K, o.group, G, (uint8_t *)o.q, o.scale,
+  w4_quantize_kernel<TYPE><<<o.N, row_threads(o.K), 0, st>>>((const typename W4Mem<TYPE>::T *)w, ld, o.K, o.group, __builtin_ctz(o.group), G, (uint8_t *)o.q, o.scale,
                                                             o.zero, o.sum);
 }
 
@@ -151,7 +154,7 @@ static void expand(const qc_w4_weight &w, void *out, int64_t ld, hipStream_t st)
   const int G = (w.K + w.group - 1) / w.group;
   const bool vec = (uintptr_t)out % 16 == 0 && ld * sizeof(T) % 16 == 0;
   auto kern = vec ? w4_expand_kernel<TYPE, true> : w4_expand_kernel<TYPE, false>;
-  kern<<<w.N, row_threads(w.K), 0, st>>>((const uint8_t *)w.q, w.scale, w.zero, w.K, w.group, G, (T *)out, ld);
+  kern<<<w.N, row_threads(w.K), 0, st>>>((const uint8_t *)w.q, w.scale, w.zero, w.K, __builtin_ctz(w.group), G, (T *)out, ld);
 }
 
 hipError_t launch_w4_expand(const qc_w4_weight &w, void *out, int type, int64_t ld, hipStream_t st) {
