@@ -58,17 +58,25 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
   w4_u4 dyv[G::NU], wv[G::NW];
   float sv[G::NS];
   int zv[G::NS];
-  // scales and zero points of a step
+  // Where a step lies: its weight, first row of W and how many are left.  Codes, scales and zero points beyond the last row read as
+  // zero; what is read beyond a row's end belongs to columns that are not stored.
+  const auto where = [&](int step, bool &second, int &n0) {
+    second = step >= steps0 && a.nw > 1;
+    n0 = (step - (second ? steps0 : 0)) * GT_N;
+    return (second ? a.N[1] : a.N[0]) - n0;
+  };
   const auto fetch_scales = [&](int step) {
-    const int i = step >= steps0 && a.nw > 1, n0 = (step - (i ? steps0 : 0)) * GT_N, N = a.N[i];
-    const W4Mat &w = a.w[i];
+    bool second;
+    int n0;
+    const int left = where(step, second, n0);
+    const __amdgpu_buffer_rsrc_t sb = w4_buffer((second ? a.w[1].scale : a.w[0].scale) + ((size_t)n0 * a.G + g0), ((int64_t)left * a.G - g0) * 4);
+    const __amdgpu_buffer_rsrc_t zb = w4_buffer((second ? a.w[1].zero : a.w[0].zero) + ((size_t)n0 * a.G + g0), (int64_t)left * a.G - g0);
 #pragma unroll
     for (int v = 0; v < G::NS; ++v) {
-      const int t = tid + G::TH * v, g = g0 + t / GT_N;                  // entries [group][row]
+      const int t = tid + G::TH * v, at = t % GT_N * a.G + t / GT_N;     // entries [group][row]
       if (t < ncol * GT_N) {
-        const size_t at = (size_t)min(n0 + t % GT_N, N - 1) * a.G + min(g, a.G - 1);
-        sv[v] = w.scale[at];
-        if (ASYM) zv[v] = w.zero[at];
+        sv[v] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sb, at * 4, 0, 0));
+        if (ASYM) zv[v] = __builtin_amdgcn_raw_buffer_load_b8(zb, at, 0, 0);
       }
     }
   };
@@ -90,31 +98,37 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
     }
   };
   const auto fetch = [&](int step) {
-    const int i = step >= steps0 && a.nw > 1, n0 = (step - (i ? steps0 : 0)) * GT_N, N = a.N[i];
-    const T *dy = (const T *)a.dy[i] + (int64_t)m0 * a.lddy[i];
-    const W4Mat &w = a.w[i];
-    const int ld = (int)a.lddy[i];
+    bool second;
+    int n0;
+    const int left = where(step, second, n0);
+    const int64_t ld = second ? a.lddy[1] : a.lddy[0];
+    const int row_bytes = (int)ld * G::ES;
+    const char *dy = (const char *)(second ? a.dy[1] : a.dy[0]) + ((int64_t)m0 * ld + n0) * G::ES;
+    if (left >= GT_N) {
 #pragma unroll
-    for (int v = 0; v < G::NU; ++v) {
-      const int t = tid + G::TH * v, r = t / G::UR, n = n0 + t % G::UR * (16 / G::ES);
-      const T *p = dy + (size_t)min(r, last) * ld + n;
-      dyv[v] = w4_u4{};
-      if (n + 16 / G::ES <= N) {
-        dyv[v] = *(const typename std::conditional<G::ES == 4, w4_u4_a4, w4_u4_a2>::type *)p;
-      } else if (n < N) {
+      for (int v = 0; v < G::NU; ++v) {
+        const int t = tid + G::TH * v, r = t / G::UR, u = t % G::UR;
+        dyv[v] = *(const typename std::conditional<G::ES == 4, w4_u4_a4, w4_u4_a2>::type *)(dy + (unsigned)(min(r, last) * row_bytes + u * 16));
+      }
+    } else {                                     // the last rows of W: zero beyond them
+#pragma unroll
+      for (int v = 0; v < G::NU; ++v) {
+        const int t = tid + G::TH * v, r = t / G::UR, n = t % G::UR * (16 / G::ES);
+        const T *p = (const T *)(dy + (unsigned)(min(r, last) * row_bytes)) + n;
         T e[16 / G::ES];
 #pragma unroll
         for (int x = 0; x < 16 / G::ES; ++x) {
           e[x] = (T)0.0f;
-          if (n + x < N) e[x] = p[x];
+          if (n + x < left) e[x] = p[x];
         }
         dyv[v] = __builtin_bit_cast(w4_u4, e);
       }
     }
+    const __amdgpu_buffer_rsrc_t qb = w4_buffer((second ? a.w[1].q : a.w[0].q) + ((size_t)n0 * KB + k0 / 2), (int64_t)left * KB - k0 / 2);
 #pragma unroll
     for (int v = 0; v < G::NW; ++v) {
       const int t = tid + G::TH * v;
-      wv[v] = w4_load16(w.q + (size_t)min(n0 + t / G::WU, N - 1) * KB, k0 / 2 + t % G::WU * 16, KB);
+      wv[v] = __builtin_bit_cast(w4_u4, __builtin_amdgcn_raw_buffer_load_b128(qb, t / G::WU * KB + t % G::WU * 16, 0, 0));
     }
     if (!PRE) fetch_scales(step);
   };
@@ -211,16 +225,23 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
           }
         }
       }
+      // the operands of a row block are read while the products of the one before run
+      typename F::X x[2][P];
+      const auto read = [&](int i) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) x[i & 1][p] = *(const typename F::X *)(cur + p * 16 * MI * 128 + gt_slot(16 * i + r16, h * 4 + kb));
+      };
+      read(0);
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
+        if (i + 1 < MI) read(i + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const typename F::X x = *(const typename F::X *)(cur + p * 16 * MI * 128 + gt_slot(16 * i + r16, h * 4 + kb));
+        for (int p = 0; p < P; ++p)
 #pragma unroll
           for (int pw = 0; pw < (PRE ? 1 : P - p); ++pw)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) acc[i][t] = F::mma(x, __builtin_bit_cast(typename F::W, wf[pw][t]), acc[i][t]);
-        }
+            for (int t = 0; t < 4; ++t) acc[i][t] = F::mma(x[i & 1][p], __builtin_bit_cast(typename F::W, wf[pw][t]), acc[i][t]);
       }
     }
     const int after = table == 2 ? 0 : table + 1;
@@ -323,7 +344,7 @@ static int shape(const W4GradArgs &a, const GradShape (&shapes)[N]) {
     if (a.group < s.group) continue;
     const int parties = 8 / s.CW;
     const int64_t groups = (int64_t)((a.M + 16 * s.MI - 1) / (16 * s.MI)) * ((a.K + 64 * s.CW - 1) / (64 * s.CW));
-    const float t = s.step * ((steps + parties - 1) / parties) * (float)((groups + 255) / 256);
+    const float t = (3.0f + s.step * ((steps + parties - 1) / parties)) * (float)((groups + 255) / 256);     // 3 us: first loads, last stores
     if (best < 0 || t < least) {
       best = i;
       least = t;
