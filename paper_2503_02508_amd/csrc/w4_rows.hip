@@ -26,14 +26,19 @@ struct RowsX {                                                           // a la
   }
 };
 
+// wavefronts of a workgroup at most: 16 where 128 registers hold a wavefront's tile
+constexpr int rows_most(int type, int MT, int NW) { return type == QC_TYPE_F32 || MT * NW > 2 ? 8 : 16; }
+
 // GC: groups in a chunk of 128 inputs; MT: tiles of 16 rows; NT: of 16 columns (of each matrix)
 // PULL: inputs are loaded like weight rows, four lanes a row, and pulled into place (a few rows cost less as they are)
 template <int TYPE, int GC, int MT, int NT, int OP, bool ASYM, bool PULL>
-__global__ __launch_bounds__(MT * NT > 2 ? 512 : 1024) void w4_rows_kernel(W4Args a) {
+__global__ __launch_bounds__(64 * rows_most(TYPE, MT, NT * (OP == W4_LINEAR ? 1 : 2))) void w4_rows_kernel(W4Args a) {
   using F = FragOf<TYPE>;
   using T = typename W4Mem<TYPE>::T;
   constexpr int P = TYPE == QC_TYPE_F32 ? 3 : 1, ES = RowsX<TYPE>::ES, MATS = OP == W4_LINEAR ? 1 : 2, NW = MATS * NT;
-  constexpr int AHEAD = MT == 1 ? 2 : 1;         // chunks whose inputs are asked for before they are needed
+  constexpr int AHEAD = MT == 1 ? 2 : 1;         // chunks asked for before they are needed
+  constexpr bool LATE = TYPE == QC_TYPE_F32 && MT > 1;                  // inputs a product ahead only: a chunk's are 32 MT registers
+  constexpr int XJ = LATE ? 2 : 4;
   extern __shared__ float red[];                 // [wavefronts][NW][MT][64][4]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int r16 = lane & 15, kb = lane >> 4;
@@ -60,25 +65,27 @@ __global__ __launch_bounds__(MT * NT > 2 ? 512 : 1024) void w4_rows_kernel(W4Arg
 
   struct Slot {
     w4_u4 q[NW];
-    typename RowsX<TYPE>::X x[MT][4];
+    typename RowsX<TYPE>::X x[MT][XJ];
   } slot[AHEAD];
   constexpr int PER = 4 / GC;                    // chunks to four groups
   unsigned s4[NW], z4[NW];
   w4_f4 y[NW][MT] = {};
+  const auto fetch_x = [&](Slot &f, int c, int j) {
+    const bool in = c * 128 + j * 32 + (PULL ? lane & 3 : kb) * 8 < a.K;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) f.x[i][j % XJ] = RowsX<TYPE>::load(xb, in ? xat[i] + j * 32 * ES : W4_NOWHERE, c * 128 * ES);
+  };
   const auto fetch = [&](Slot &f, int c) {
 #pragma unroll
     for (int w = 0; w < NW; ++w) f.q[w] = __builtin_bit_cast(w4_u4, __builtin_amdgcn_raw_buffer_load_b128(qb[w / NT], qat[w % NT], c * 64, 0));
     if ((c + 1) * 128 <= a.K) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < (LATE ? 1 : 4); ++j)
 #pragma unroll
         for (int i = 0; i < MT; ++i) f.x[i][j] = RowsX<TYPE>::load(xb, xat[i] + j * 32 * ES, c * 128 * ES);
     } else {                                     // a row's end is not the buffer's
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-          f.x[i][j] = RowsX<TYPE>::load(xb, c * 128 + j * 32 + (PULL ? lane & 3 : kb) * 8 < a.K ? xat[i] + j * 32 * ES : W4_NOWHERE, c * 128 * ES);
+      for (int j = 0; j < (LATE ? 1 : 4); ++j) fetch_x(f, c, j);
     }
   };
   const auto fetch4 = [&](int c) {               // scales and zero points of the four groups that chunk c's are among
@@ -111,39 +118,37 @@ __global__ __launch_bounds__(MT * NT > 2 ? 512 : 1024) void w4_rows_kernel(W4Arg
 #pragma unroll
       for (int t = 0; t < 4 / GC; ++t) {
         const int j = g * (4 / GC) + t;
-        if (PULL) {
+        if (LATE && j < 3) fetch_x(f, c, j + 1);
+        typename F::W wf[NW];
 #pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            typedef unsigned XU __attribute__((ext_vector_type(2 * ES)));
-            XU v = __builtin_bit_cast(XU, f.x[i][j]);
-#pragma unroll
-            for (int e = 0; e < 2 * ES; ++e) v[e] = w4_pull(v[e], from);
-            f.x[i][j] = __builtin_bit_cast(typename RowsX<TYPE>::X, v);
-          }
-        }
-        typename F::X xf[MT][P];
+        for (int w = 0; w < NW; ++w)
+          wf[w] = F::template weights<ASYM>(f.q[w][j], ASYM ? (float)(z[w][g] - 8) * 0.0625f : 0.0f, ASYM ? (unsigned)z[w][g] * 0x01010101u : 0u);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
+          typename RowsX<TYPE>::X x = f.x[i][j % XJ];
+          if (PULL) {
+            typedef unsigned XU __attribute__((ext_vector_type(2 * ES)));
+            XU v = __builtin_bit_cast(XU, x);
+#pragma unroll
+            for (int e = 0; e < 2 * ES; ++e) v[e] = w4_pull(v[e], from);
+            x = __builtin_bit_cast(typename RowsX<TYPE>::X, v);
+          }
+          typename F::X xf[P];
           if constexpr (TYPE == QC_TYPE_F32) {
             float p[8][3];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w4_split(f.x[i][j][e], p[e]);
+            for (int e = 0; e < 8; ++e) w4_split(x[e], p[e]);
 #pragma unroll
             for (int s = 0; s < 3; ++s)
-              xf[i][s] = __builtin_bit_cast(w4_bf8, w4_u4{w4_pack_bf16(p[0][s], p[1][s]), w4_pack_bf16(p[2][s], p[3][s]),
-                                                          w4_pack_bf16(p[4][s], p[5][s]), w4_pack_bf16(p[6][s], p[7][s])});
+              xf[s] = __builtin_bit_cast(w4_bf8, w4_u4{w4_pack_bf16(p[0][s], p[1][s]), w4_pack_bf16(p[2][s], p[3][s]),
+                                                       w4_pack_bf16(p[4][s], p[5][s]), w4_pack_bf16(p[6][s], p[7][s])});
           } else {
-            xf[i][0] = f.x[i][j];
+            xf[0] = x;
           }
-        }
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-          const float z16 = ASYM ? (float)(z[w][g] - 8) * 0.0625f : 0.0f;
-          const typename F::W wf = F::template weights<ASYM>(f.q[w][j], z16, ASYM ? (unsigned)z[w][g] * 0x01010101u : 0u);
 #pragma unroll
           for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) acc[w][i] = F::mma(xf[i][p], wf, acc[w][i]);
+            for (int w = 0; w < NW; ++w) acc[w][i] = F::mma(xf[p], wf[w], acc[w][i]);
         }
       }
 #pragma unroll
@@ -217,8 +222,8 @@ __global__ __launch_bounds__(MT * NT > 2 ? 512 : 1024) void w4_rows_kernel(W4Arg
 }
 
 // wavefronts of a workgroup: up to 16 (8 of the larger tiles), no more than chunks (pairs of chunks) and than fill the chip
-static int rows_waves(const W4Args &a, int MT, int NW, int groups) {
-  const int chunks = (a.K + 127) / 128, turns = MT == 1 ? (chunks + 1) / 2 : chunks, most = MT * NW > 2 ? 8 : 16;
+static int rows_waves(const W4Args &a, int type, int MT, int NW, int groups) {
+  const int chunks = (a.K + 127) / 128, turns = MT == 1 ? (chunks + 1) / 2 : chunks, most = rows_most(type, MT, NW);
   int waves = 1;
   while (waves < most && waves < turns && groups * waves < 4096) waves *= 2;
   return waves;
@@ -227,7 +232,7 @@ static int rows_waves(const W4Args &a, int MT, int NW, int groups) {
 template <int TYPE, int GC, int MT, int NW, int OP, bool PULL>
 static hipError_t rows_launch(const W4Args &a, hipStream_t st) {
   constexpr int NT = NW / (OP == W4_LINEAR ? 1 : 2);
-  const int ntn = (a.N + 16 * NT - 1) / (16 * NT), ntm = (a.M + 16 * MT - 1) / (16 * MT), waves = rows_waves(a, MT, NW, ntn * ntm);
+  const int ntn = (a.N + 16 * NT - 1) / (16 * NT), ntm = (a.M + 16 * MT - 1) / (16 * MT), waves = rows_waves(a, TYPE, MT, NW, ntn * ntm);
   const int lds = waves * NW * MT * 1024;
   static std::atomic<unsigned long long> done[2];
   auto kern = a.w[0].zero ? w4_rows_kernel<TYPE, GC, MT, NT, OP, true, PULL> : w4_rows_kernel<TYPE, GC, MT, NT, OP, false, PULL>;
@@ -240,25 +245,36 @@ static hipError_t rows_launch(const W4Args &a, hipStream_t st) {
 }
 
 // Tiles of this kernel, MT row blocks by NW column blocks of both matrices, and what a step (a chunk of every wavefront of a workgroup)
-// of theirs takes in us, measured with bfloat16 and groups of 128 at 4608 x 1152, 1152 x 4608, 8192 x 8192 and 2000 x 1040, 1 - 512
-// rows: alone, and for each 16 (8 of the larger tiles) wavefronts a compute unit has to run.  A launch takes the tile whose steps
-// come to least; against the best of all tiles that loses 18 % at most and mostly nothing.
+// of theirs takes in us: alone, and for each 8 or 16 wavefronts (rows_most) that a compute unit has to run.  And what a chunk takes the
+// kernel of large tiles (w4_tile.hip), alone and with every compute unit holding as many of its workgroups as fit, `full_at` in all.
+// Measured with groups of 128 at 4608 x 1152, 1152 x 4608 and 8192 x 8192, 1 - 512 rows and, the large tiles, 4096 and 8192.  A
+// launch takes what comes to least; against the best there that loses up to a fifth, and mostly nothing.
 struct RowsTile {
   int MT, NW;
   float alone, full;
 };
-static constexpr RowsTile ROWS_TILES[] = {{1, 1, 0.7f, 1.2f}, {1, 2, 0.9f, 2.0f}, {2, 2, 1.9f, 1.4f}, {4, 2, 2.3f, 2.6f}, {4, 4, 3.7f, 4.0f}};
+struct RowsCosts {
+  int tiles;
+  RowsTile tile[5];
+  float alone, full;
+  int full_at;
+};
+static constexpr RowsCosts COSTS_16 = {5, {{1, 1, 0.7f, 1.2f}, {1, 2, 0.9f, 2.0f}, {2, 2, 1.9f, 1.4f}, {4, 2, 2.3f, 2.6f}, {4, 4, 3.7f, 4.0f}}, 2.0f, 2.8f, 512};
+static constexpr RowsCosts COSTS_F32 = {4, {{1, 1, 1.5f, 1.75f}, {1, 2, 1.8f, 2.1f}, {2, 2, 3.8f, 3.4f}, {4, 2, 6.2f, 6.6f}}, 3.4f, 3.9f, 256};
+static constexpr RowsCosts COSTS_I8 = {5, {{1, 1, 0.7f, 0.95f}, {1, 2, 0.9f, 1.6f}, {2, 2, 1.3f, 1.15f}, {4, 2, 1.9f, 2.0f}, {4, 4, 3.2f, 3.3f}}, 1.8f, 2.9f, 512};
+static const RowsCosts &rows_costs(int type) { return type == QC_TYPE_F32 ? COSTS_F32 : type == QC_TYPE_I8 ? COSTS_I8 : COSTS_16; }
 
-static float rows_time(const W4Args &a, int op, const RowsTile &t) {
+static float rows_time(const W4Args &a, int type, int op, const RowsTile &t) {
   const int cols = 16 * t.NW / (op == W4_LINEAR ? 1 : 2), groups = ((a.N + cols - 1) / cols) * ((a.M + 16 * t.MT - 1) / (16 * t.MT));
-  const int waves = rows_waves(a, t.MT, t.NW, groups), chunks = (a.K + 127) / 128, steps = (chunks + waves - 1) / waves;
-  return steps * std::max(t.alone, t.full * groups * waves / (256.0f * (t.MT * t.NW > 2 ? 8 : 16)));
+  const int waves = rows_waves(a, type, t.MT, t.NW, groups), chunks = (a.K + 127) / 128, steps = (chunks + waves - 1) / waves;
+  return steps * std::max(t.alone, t.full * groups * waves / (256.0f * rows_most(type, t.MT, t.NW)));
 }
 
-static int rows_tile(const W4Args &a, int op, float &time) {
+static int rows_tile(const W4Args &a, int type, int op, float &time) {
+  const RowsCosts &c = rows_costs(type);
   int best = -1;
-  for (int i = op == W4_LINEAR ? 0 : 1; i < 5; ++i) {
-    const float t = rows_time(a, op, ROWS_TILES[i]);
+  for (int i = op == W4_LINEAR ? 0 : 1; i < c.tiles; ++i) {              // the gated block has two column blocks at least
+    const float t = rows_time(a, type, op, c.tile[i]);
     if (best < 0 || t < time) {
       best = i;
       time = t;
@@ -267,26 +283,27 @@ static int rows_tile(const W4Args &a, int op, float &time) {
   return best;
 }
 
-// The kernel of large tiles (w4_tile.hip) takes 2 us a chunk while a compute unit has one of its workgroups, and 2.8 for two.
 bool w4_tile_pays(const W4Args &a, int type, int op) {
   float rows;
-  rows_tile(a, op, rows);
+  rows_tile(a, type, op, rows);
+  const RowsCosts &c = rows_costs(type);
   const int tr = w4_tile_rows(a, type), tc = op == W4_LINEAR ? 256 : 128;
   const float tiles = (float)((a.M + tr - 1) / tr) * (float)((a.N + tc - 1) / tc);
-  return (a.K + 127) / 128 * std::max(2.0f, 2.8f * tiles / 512.0f) < rows;
+  return (a.K + 127) / 128 * std::max(c.alone, c.full * tiles / c.full_at) < rows;
 }
 
 template <int TYPE, int GC, int OP>
 static hipError_t rows_mt(const W4Args &a, hipStream_t st) {
   float time;
-  const int i = rows_tile(a, OP, time);
+  const int i = rows_tile(a, TYPE, OP, time);
   const bool pull = a.M > 4;       // 8192 x 8192, bfloat16: 11.7 us without and 12.1 with at 4 rows, 12.8 and 12.6 at 8
   if constexpr (OP == W4_LINEAR)
     if (i == 0) return pull ? rows_launch<TYPE, GC, 1, 1, OP, true>(a, st) : rows_launch<TYPE, GC, 1, 1, OP, false>(a, st);
   if (i == 1) return pull ? rows_launch<TYPE, GC, 1, 2, OP, true>(a, st) : rows_launch<TYPE, GC, 1, 2, OP, false>(a, st);
   if (i == 2) return rows_launch<TYPE, GC, 2, 2, OP, true>(a, st);
-  if (i == 3) return rows_launch<TYPE, GC, 4, 2, OP, true>(a, st);
-  return rows_launch<TYPE, GC, 4, 4, OP, true>(a, st);
+  if constexpr (TYPE != QC_TYPE_F32)
+    if (i == 4) return rows_launch<TYPE, GC, 4, 4, OP, true>(a, st);
+  return rows_launch<TYPE, GC, 4, 2, OP, true>(a, st);
 }
 
 template <int TYPE, int OP>
