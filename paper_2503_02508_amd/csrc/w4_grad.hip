@@ -13,21 +13,26 @@ namespace qc {
 
 constexpr int GT_N = 64;                       // rows of W a step
 
-// MI: blocks of 16 rows; CW: wavefronts side by side, 64 columns each; the workgroup's eight wavefronts are 8 / CW such parties
+// MI: blocks of 16 rows; CW: wavefronts side by side, 64 columns each; the workgroup's WV wavefronts are WV / CW such parties.  A party of
+// one wavefront (SOLO) has its part of LDS to itself: it needs no barrier and no second buffer, and the smallest tile has registers
+// left to ask for its steps two ahead.
 template <int TYPE, int MI, int CW, bool PRE>
 struct GradTile {
   static constexpr int P = TYPE == QC_TYPE_F32 ? 3 : 1;
   static constexpr int ES = TYPE == QC_TYPE_F32 ? 4 : 2;
-  static constexpr int S = 8 / CW, TH = 64 * CW;                         // parties, threads of one
+  static constexpr bool SOLO = CW == 1;
+  static constexpr int AHEAD = SOLO && MI == 1 && TYPE != QC_TYPE_F32 ? 2 : 1;
+  static constexpr int WV = AHEAD == 2 ? 16 : 8, BUFS = SOLO ? 1 : 2;
+  static constexpr int S = WV / CW, TH = 64 * CW;                        // parties, threads of one
   static constexpr int WROW = 32 * CW + 8;                               // bytes between rows of packed codes in LDS: four rows 8 apart share no bank
   static constexpr int GR = CW < 2 ? 2 : 2 * CW;                         // groups of up to 64 CW columns
   static constexpr int DY = 16 * MI * 128 * P;                           // bytes: planes of 16 MI rows of 64 gradients
   static constexpr int W = GT_N * WROW;
   static constexpr int BUF = DY + W + (PRE ? 0 : GR * GT_N * 8);         // and (scale, offset) of every row and group
-  // two buffers a party; afterwards the sums, of two parties only the half that the other finishes
-  static constexpr int SUMS = (S == 2 ? MI / 2 : MI) * 4 * 512 * 16;
+  // buffers of all parties; afterwards the sums, of two parties only the half that the other finishes
+  static constexpr int SUMS = (S == 2 ? MI / 2 : MI) * 4 * 64 * WV * 16;
   static constexpr int TABLES = PRE ? S * 3 * 2 * GT_N * 4 : 0;
-  static constexpr int LDS = 2 * S * BUF + TABLES > SUMS ? 2 * S * BUF + TABLES : SUMS;
+  static constexpr int LDS = BUFS * S * BUF + TABLES > SUMS ? BUFS * S * BUF + TABLES : SUMS;
   static constexpr int UR = GT_N * ES / 16, NU = 16 * MI * UR / TH;
   static constexpr int WU = 2 * CW, NW = GT_N * WU / TH;                 // units of a row of codes, a thread's
   static constexpr int NS = GR * GT_N / TH;
@@ -40,7 +45,7 @@ __device__ __forceinline__ int gt_slot(int r, int u) { return r * 128 + ((u ^ ((
 // PRE (float32): the tile's columns lie in one group, so that the scale of a weight row multiplies the gradients as they go to LDS, and the
 // weights are exact codes: three products for six, and nothing of the weights to split
 template <int TYPE, int MI, int CW, bool ASYM, bool PRE>
-__global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, int tk) {
+__global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_grad_kernel(W4GradArgs a, int tm, int tk) {
   using T = typename W4Mem<TYPE>::T;
   using F = Frag<TYPE == QC_TYPE_F32 ? QC_TYPE_BF16 : TYPE>;
   using G = GradTile<TYPE, MI, CW, PRE>;
@@ -55,9 +60,11 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
   const int g0 = k0 / a.group, mine = (k0 + wave * 64 + r16 * 4) / a.group - g0;   // the lane's own
   const int steps0 = (a.N[0] + GT_N - 1) / GT_N, steps = steps0 + (a.nw > 1 ? (a.N[1] + GT_N - 1) / GT_N : 0);
 
-  w4_u4 dyv[G::NU], wv[G::NW];
-  float sv[G::NS];
-  int zv[G::NS];
+  struct Stage {                                 // a step on its way to LDS
+    w4_u4 dy[G::NU], w[G::NW];
+    float s[G::NS];
+    int z[G::NS];
+  } stage[G::AHEAD];
   // Where a step lies: its weight, first row of W and how many are left.  Codes, scales and zero points beyond the last row read as
   // zero; what is read beyond a row's end belongs to columns that are not stored.
   const auto where = [&](int step, bool &second, int &n0) {
@@ -65,7 +72,7 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
     n0 = (step - (second ? steps0 : 0)) * GT_N;
     return (second ? a.N[1] : a.N[0]) - n0;
   };
-  const auto fetch_scales = [&](int step) {
+  const auto fetch_scales = [&](Stage &f, int step) {
     bool second;
     int n0;
     const int left = where(step, second, n0);
@@ -75,29 +82,29 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
     for (int v = 0; v < G::NS; ++v) {
       const int t = tid + G::TH * v, at = t % GT_N * a.G + t / GT_N;     // entries [group][row]
       if (t < ncol * GT_N) {
-        sv[v] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sb, at * 4, 0, 0));
-        if (ASYM) zv[v] = __builtin_amdgcn_raw_buffer_load_b8(zb, at, 0, 0);
+        f.s[v] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sb, at * 4, 0, 0));
+        if (ASYM) f.z[v] = __builtin_amdgcn_raw_buffer_load_b8(zb, at, 0, 0);
       }
     }
   };
-  const auto put_scales = [&](float *s) {
+  const auto put_scales = [&](const Stage &f, float *s) {
 #pragma unroll
     for (int v = 0; v < G::NS; ++v) {
       const int t = tid + G::TH * v;
       if (t < ncol * GT_N) {
         if (PRE) {                                                       // [row] scales, then [row] offsets
-          s[t] = sv[v] * 16.0f;
-          if (ASYM) s[GT_N + t] = (float)(zv[v] - 8) * 0.0625f;
+          s[t] = f.s[v] * 16.0f;
+          if (ASYM) s[GT_N + t] = (float)(f.z[v] - 8) * 0.0625f;
         } else if (ASYM) {
-          s[2 * t] = sv[v] * 16.0f;
-          s[2 * t + 1] = -(float)(zv[v] - 8) * sv[v];
+          s[2 * t] = f.s[v] * 16.0f;
+          s[2 * t + 1] = -(float)(f.z[v] - 8) * f.s[v];
         } else {
-          s[t] = sv[v] * 16.0f;
+          s[t] = f.s[v] * 16.0f;
         }
       }
     }
   };
-  const auto fetch = [&](int step) {
+  const auto fetch = [&](Stage &f, int step) {
     bool second;
     int n0;
     const int left = where(step, second, n0);
@@ -108,7 +115,7 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
 #pragma unroll
       for (int v = 0; v < G::NU; ++v) {
         const int t = tid + G::TH * v, r = t / G::UR, u = t % G::UR;
-        dyv[v] = *(const typename std::conditional<G::ES == 4, w4_u4_a4, w4_u4_a2>::type *)(dy + (unsigned)(min(r, last) * row_bytes + u * 16));
+        f.dy[v] = *(const typename std::conditional<G::ES == 4, w4_u4_a4, w4_u4_a2>::type *)(dy + (unsigned)(min(r, last) * row_bytes + u * 16));
       }
     } else {                                     // the last rows of W: zero beyond them
 #pragma unroll
@@ -121,65 +128,74 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
           e[x] = (T)0.0f;
           if (n + x < left) e[x] = p[x];
         }
-        dyv[v] = __builtin_bit_cast(w4_u4, e);
+        f.dy[v] = __builtin_bit_cast(w4_u4, e);
       }
     }
     const __amdgpu_buffer_rsrc_t qb = w4_buffer((second ? a.w[1].q : a.w[0].q) + ((size_t)n0 * KB + k0 / 2), (int64_t)left * KB - k0 / 2);
 #pragma unroll
     for (int v = 0; v < G::NW; ++v) {
       const int t = tid + G::TH * v;
-      wv[v] = __builtin_bit_cast(w4_u4, __builtin_amdgcn_raw_buffer_load_b128(qb, t / G::WU * KB + t % G::WU * 16, 0, 0));
+      f.w[v] = __builtin_bit_cast(w4_u4, __builtin_amdgcn_raw_buffer_load_b128(qb, t / G::WU * KB + t % G::WU * 16, 0, 0));
     }
-    if (!PRE) fetch_scales(step);
+    if (!PRE) fetch_scales(f, step);
   };
-  const auto put = [&](char *buf, const float *scales) {
+  const auto put = [&](const Stage &f, char *buf, const float *scales) {
 #pragma unroll
     for (int v = 0; v < G::NU; ++v) {
       const int t = tid + G::TH * v, r = t / G::UR, u = t % G::UR;
       if constexpr (TYPE == QC_TYPE_F32) {
         float p[4][3];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w4_split(__builtin_bit_cast(w4_f4, dyv[v])[e] * (PRE ? scales[u * 4 + e] : 1.0f), p[e]);
+        for (int e = 0; e < 4; ++e) w4_split(__builtin_bit_cast(w4_f4, f.dy[v])[e] * (PRE ? scales[u * 4 + e] : 1.0f), p[e]);
 #pragma unroll
         for (int s = 0; s < 3; ++s)
           *(w4_u2 *)(buf + s * 16 * MI * 128 + gt_slot(r, u >> 1) + (u & 1) * 8) = w4_u2{w4_pack_bf16(p[0][s], p[1][s]), w4_pack_bf16(p[2][s], p[3][s])};
       } else {
-        *(w4_u4 *)(buf + gt_slot(r, u)) = dyv[v];
+        *(w4_u4 *)(buf + gt_slot(r, u)) = f.dy[v];
       }
     }
 #pragma unroll
     for (int v = 0; v < G::NW; ++v) {
       const int t = tid + G::TH * v;
       char *at = buf + G::DY + t / G::WU * G::WROW + t % G::WU * 16;
-      *(w4_u2 *)at = w4_u2{wv[v][0], wv[v][1]};
-      *(w4_u2 *)(at + 8) = w4_u2{wv[v][2], wv[v][3]};
+      *(w4_u2 *)at = w4_u2{f.w[v][0], f.w[v][1]};
+      *(w4_u2 *)(at + 8) = w4_u2{f.w[v][2], f.w[v][3]};
     }
-    if (!PRE) put_scales((float *)(buf + G::DY + G::W));
+    if (!PRE) put_scales(f, (float *)(buf + G::DY + G::W));
   };
 
   w4_f4 acc[MI][4] = {};
-  char *mybuf = lds + party * (2 * G::BUF);
+  char *mybuf = lds + party * (G::BUFS * G::BUF);
   const int turns = (steps + G::S - 1) / G::S;                           // of every party: the last step of one may lie beyond the rows
-  // PRE: three tables of scales, since a step's are needed when its gradients are stored, a step before its weights are used
-  float *tables = (float *)(lds + 2 * G::S * G::BUF) + party * (3 * 2 * GT_N);
-  if (turns) {
-    if (PRE) {
-      fetch_scales(party);
-      put_scales(tables);
-      fetch_scales(G::S + party);
-      put_scales(tables + 2 * GT_N);
+  const auto turned = [&]() {
+    if constexpr (G::SOLO) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    } else {
       __syncthreads();
     }
-    fetch(party);
-    put(mybuf, tables);
+  };
+  // PRE: three tables of scales, since a step's are needed when its gradients are stored, a step before its weights are used
+  float *tables = (float *)(lds + G::BUFS * G::S * G::BUF) + party * (3 * 2 * GT_N);
+  if (turns) {
+    if (PRE) {
+      fetch_scales(stage[0], party);
+      put_scales(stage[0], tables);
+      fetch_scales(stage[0], G::S + party);
+      put_scales(stage[0], tables + 2 * GT_N);
+      turned();
+    }
+#pragma unroll
+    for (int d = 0; d < G::AHEAD; ++d) fetch(stage[d], G::S * d + party);
+    put(stage[0], mybuf, tables);
   }
-  __syncthreads();
+  turned();
   int table = 0;                                                         // of the present step
-  for (int turn = 0; turn < turns; ++turn) {
-    const char *cur = mybuf + (turn & 1) * G::BUF;
+  const auto work = [&](int turn, Stage &later, Stage &next) {
+    const char *cur = mybuf + (turn % G::BUFS) * G::BUF;
     const float *now = tables + table * (2 * GT_N);
-    if (turn + 1 < turns) fetch(G::S * (turn + 1) + party);
-    if (PRE && turn + 2 < turns) fetch_scales(G::S * (turn + 2) + party);
+    if (turn + G::AHEAD < turns) fetch(later, G::S * (turn + G::AHEAD) + party);
+    if (PRE && turn + 2 < turns) fetch_scales(later, G::S * (turn + 2) + party);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       unsigned short q[8];
@@ -245,11 +261,17 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
       }
     }
     const int after = table == 2 ? 0 : table + 1;
-    if (turn + 1 < turns) put(mybuf + ((turn + 1) & 1) * G::BUF, tables + after * (2 * GT_N));
-    if (PRE && turn + 2 < turns) put_scales(tables + (after == 2 ? 0 : after + 1) * (2 * GT_N));
+    if (G::SOLO) turned();                                               // its one buffer is read
+    if (turn + 1 < turns) put(next, mybuf + ((turn + 1) % G::BUFS) * G::BUF, tables + after * (2 * GT_N));
+    if (PRE && turn + 2 < turns) put_scales(later, tables + (after == 2 ? 0 : after + 1) * (2 * GT_N));
     table = after;
-    __syncthreads();
+    turned();
+  };
+  for (int turn = 0; turn < turns; turn += G::AHEAD) {
+    work(turn, stage[0], stage[G::AHEAD - 1]);
+    if (G::AHEAD == 2 && turn + 1 < turns) work(turn + 1, stage[G::AHEAD - 1], stage[0]);
   }
+  if (G::SOLO) __syncthreads();
 
   w4_f4 *there = (w4_f4 *)lds;
   const auto store = [&](int row0, int k, const w4_f4 sum[4]) {
@@ -291,16 +313,16 @@ __global__ __launch_bounds__(512, 2) void w4_grad_kernel(W4GradArgs a, int tm, i
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) there[(i * 4 + t) * 512 + threadIdx.x] = acc[i][t];
+      for (int t = 0; t < 4; ++t) there[(i * 4 + t) * (64 * G::WV) + threadIdx.x] = acc[i][t];
     __syncthreads();
-    for (int o = threadIdx.x; o < MI * G::TH; o += 512) {
+    for (int o = threadIdx.x; o < MI * G::TH; o += 64 * G::WV) {
       const int i = o / G::TH, th = o % G::TH;
       w4_f4 sum[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        sum[t] = there[(i * 4 + t) * 512 + th];
+        sum[t] = there[(i * 4 + t) * (64 * G::WV) + th];
 #pragma unroll
-        for (int p = 1; p < G::S; ++p) sum[t] += there[(i * 4 + t) * 512 + p * G::TH + th];
+        for (int p = 1; p < G::S; ++p) sum[t] += there[(i * 4 + t) * (64 * G::WV) + p * G::TH + th];
       }
       store(16 * i + (th >> 4 & 3) * 4, k0 + (th >> 6) * 64 + (th & 15) * 4, sum);
     }
@@ -318,21 +340,22 @@ static hipError_t launch(const W4GradArgs &a, hipStream_t st) {
     hipError_t e = allow_lds((const void *)kern, lds, done);
     if (e != hipSuccess) return e;
   }
-  kern<<<(unsigned)(tm * tk), 512, lds, st>>>(a, (int)tm, (int)tk);
+  kern<<<(unsigned)(tm * tk), 64 * GradTile<TYPE, MI, CW, PRE>::WV, lds, st>>>(a, (int)tm, (int)tk);
   return hipGetLastError();
 }
 
-// Tiles: row blocks, wavefronts side by side, and us of a step of all parties of a workgroup, 8 / CW * 64 rows of W (a compute unit runs one
-// workgroup at a time).  Measured at 4608 x 1152, 1152 x 4608, 8192 x 8192 and 1000 x 400, 1 - 2048 rows; the tile whose steps come to
-// least is within 20 % of the best of all there.  Few rows want many parties and narrow tiles (1 row of 4608 x 1152, bfloat16: 16.8 us;
-// tiles of 128 columns 32, of 256 columns 72), many rows tall and wide ones (2048 rows of 8192 x 8192: 300 us, 376 with 96 rows a tile).
+// Tiles: row blocks, wavefronts side by side, parties, the smallest group they take, and us of a step of all parties, 64 rows of W each (a
+// compute unit runs one workgroup at a time).  Measured at 4608 x 1152, 1152 x 4608, 8192 x 8192 and 1000 x 400, 1 - 2048 rows; the
+// tile whose steps come to least is within a fifth of the best of all there.  Few rows want many parties and narrow tiles (1 row of 4608
+// x 1152, bfloat16: 15 us; tiles of 128 columns 32, of 256 columns 72), many rows tall and wide ones (2048 rows of 8192 x 8192: 300 us,
+// 376 with 96 rows a tile).
 struct GradShape {
-  int MI, CW, group;       // group: the smallest the tile takes
+  int MI, CW, parties, group;
   float step;
 };
-static constexpr GradShape SHAPES_16[] = {{1, 1, 32, 1.5f}, {2, 1, 32, 1.8f}, {2, 2, 32, 1.55f}, {4, 2, 32, 1.95f}, {4, 4, 32, 2.2f}, {6, 4, 32, 2.55f}, {8, 4, 32, 2.8f}};
+static constexpr GradShape SHAPES_16[] = {{1, 1, 16, 32, 2.7f}, {2, 1, 8, 32, 1.7f}, {2, 2, 4, 32, 1.55f}, {4, 2, 4, 32, 1.95f}, {4, 4, 2, 32, 2.2f}, {6, 4, 2, 32, 2.2f}, {8, 4, 2, 32, 2.6f}};
 // the first two with the scale in the gradients (PRE)
-static constexpr GradShape SHAPES_F32[] = {{1, 1, 64, 2.7f}, {2, 2, 128, 2.9f}, {1, 1, 32, 3.6f}, {2, 2, 32, 4.1f}, {2, 4, 32, 4.1f}, {4, 4, 32, 5.5f}};
+static constexpr GradShape SHAPES_F32[] = {{1, 1, 8, 64, 1.85f}, {2, 2, 4, 128, 2.8f}, {1, 1, 8, 32, 3.05f}, {2, 2, 4, 32, 4.0f}, {2, 4, 2, 32, 4.1f}, {4, 4, 2, 32, 5.4f}};
 
 template <int N>
 static int shape(const W4GradArgs &a, const GradShape (&shapes)[N]) {
@@ -342,9 +365,8 @@ static int shape(const W4GradArgs &a, const GradShape (&shapes)[N]) {
   for (int i = 0; i < N; ++i) {
     const GradShape &s = shapes[i];
     if (a.group < s.group) continue;
-    const int parties = 8 / s.CW;
     const int64_t groups = (int64_t)((a.M + 16 * s.MI - 1) / (16 * s.MI)) * ((a.K + 64 * s.CW - 1) / (64 * s.CW));
-    const float t = (3.0f + s.step * ((steps + parties - 1) / parties)) * (float)((groups + 255) / 256);     // 3 us: first loads, last stores
+    const float t = (3.0f + s.step * ((steps + s.parties - 1) / s.parties)) * (float)((groups + 255) / 256);     // 3 us: first loads, last stores
     if (best < 0 || t < least) {
       best = i;
       least = t;
