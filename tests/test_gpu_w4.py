@@ -447,3 +447,120 @@ def test_streams_graphs_and_repeats(qc, M, dtype):
         torch.cuda.synchronize()
         want = eager if dtype != "i8" else eager[:2]
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+# ---------------------------------------------------------------- launches of many rows: every tile of the rules
+# where a tile ends inside a row block, a column block, a chunk and a group; rows around every multiple of 16 are checked, and some between
+LARGE = [(4100, 1300, 336), (16500, 130, 528), (9000, 70, 1040), (2050, 516, 2064), (3000, 1000, 272), (1500, 516, 1040), (1999, 700, 272),
+         (4100, 100, 1040), (510, 1150, 4608), (40, 7000, 144)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16", "i8"])
+@pytest.mark.parametrize("group,asym", [(128, True), (64, False), (32, True)])
+@pytest.mark.parametrize("M,N,K", LARGE)
+def test_large_launches(qc, M, N, K, group, asym, dtype):
+    import torch
+    rng = np.random.default_rng(M + N + K + group)
+    w, w2 = Weight(qc, rng, N, K, group, asym, 2.0), Weight(qc, rng, N, K, group, asym)
+    b, b2 = rng.standard_normal(N).astype(np.float32), rng.standard_normal(N).astype(np.float32)
+    bd, b2d = torch.from_numpy(b).cuda(), torch.from_numpy(b2).cuda()
+    x, xs, zp, xv, mag, zmag = _inputs(rng, M, K, dtype, 1)
+    t = _out(dtype)
+    rows = np.unique(np.concatenate([np.arange(0, M, 16), np.arange(15, M, 16), rng.integers(0, M, 60), [M - 2, M - 1]]))
+    rows = rows[rng.permutation(len(rows))[:400]]
+    rows = np.unique(np.concatenate([rows, [0, 1, M - 2, M - 1]]))
+    xr, mr = xv[rows], mag[rows]
+    pick = lambda y: y[torch.from_numpy(rows).cuda()]  # noqa: E731
+
+    y, buf = _strided(M, N, _type(t), 5, offset=2)
+    qc.qc_w4_linear(x, w.h, y, bias=bd, x_scale=xs, x_zp=zp)
+    _check(pick(y), O.linear(xr, w.v, b), _sum_tol(w, b, mr, zmag, K), t, "y")
+    assert _untouched(y, buf) and bool(torch.isfinite(y).all())
+
+    h, buf = _strided(M, N, _type(t), 3, offset=1)
+    qc.qc_w4_gated(x, w.h, w2.h, h, qc.QC_ACT_SILU, gate_bias=bd, up_bias=b2d, x_scale=xs, x_zp=zp)
+    v, p, a, d, dv, dp, da, dd = _gated_terms(xr, xs, zp, xr, mr, zmag, w, w2, b, b2, K, "silu")
+    _check(pick(h), a * p, da * (np.abs(p) + dp) + np.abs(a) * dp + 4 * E * np.abs(a * p), t, "h")
+    assert _untouched(h, buf) and bool(torch.isfinite(h).all())
+    if dtype == "i8":
+        return
+
+    dh = torch.from_numpy(rng.standard_normal((M, N))).cuda().to(_type(dtype))
+    both, buf = _strided(M, 2 * N, _type(dtype), 5, offset=1)
+    dg, du = both[:, :N], both[:, N:]
+    qc.qc_w4_gated_grad(x, w.h, w2.h, dh, dg, du, qc.QC_ACT_SILU, gate_bias=bd, up_bias=b2d)
+    z = _np(pick(dh))
+    _check(pick(dg), z * p * d, np.abs(z) * (dp * (np.abs(d) + dd) + np.abs(p) * dd + 4 * E * np.abs(p * d)), dtype, "dgate")
+    _check(pick(du), z * a, np.abs(z) * (da + 4 * E * np.abs(a)), dtype, "dup")
+    assert _untouched(both, buf) and bool(torch.isfinite(both).all())
+
+    for kw in ({}, dict(dy2=dh, w2=w2.h)):
+        dx, buf = _strided(M, K, _type(dtype), 5, offset=3)
+        dy = dg if kw else dh                              # one with odd rows, one contiguous
+        qc.qc_w4_linear_grad(dy, w.h, dx, **kw)
+        g = _np(pick(dy))
+        want, tol = g @ w.v, _grad_tol(g, w.v, dtype)
+        if kw:
+            want, tol = want + z @ w2.v, tol + _grad_tol(z, w2.v, dtype)
+        _check(pick(dx), want, tol, dtype, "dx")
+        assert _untouched(dx, buf) and bool(torch.isfinite(dx).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "i8"])
+def test_long_leading_dimensions(qc, dtype):
+    """Rows 4 MiB and more apart: offsets inside a tile of rows pass 2^30 bytes."""
+    import torch
+    M, N, K, ld = 130, 40, 272, (1 << 22) - 16
+    rng = np.random.default_rng(1)
+    w = Weight(qc, rng, N, K, 64, True)
+    x, xs, zp, xv, mag, zmag = _inputs(rng, M, K, dtype, 0)
+    big = torch.empty((M - 1) * ld + K, dtype=x.dtype, device="cuda")
+    far = big.as_strided((M, K), (ld, 1))
+    far.copy_(x)
+    y = [torch.empty((M, N), dtype=_type(_out(dtype)), device="cuda") for _ in range(2)]
+    qc.qc_w4_linear(far, w.h, y[0], x_scale=xs, x_zp=zp)
+    qc.qc_w4_linear(x.contiguous(), w.h, y[1], x_scale=xs, x_zp=zp)
+    assert torch.equal(y[0], y[1])
+    _check(y[0], O.linear(xv, w.v), _sum_tol(w, None, mag, zmag, K), _out(dtype), "y")
+    if dtype != "i8":
+        dx = [torch.empty((M, N * 16), dtype=x.dtype, device="cuda") for _ in range(2)]
+        w2 = Weight(qc, rng, K, N * 16, 64, True)
+        qc.qc_w4_linear_grad(far, w2.h, dx[0])
+        qc.qc_w4_linear_grad(x.contiguous(), w2.h, dx[1])
+        assert torch.equal(dx[0], dx[1])
+
+
+def test_concurrent_threads(qc):
+    """Two host threads with a stream each, first calls of their kernels among them."""
+    import threading
+    import torch
+    rng = np.random.default_rng(8)
+    w, w2 = Weight(qc, rng, 500, 400, 32, True), Weight(qc, rng, 500, 400, 32, True)
+    xs = [torch.from_numpy(rng.standard_normal((m, 400))).cuda().half() for m in (3, 333)]
+    want, got, errors = [], [[None] * 20 for _ in xs], []
+
+    def chain(x):
+        h = torch.empty((x.shape[0], 500), dtype=x.dtype, device="cuda")
+        dx = torch.empty_like(x)
+        qc.qc_w4_gated(x, w.h, w2.h, h, qc.QC_ACT_GELU)
+        qc.qc_w4_linear_grad(h, w.h, dx)
+        return h, dx
+
+    def run(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for n in range(20):
+                    got[i][n] = chain(xs[i])
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    torch.cuda.synchronize()
+    ts = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    [t.start() for t in ts]
+    [t.join() for t in ts]
+    assert not errors
+    want = [chain(x) for x in xs]
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
