@@ -91,7 +91,8 @@ int qc_w4_gated(const void *x, int type, int64_t ldx, float x_scale, int x_zp, c
  * dy, dy2: dev [M, N] (each of its weight's N) of `type` (float32, float16, bfloat16); dx: dev [M, K] of that type.
  * w and w2 have the same K and group, and both or neither have zero points.  The weights are fixed: no gradient of
  * theirs is formed.  For float16 and bfloat16 the product scale * (u - zero) is rounded to the type before it enters
- * the matrix product (the scales vary along the summed axis and cannot be applied behind it). */
+ * the matrix product (the scales vary along the summed axis and cannot be applied behind it); for float32 a row of dy
+ * that is not finite gives results that are not, infinities or NaN. */
 int qc_w4_linear_grad(const void *dy, int type, int64_t lddy, const qc_w4_weight *w, const void *dy2, int64_t lddy2,
                       const qc_w4_weight *w2, int M, void *dx, int64_t lddx, void *stream);
 
