@@ -14,8 +14,6 @@ typedef float w4_f4 __attribute__((ext_vector_type(4)));
 typedef int w4_i4 __attribute__((ext_vector_type(4)));
 typedef unsigned w4_u4 __attribute__((ext_vector_type(4)));
 typedef unsigned w4_u2 __attribute__((ext_vector_type(2)));
-// rows of packed codes start at multiples of 8 bytes (K % 16 == 0)
-typedef w4_u4 w4_u4_a8 __attribute__((aligned(8)));
 // rows of gradients start at any element
 typedef w4_u4 w4_u4_a4 __attribute__((aligned(4)));
 typedef w4_u4 w4_u4_a2 __attribute__((aligned(2)));
@@ -192,14 +190,6 @@ __device__ __forceinline__ void w4_swap32(w4_u4 &v) {
   const u2 a = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
   const u2 b = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
   v = w4_u4{a[0], b[0], a[1], b[1]};
-}
-
-// 16 bytes of a row of KB bytes at `at`; beyond the row's end: anything of the row (the inputs there count as zero)
-__device__ __forceinline__ w4_u4 w4_load16(const uint8_t *row, int at, int KB) {
-  if (at + 16 <= KB) return *(const w4_u4_a8 *)(row + at);
-  const int p = at + 8 <= KB ? at : KB - 8;
-  const w4_u2 v = *(const w4_u2 *)(row + p);
-  return w4_u4{v[0], v[1], v[0], v[1]};
 }
 
 // float32 as three bfloat16 numbers whose sum it is exactly: truncation leaves 8 bits of the 24 each time.  What does not
