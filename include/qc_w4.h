@@ -61,7 +61,7 @@ typedef struct qc_w4_weight {
   int32_t group;    /* 32, 64 or 128                                                                */
 } qc_w4_weight;
 
-/* Quantises a matrix w: dev [N, K] of `type` (float32, float16 or bfloat16; finite), rows ld apart, into out->q,
+/* Quantises a matrix w: dev [N, K] of `type` (float32, float16 or bfloat16; finite, the range h - l too), rows ld apart, into out->q,
  * out->scale, out->zero (unless it is NULL) and out->sum (unless it is NULL).  Per group of a row, in float32:
  *   symmetric (out->zero NULL):  s = max|w| / 7,  u = clip(round(w / s), -7, 7) + 8
  *   with zero points:  l = min(min w, 0), h = max(max w, 0), s = (h - l) / 15, z = clip(round(-l / s), 0, 15),
