@@ -90,9 +90,9 @@ int qc_w4_gated(const void *x, int type, int64_t ldx, float x_scale, int x_zp, c
  *   dx[m, k] = sum_n dy[m, n] w[n, k]  (+ sum_n dy2[m, n] w2[n, k], if w2 is not NULL)
  * dy, dy2: dev [M, N] (each of its weight's N) of `type` (float32, float16, bfloat16); dx: dev [M, K] of that type.
  * w and w2 have the same K and group, and both or neither have zero points.  The weights are fixed: no gradient of
- * theirs is formed.  For float16 and bfloat16 the product scale * (u - zero) is rounded to the type before it enters
- * the matrix product (the scales vary along the summed axis and cannot be applied behind it); for float32 a row of dy
- * that is not finite gives results that are not, infinities or NaN. */
+ * theirs is formed.  The scales vary along the summed axis and enter the matrix product: for float16 and bfloat16
+ * either dy * scale, or scale * (u - zero) (and of float16 dy), is taken to 15 bits or more, whatever the type, for
+ * float32 to 24.  For float32 a row of dy that is not finite gives results that are not, infinities or NaN. */
 int qc_w4_linear_grad(const void *dy, int type, int64_t lddy, const qc_w4_weight *w, const void *dy2, int64_t lddy2,
                       const qc_w4_weight *w2, int M, void *dx, int64_t lddx, void *stream);
 

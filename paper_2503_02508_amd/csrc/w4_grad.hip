@@ -1,12 +1,14 @@
 // Gradient of a linear layer's input through fixed 4-bit weights of groups: dx = dy W (+ dy2 W2).
 //
-// The summed axis is the rows of W.  A workgroup makes 16 MI rows by 64 CW columns of dx; its eight wavefronts are 8 / CW parties that take
+// The summed axis is the rows of W.  A workgroup makes 16 MI rows by 64 CW columns of dx; its WV wavefronts are WV / CW parties that take
 // the steps, 64 rows of W, in turn and add their sums at the end, so that a narrow dx still has every wavefront at work.  A step's
 // gradients, packed codes and scales go through LDS.  A lane expands, of 8 neighbouring rows of W, the 4 neighbouring columns it will hold
 // results of (nibble t of its two bytes belongs to product t).  The scales vary along the summed axis, so a weight is scaled before it
-// enters a product.  float16 and bfloat16: it is rounded to the type, half a step like every stored value; two products for one
-// would keep it whole and cost twice the time.  float32: gradients and scaled weights are each the sum of three bfloat16 numbers, and six of
-// the nine products are formed (the others are below 2^-22 of the largest).
+// enters a product, and is not a number of few bits any more.  All products are of bfloat16 parts, whose exponents are float32's:
+//   bfloat16   gradients as they are; weights of two parts, the second rounded, off by 2^-15 of themselves at most: two products
+//   float16    gradients of two parts, exactly; weights of two; the product of the two second parts, below 2^-15, is left out: three
+//   float32    both of three parts, exactly; six of the nine products are formed (the others are below 2^-22 of the largest)
+// Where a tile's columns lie in one group the scale can multiply the gradients instead (PRE below), and the codes stay exact.
 #include "w4_common.h"
 
 namespace qc {
@@ -18,7 +20,9 @@ constexpr int GT_N = 64;                       // rows of W a step
 // left to ask for its steps two ahead.
 template <int TYPE, int MI, int CW, bool PRE>
 struct GradTile {
-  static constexpr int P = TYPE == QC_TYPE_F32 ? 3 : 1;
+  static constexpr int P = TYPE == QC_TYPE_F32 ? 3 : PRE || TYPE == QC_TYPE_F16 ? 2 : 1;   // parts of a gradient
+  static constexpr int PW = PRE ? 1 : TYPE == QC_TYPE_F32 ? 3 : 2;       // of a weight
+  static constexpr int TERMS = TYPE == QC_TYPE_F32 ? 3 : 2;              // parts p and q are multiplied where p + q is less
   static constexpr int ES = TYPE == QC_TYPE_F32 ? 4 : 2;
   static constexpr bool SOLO = CW == 1;
   static constexpr int AHEAD = SOLO && MI == 1 && TYPE != QC_TYPE_F32 ? 2 : 1;
@@ -42,14 +46,27 @@ struct GradTile {
 // 16-byte unit u of row r of a plane: 16 rows of one unit lie in 16 different slots of 256 bytes
 __device__ __forceinline__ int gt_slot(int r, int u) { return r * 128 + ((u ^ ((r >> 1) & 7)) << 4); }
 
-// PRE (float32): the tile's columns lie in one group, so that the scale of a weight row multiplies the gradients as they go to LDS, and the
-// weights are exact codes: three products for six, and nothing of the weights to split
+// PRE: the tile's columns lie in one group, so that the scale of a weight row multiplies the gradients as they go to LDS, and the
+// weights are exact codes, of which nothing has to be split: three products for six (float32), two for three (float16), and few instructions a
+// weight where there are few rows to pay for it
+// a weight in two parts.  The first is cut off below the weight itself, so that the second has its sign and is not zero either: what an
+// infinite gradient gives is the weight's infinity, and NaN only where the weight is zero.
+__device__ __forceinline__ void gt_weight(float v, float p[2]) {
+  p[0] = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v * (1.0f - 0x1p-22f)) & 0xFFFF0000u);
+  p[1] = v - p[0];
+}
+__device__ __forceinline__ unsigned gt_round_bf16(float lo, float hi) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{lo, hi}), b2));
+}
+
 template <int TYPE, int MI, int CW, bool ASYM, bool PRE>
 __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_grad_kernel(W4GradArgs a, int tm, int tk) {
   using T = typename W4Mem<TYPE>::T;
-  using F = Frag<TYPE == QC_TYPE_F32 ? QC_TYPE_BF16 : TYPE>;
+  using F = Frag<QC_TYPE_BF16>;
   using G = GradTile<TYPE, MI, CW, PRE>;
-  constexpr int P = G::P;
+  constexpr int P = G::P, PW = G::PW;
   extern __shared__ __align__(16) char lds[];
   const int party = __builtin_amdgcn_readfirstlane(threadIdx.x / G::TH), tid = threadIdx.x % G::TH;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, kb = lane >> 4;
@@ -150,6 +167,36 @@ __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_
 #pragma unroll
         for (int s = 0; s < 3; ++s)
           *(w4_u2 *)(buf + s * 16 * MI * 128 + gt_slot(r, u >> 1) + (u & 1) * 8) = w4_u2{w4_pack_bf16(p[0][s], p[1][s]), w4_pack_bf16(p[2][s], p[3][s])};
+      } else if constexpr (PRE) {
+        typedef T T8 __attribute__((ext_vector_type(8)));
+        const T8 e = __builtin_bit_cast(T8, f.dy[v]);
+        float p[8][2];                                                   // a part cut off, the rest rounded; of infinities nothing is left
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float t = (float)e[i] * scales[u * 8 + i];
+          p[i][0] = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, t) & 0xFFFF0000u);
+          p[i][1] = p[i][0] == t ? 0.0f : t - p[i][0];
+        }
+        w4_u4 h, rest;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          h[i] = w4_pack_bf16(p[2 * i][0], p[2 * i + 1][0]);
+          rest[i] = gt_round_bf16(p[2 * i][1], p[2 * i + 1][1]);
+        }
+        *(w4_u4 *)(buf + gt_slot(r, u)) = h;
+        *(w4_u4 *)(buf + 16 * MI * 128 + gt_slot(r, u)) = rest;
+      } else if constexpr (TYPE == QC_TYPE_F16) {
+        const w4_h8 e = __builtin_bit_cast(w4_h8, f.dy[v]);
+        w4_u4 h, rest;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float a = (float)e[2 * i], b = (float)e[2 * i + 1];
+          h[i] = gt_round_bf16(a, b);
+          const float ah = __builtin_bit_cast(float, h[i] << 16), bh = __builtin_bit_cast(float, h[i] & 0xFFFF0000u);
+          rest[i] = w4_pack_bf16(ah == a ? 0.0f : a - ah, bh == b ? 0.0f : b - bh);      // three bits of it are left, of infinities none
+        }
+        *(w4_u4 *)(buf + gt_slot(r, u)) = h;
+        *(w4_u4 *)(buf + 16 * MI * 128 + gt_slot(r, u)) = rest;
       } else {
         *(w4_u4 *)(buf + gt_slot(r, u)) = f.dy[v];
       }
@@ -194,8 +241,8 @@ __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_
   const auto work = [&](int turn, Stage &later, Stage &next) {
     const char *cur = mybuf + (turn % G::BUFS) * G::BUF;
     const float *now = tables + table * (2 * GT_N);
-    if (turn + G::AHEAD < turns) fetch(later, G::S * (turn + G::AHEAD) + party);
     if (PRE && turn + 2 < turns) fetch_scales(later, G::S * (turn + 2) + party);
+    if (turn + G::AHEAD < turns) fetch(later, G::S * (turn + G::AHEAD) + party);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       unsigned short q[8];
@@ -209,7 +256,7 @@ __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_
         s[i] = PRE ? 1.0f : sp[ASYM ? 2 * i : i];
         o[i] = !ASYM ? 0.0f : PRE ? -sp[i] : sp[2 * i + 1];
       }
-      w4_u4 wf[PRE ? 1 : P][4];
+      w4_u4 wf[PW][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {                                      // rows 2 i and 2 i + 1
         float v[2][4];
@@ -234,10 +281,11 @@ __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_
 #pragma unroll
             for (int p = 0; p < 3; ++p) wf[p][t][i] = w4_pack_bf16(p0[p], p1[p]);
           } else {
-            typedef T T2 __attribute__((ext_vector_type(2)));
-            typedef float f2 __attribute__((ext_vector_type(2)));
-            asm("" : "+v"(v[0][t]), "+v"(v[1][t]));                      // rounded to float32 before it is rounded to the type
-            wf[0][t][i] = __builtin_bit_cast(unsigned, __builtin_convertvector((f2{v[0][t], v[1][t]}), T2));
+            float p0[2], p1[2];
+            gt_weight(v[0][t], p0);
+            gt_weight(v[1][t], p1);
+            wf[0][t][i] = w4_pack_bf16(p0[0], p1[0]);
+            wf[1][t][i] = gt_round_bf16(p0[1], p1[1]);
           }
         }
       }
@@ -255,7 +303,7 @@ __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
-          for (int pw = 0; pw < (PRE ? 1 : P - p); ++pw)
+          for (int pw = 0; pw < (PW < G::TERMS - p ? PW : G::TERMS - p); ++pw)
 #pragma unroll
             for (int t = 0; t < 4; ++t) acc[i][t] = F::mma(x[i & 1][p], __builtin_bit_cast(typename F::W, wf[pw][t]), acc[i][t]);
       }
@@ -345,16 +393,21 @@ static hipError_t launch(const W4GradArgs &a, hipStream_t st) {
 }
 
 // Tiles: row blocks, wavefronts side by side, parties, the smallest group they take, and us of a step of all parties, 64 rows of W each (a
-// compute unit runs one workgroup at a time).  Measured at 4608 x 1152, 1152 x 4608, 8192 x 8192 and 1000 x 400, 1 - 2048 rows; the
-// tile whose steps come to least is within a fifth of the best of all there.  Few rows want many parties and narrow tiles (1 row of 4608
-// x 1152, bfloat16: 15 us; tiles of 128 columns 32, of 256 columns 72), many rows tall and wide ones (2048 rows of 8192 x 8192: 300 us,
-// 376 with 96 rows a tile).
+// compute unit runs one workgroup at a time).  Measured at 4608 x 1152, 1152 x 4608 and 8192 x 8192, 1 - 4096 rows; the tile whose steps
+// come to least is within a seventh of the best of all there.  Few rows want many parties, narrow tiles and the scale in the gradients (1 row
+// of 4608 x 1152, bfloat16: 20 us; with weights in two parts 23, with tiles of 128 columns 42 and 46, of 256 columns 101 and more), many
+// rows tall and wide tiles (2048 rows of 8192 x 8192, bfloat16: 480 us, 620 with 96 rows a tile and 1050 with the scale in the gradients).
+// Those run at the rate of a large library product of 16-bit numbers, counted as the two products they are: 1145 TFLOP/s; float16, three
+// products, 790 us.  Weights rounded to the type, one product, would take 330 and be off by half a step each.
 struct GradShape {
   int MI, CW, parties, group;
   float step;
 };
-static constexpr GradShape SHAPES_16[] = {{1, 1, 16, 32, 2.7f}, {2, 1, 8, 32, 1.7f}, {2, 2, 4, 32, 1.55f}, {4, 2, 4, 32, 1.95f}, {4, 4, 2, 32, 2.2f}, {6, 4, 2, 32, 2.2f}, {8, 4, 2, 32, 2.6f}};
-// the first two with the scale in the gradients (PRE)
+// the first two of each with the scale in the gradients (PRE)
+static constexpr GradShape SHAPES_BF16[] = {{1, 1, 16, 64, 3.3f}, {2, 2, 4, 128, 2.05f}, {1, 1, 16, 32, 4.0f}, {2, 1, 8, 32, 2.2f}, {2, 2, 4, 32, 2.3f},
+                                            {4, 2, 4, 32, 2.85f}, {4, 4, 2, 32, 2.75f}, {6, 4, 2, 32, 3.2f}, {8, 4, 2, 32, 3.7f}};
+static constexpr GradShape SHAPES_F16[] = {{1, 1, 16, 64, 3.3f}, {2, 2, 4, 128, 2.05f}, {1, 1, 16, 32, 4.7f}, {2, 1, 8, 32, 3.05f}, {2, 2, 4, 32, 2.8f},
+                                           {4, 4, 2, 32, 3.25f}, {6, 4, 2, 32, 4.1f}};
 static constexpr GradShape SHAPES_F32[] = {{1, 1, 8, 64, 1.85f}, {2, 2, 4, 128, 2.8f}, {1, 1, 8, 32, 3.05f}, {2, 2, 4, 32, 4.0f}, {2, 4, 2, 32, 4.1f}, {4, 4, 2, 32, 5.4f}};
 
 template <int N>
@@ -386,14 +439,26 @@ static hipError_t rows(const W4GradArgs &a, hipStream_t st) {
       case 4: return launch<TYPE, 2, 4, ASYM, false>(a, st);
       default: return launch<TYPE, 4, 4, ASYM, false>(a, st);
     }
+  } else if constexpr (TYPE == QC_TYPE_F16) {
+    switch (shape(a, SHAPES_F16)) {
+      case 0: return launch<TYPE, 1, 1, ASYM, true>(a, st);
+      case 1: return launch<TYPE, 2, 2, ASYM, true>(a, st);
+      case 2: return launch<TYPE, 1, 1, ASYM, false>(a, st);
+      case 3: return launch<TYPE, 2, 1, ASYM, false>(a, st);
+      case 4: return launch<TYPE, 2, 2, ASYM, false>(a, st);
+      case 5: return launch<TYPE, 4, 4, ASYM, false>(a, st);
+      default: return launch<TYPE, 6, 4, ASYM, false>(a, st);
+    }
   } else {
-    switch (shape(a, SHAPES_16)) {
-      case 0: return launch<TYPE, 1, 1, ASYM, false>(a, st);
-      case 1: return launch<TYPE, 2, 1, ASYM, false>(a, st);
-      case 2: return launch<TYPE, 2, 2, ASYM, false>(a, st);
-      case 3: return launch<TYPE, 4, 2, ASYM, false>(a, st);
-      case 4: return launch<TYPE, 4, 4, ASYM, false>(a, st);
-      case 5: return launch<TYPE, 6, 4, ASYM, false>(a, st);
+    switch (shape(a, SHAPES_BF16)) {
+      case 0: return launch<TYPE, 1, 1, ASYM, true>(a, st);
+      case 1: return launch<TYPE, 2, 2, ASYM, true>(a, st);
+      case 2: return launch<TYPE, 1, 1, ASYM, false>(a, st);
+      case 3: return launch<TYPE, 2, 1, ASYM, false>(a, st);
+      case 4: return launch<TYPE, 2, 2, ASYM, false>(a, st);
+      case 5: return launch<TYPE, 4, 2, ASYM, false>(a, st);
+      case 6: return launch<TYPE, 4, 4, ASYM, false>(a, st);
+      case 7: return launch<TYPE, 6, 4, ASYM, false>(a, st);
       default: return launch<TYPE, 8, 4, ASYM, false>(a, st);
     }
   }

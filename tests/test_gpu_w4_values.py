@@ -1,0 +1,75 @@
+"""Operators on 4-bit weights with a scale per group: values that the shapes of test_gpu_w4.py do not bring, and every tile, against float64.
+
+Tolerances count half steps of the result's type (HALF) and, in e = 2^-24, sums as in test_gpu_w4.py.  Input gradients besides, relative
+to S = sum |dy| |w|: a weight of float16 and bfloat16 calls is the sum of a part of 8 bits, cut off (what is left is below 2^-7 of it), and
+that rest, rounded to 8 bits (half a step: 2^-8 of it), 2^-15 in all; float16 gradients are 8 bits, rounded, and an exact rest (2^-8 at
+most), whose product with the weight's rest is left out, another 2^-15."""
+import numpy as np
+import pytest
+
+from oracle import w4 as O
+from test_gpu_w4 import E, HALF, TINY, Weight, _np, _strided, _type, _untouched
+
+pytestmark = pytest.mark.gpu
+PARTS = {"f32": 0.0, "f16": 2.0 ** -14, "bf16": 2.0 ** -15}
+
+
+@pytest.fixture(scope="module")
+def qc():
+    import paper_2503_02508_amd as m
+    return m
+
+
+def _dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+# ---------------------------------------------------------------- input gradients keep their weights whole
+def _grad_limit(t, dys, ws, want):
+    """What dx may be off by, from float64 gradients and weights on the GPU."""
+    tol = 0
+    for dy, w in zip(dys, ws):
+        tol = tol + ((200 + w.shape[0] / 4) * E + PARTS[t]) * (dy.abs() @ w.abs())
+    return tol + HALF[t] * (want.abs() + tol) + TINY[t]
+
+
+# one term; few rows; odd everything; each tile of the rule, 16-row blocks and column blocks cut, an odd number of steps
+GRADS = [(1, 1, 16), (3, 2, 176), (1, 700, 1168), (17, 129, 1040), (77, 257, 4112), (130, 65, 8208), (250, 400, 8208), (700, 300, 4112), (1500, 130, 4624),
+         (4100, 200, 1040)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("group,asym", [(32, True), (64, False), (128, True)])
+@pytest.mark.parametrize("M,N,K", GRADS)
+def test_input_gradients_keep_the_weights_whole(qc, M, N, K, group, asym, dtype):
+    import torch
+    rng = np.random.default_rng(M + 3 * N + K + group)
+    ws = [Weight(qc, rng, n, K, group, asym) for n in ([N, 2 * N + 1] if M % 2 else [N])]
+    dys = [_dev(rng.standard_normal((M, w.h.N))).to(_type(dtype)) for w in ws]
+    dx, buf = _strided(M, K, _type(dtype), 5, torch.full((M, K), float("nan")), offset=3)
+    qc.qc_w4_linear_grad(dys[0], ws[0].h, dx, **(dict(dy2=dys[1], w2=ws[1].h) if len(ws) > 1 else {}))
+    d64, v64 = [d.double() for d in dys], [_dev(w.v) for w in ws]
+    want = sum(d @ v for d, v in zip(d64, v64))
+    off = (dx.double() - want).abs() / _grad_limit(dtype, d64, v64, want)
+    assert bool((off <= 1).all()), float(off.nan_to_num(float("inf")).max())
+    assert _untouched(dx, buf)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_an_infinite_gradient_gives_the_weights_signs(qc, M, dtype):
+    """Of a row with one infinite gradient: an infinity of the weight's sign, NaN where the weight is zero; the other rows keep their values."""
+    import torch
+    rng = np.random.default_rng(M)
+    w = Weight(qc, rng, 90, 272, 64, False)
+    dy = _dev(rng.standard_normal((M, 90))).to(_type(dtype))
+    dx = [torch.empty((M, 272), dtype=dy.dtype, device="cuda") for _ in range(2)]
+    qc.qc_w4_linear_grad(dy, w.h, dx[0])
+    r = M // 2
+    dy[r, 7] = -float("inf")
+    qc.qc_w4_linear_grad(dy, w.h, dx[1])
+    v, got = w.v[7], _np(dx[1])[r]
+    assert (v == 0).any() and np.isnan(got[v == 0]).all() and np.array_equal(got[v != 0], -np.sign(v[v != 0]) * np.inf)
+    keep = torch.arange(M, device="cuda") != r
+    assert torch.equal(dx[0][keep], dx[1][keep])
