@@ -32,7 +32,7 @@ struct GradTile {
   static constexpr int GR = CW < 2 ? 2 : 2 * CW;                         // groups of up to 64 CW columns
   static constexpr int DY = 16 * MI * 128 * P;                           // bytes: planes of 16 MI rows of 64 gradients
   static constexpr int W = GT_N * WROW;
-  static constexpr int BUF = DY + W + (PRE ? 0 : GR * GT_N * 8);         // and (scale, offset) of every row and group
+  static constexpr int BUF = DY + W + (PRE ? 0 : GR * GT_N * 8);         // and (scale, zero point) of every row and group
   // buffers of all parties; afterwards the sums, of two parties only the half that the other finishes
   static constexpr int SUMS = (S == 2 ? MI / 2 : MI) * 4 * 64 * WV * 16;
   static constexpr int TABLES = PRE ? S * 3 * 2 * GT_N * 4 : 0;
@@ -109,12 +109,12 @@ __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_
     for (int v = 0; v < G::NS; ++v) {
       const int t = tid + G::TH * v;
       if (t < ncol * GT_N) {
-        if (PRE) {                                                       // [row] scales, then [row] offsets
+        if (PRE) {                                                       // [row] scales, then [row] zero points
           s[t] = f.s[v] * 16.0f;
           if (ASYM) s[GT_N + t] = (float)(f.z[v] - 8) * 0.0625f;
         } else if (ASYM) {
           s[2 * t] = f.s[v] * 16.0f;
-          s[2 * t + 1] = -(float)(f.z[v] - 8) * f.s[v];
+          s[2 * t + 1] = (float)(f.z[v] - 8) * 0.0625f;
         } else {
           s[t] = f.s[v] * 16.0f;
         }
@@ -254,7 +254,7 @@ __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         s[i] = PRE ? 1.0f : sp[ASYM ? 2 * i : i];
-        o[i] = !ASYM ? 0.0f : PRE ? -sp[i] : sp[2 * i + 1];
+        o[i] = !ASYM ? 0.0f : sp[PRE ? i : 2 * i + 1];
       }
       w4_u4 wf[PW][4];
 #pragma unroll
@@ -266,8 +266,9 @@ __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_
           asm("" : "+v"(odd));
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            const float c = w4_nibble(((t & 1 ? odd : even) >> (t & 2 ? 8 : 0)) & 0xFF);
-            v[b][t] = PRE ? (ASYM ? c + o[2 * i + b] : c) : ASYM ? fmaf(c, s[2 * i + b], o[2 * i + b]) : c * s[2 * i + b];
+            float c = w4_nibble(((t & 1 ? odd : even) >> (t & 2 ? 8 : 0)) & 0xFF);
+            if (ASYM) c -= o[2 * i + b];                                 // among the codes, where it is exact: u = z is a weight of zero
+            v[b][t] = PRE ? c : c * s[2 * i + b];
           }
         }
 #pragma unroll

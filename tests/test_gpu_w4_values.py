@@ -73,3 +73,31 @@ def test_an_infinite_gradient_gives_the_weights_signs(qc, M, dtype):
     assert (v == 0).any() and np.isnan(got[v == 0]).all() and np.array_equal(got[v != 0], -np.sign(v[v != 0]) * np.inf)
     keep = torch.arange(M, device="cuda") != r
     assert torch.equal(dx[0][keep], dx[1][keep])
+
+
+# ---------------------------------------------------------------- codes that equal their zero point
+def _with_zero_columns(qc, rng, N, K, group):
+    """A weight with zero points 0..15 and scales of full mantissas, every third column zero: u = z in every row.  And its matrix."""
+    import torch
+    G = -(-K // group)
+    z, u = rng.integers(0, 16, (N, G)), rng.integers(0, 16, (N, K))
+    full = np.repeat(z, group, 1)[:, :K]
+    u[:, ::3] = full[:, ::3]
+    s = rng.uniform(0.01, 0.02, (N, G)).astype(np.float32)
+    return O.values(u, s, z, group), qc.W4Weight(_dev(O.pack(u)), _dev(s), group, _dev(z.astype(np.uint8)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N,K", [(16, 130, 272), (40, 900, 2064), (500, 2000, 1168), (1000, 700, 1168), (250, 400, 8208), (1500, 130, 4624), (4100, 200, 1040)])
+def test_gradients_through_zero_columns_are_zero(qc, M, N, K, group, dtype):
+    import torch
+    rng = np.random.default_rng(M + N + group)
+    v, W = _with_zero_columns(qc, rng, N, K, group)
+    dy = _dev(rng.standard_normal((M, N))).to(_type(dtype))
+    dx = torch.full((M, K), float("nan"), dtype=dy.dtype, device="cuda")
+    qc.qc_w4_linear_grad(dy, W, dx)
+    assert bool((dx[:, ::3] == 0).all())
+    d64, v64 = dy.double(), _dev(v)
+    want = d64 @ v64
+    assert bool(((dx.double() - want).abs() <= _grad_limit(dtype, [d64], [v64], want)).all())
