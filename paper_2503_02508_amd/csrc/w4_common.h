@@ -240,9 +240,10 @@ __device__ __forceinline__ float w4_act(int act, float v, float &d) {
     d = e * (1.0f + v * (1.0f - e));
     return v * e;
   }
-  // (1 + tanh(y)) / 2 = logistic(2 y), which keeps its digits where it is small; |v| > 30 is 0 or 1 already
+  // (1 + tanh(y)) / 2 = logistic(2 y), which keeps its digits where it is small; |v| > 30 is 0 or 1 already.  The
+  // comparison leaves NaN as it is (minimum and maximum would not).
   const float c0 = 1.5957691216057308f, c1 = 0.044715f;
-  const float b = fminf(fmaxf(v, -30.0f), 30.0f), b2 = b * b;
+  const float b = fabsf(v) > 30.0f ? copysignf(30.0f, v) : v, b2 = b * b;
   const float e = w4_logistic(c0 * b * (1.0f + c1 * b2));
   d = e + c0 * b * (1.0f + 3.0f * c1 * b2) * (e * (1.0f - e));
   return v * e;

@@ -101,3 +101,40 @@ def test_gradients_through_zero_columns_are_zero(qc, M, N, K, group, dtype):
     d64, v64 = dy.double(), _dev(v)
     want = d64 @ v64
     assert bool(((dx.double() - want).abs() <= _grad_limit(dtype, [d64], [v64], want)).all())
+
+
+# ---------------------------------------------------------------- the gate far out and not a number
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M,N,K", [(3, 130, 272), (40, 130, 272), (4100, 1300, 144)])
+def test_large_gates_and_gates_that_are_not_numbers(qc, M, N, K, act, dtype):
+    """v of 30 and far more by the gate's bias, and a bias that is NaN: h, dgate and dup are NaN in its columns and right in the others."""
+    import torch
+    rng = np.random.default_rng(M)
+    g, u = Weight(qc, rng, N, K, 64, True), Weight(qc, rng, N, K, 64, True)
+    big = [30.0, -30.0, 60.0, -60.0, 100.0, -100.0, 900.0, -900.0] + ([] if dtype == "f16" else [1e4, -1e4, 1e30, -1e30])
+    b = np.zeros(N, np.float32)
+    b[:len(big) * 4] = np.repeat(big, 4)
+    b[60::40] = np.nan
+    x, dh = (_dev(rng.standard_normal(s)).to(_type(dtype)) for s in ((M, K), (M, N)))
+    h, dg, du = (torch.full((M, N), 777.0, dtype=x.dtype, device="cuda") for _ in range(3))
+    code = {"silu": qc.QC_ACT_SILU, "gelu": qc.QC_ACT_GELU}[act]
+    qc.qc_w4_gated(x, g.h, u.h, h, code, gate_bias=_dev(b))
+    qc.qc_w4_gated_grad(x, g.h, u.h, dh, dg, du, code, gate_bias=_dev(b))
+    nan = np.isnan(b)
+    assert all(bool(t[:, torch.from_numpy(nan).cuda()].isnan().all()) for t in (h, dg, du))
+    ok = ~nan
+    xv, z = _np(x), _np(dh)[:, ok]
+    v, p = O.linear(xv, g.v[ok], b[ok].astype(np.float64)), O.linear(xv, u.v[ok])
+    a, d = O.act(act, v)
+    # sums as in test_gpu_w4.py; the activation's slope is at most 1.13 and its derivative's at most 1, and both are constant beyond |v| = 30
+    # but for rounding: a is v, or 0 to an absolute 2^-100
+    S = [np.abs(xv) @ np.abs(w.v[ok]).T for w in (g, u)]
+    dv, dp = (200 + K / 16) * E * (S[0] + np.abs(b[ok])), (200 + K / 16) * E * S[1]
+    da = 1.13 * dv + 16 * E * (1 + np.abs(v)) * np.abs(a) + 16 * E * (1 + np.minimum(np.abs(v), 30)) ** 2 * (np.abs(v) <= 30) + 2.0 ** -100
+    dd = 1.0 * np.where(np.abs(v) > 30, 0, dv) + 16 * E * (1 + np.minimum(np.abs(v), 30))
+    for got, want, tol in ((h, a * p, da * (np.abs(p) + dp) + np.abs(a) * dp), (dg, z * p * d, np.abs(z) * (dp * (np.abs(d) + dd) + np.abs(p) * dd)),
+                           (du, z * a, np.abs(z) * da)):
+        tol = tol + 8 * E * np.abs(want)
+        lim = tol + HALF[dtype] * (np.abs(want) + tol) + TINY[dtype]
+        assert (np.abs(_np(got)[:, ok] - want) <= lim).all()
