@@ -46,11 +46,11 @@ int check_weight(const qc_w4_weight *w, const char *name) {
   return QC_OK;
 }
 
-// two weights of one call
+// two weights of one call; one without rows has no zero points to have or not (its pointers may be NULL)
 int check_pair(const qc_w4_weight *a, const qc_w4_weight *b, bool rows) {
   if (a->K != b->K || a->group != b->group || (rows && a->N != b->N))
     QC_FAIL(QC_ERR_SHAPE, "the weights differ: %d x %d in groups of %d, %d x %d in groups of %d", a->N, a->K, a->group, b->N, b->K, b->group);
-  if (!a->zero != !b->zero) QC_FAIL(QC_ERR_UNSUPPORTED, "one of the weights has zero points, the other has none");
+  if (a->N && b->N && !a->zero != !b->zero) QC_FAIL(QC_ERR_UNSUPPORTED, "one of the weights has zero points, the other has none");
   return QC_OK;
 }
 
@@ -73,7 +73,7 @@ int check_codes(int type, float x_scale, int x_zp, const qc_w4_weight *w) {
   if (type != QC_TYPE_I8) return QC_OK;
   if (!(x_scale > 0.0f) || !std::isfinite(x_scale)) QC_FAIL(QC_ERR_RANGE, "scale must be positive and finite");
   if (x_zp < 0 || x_zp > 255) QC_FAIL(QC_ERR_RANGE, "zero point %d outside 0..255", x_zp);
-  if (!w->sum) QC_FAIL(QC_ERR_NULL, "8-bit inputs need the weight's row sums");
+  if (w->N && !w->sum) QC_FAIL(QC_ERR_NULL, "8-bit inputs need the weight's row sums");
   return QC_OK;
 }
 

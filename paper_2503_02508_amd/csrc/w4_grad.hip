@@ -466,7 +466,8 @@ static hipError_t rows(const W4GradArgs &a, hipStream_t st) {
 }
 
 hipError_t launch_w4_grad(const W4GradArgs &a, int type, hipStream_t st) {
-  const bool z = a.w[0].zero != nullptr;
+  // a weight without rows may have zero points or none, whatever the other has
+  const bool z = (a.N[0] && a.w[0].zero) || (a.nw > 1 && a.N[1] && a.w[1].zero);
   if (type == QC_TYPE_F32) return z ? rows<QC_TYPE_F32, true>(a, st) : rows<QC_TYPE_F32, false>(a, st);
   if (type == QC_TYPE_F16) return z ? rows<QC_TYPE_F16, true>(a, st) : rows<QC_TYPE_F16, false>(a, st);
   return z ? rows<QC_TYPE_BF16, true>(a, st) : rows<QC_TYPE_BF16, false>(a, st);

@@ -138,3 +138,25 @@ def test_large_gates_and_gates_that_are_not_numbers(qc, M, N, K, act, dtype):
         tol = tol + 8 * E * np.abs(want)
         lim = tol + HALF[dtype] * (np.abs(want) + tol) + TINY[dtype]
         assert (np.abs(_np(got)[:, ok] - want) <= lim).all()
+
+
+# ---------------------------------------------------------------- weights without rows
+@pytest.mark.parametrize("asym", [False, True])
+def test_weights_without_rows(qc, asym):
+    """A layer of no outputs adds nothing to the gradient of two, whichever it is; products with it do nothing, 8-bit inputs too."""
+    import torch
+    rng = np.random.default_rng(1)
+    w, none = Weight(qc, rng, 40, 64, 32, asym), qc.W4Weight.empty(0, 64, 32, asym)
+    if not asym:
+        none.desc.zero = w.h.q.data_ptr()              # a pointer that nothing reads: w has no zero points
+    dy, empty = _dev(rng.standard_normal((5, 40)).astype(np.float32)), torch.empty((5, 0), device="cuda")
+    dx = [torch.full((5, 64), float("nan"), device="cuda") for _ in range(4)]
+    qc.qc_w4_linear_grad(dy, w.h, dx[0])
+    qc.qc_w4_linear_grad(dy, w.h, dx[1], dy2=empty, w2=none)
+    qc.qc_w4_linear_grad(empty, none, dx[2], dy2=dy, w2=w.h)
+    qc.qc_w4_linear_grad(empty, none, dx[3], dy2=empty, w2=none)
+    assert torch.equal(dx[0], dx[1]) and torch.equal(dx[0], dx[2]) and bool((dx[3] == 0).all())
+    for x in (torch.ones((5, 64), device="cuda"), torch.ones((5, 64), dtype=torch.int8, device="cuda")):
+        qc.qc_w4_linear(x, none, empty)
+        qc.qc_w4_gated(x, none, none, empty)
+    torch.cuda.synchronize()

@@ -162,3 +162,14 @@ def test_the_binding_refuses_what_the_c_abi_cannot_see(qc):
         qc.qc_w4_linear_grad(y, w, x, dy2=y)
     with pytest.raises(qc.QCError):
         qc.qc_w4_gated_grad(x, w, w, y, y, torch.zeros(2, 8)[:, :4])
+
+
+def test_weights_without_rows_may_lie_nowhere(qc):
+    """N = 0 does nothing, also where the sums of 8-bit inputs or the zero points of a pair have no memory."""
+    L, none = qc.lib, C.byref(_desc(qc, N=0, q=None, scale=None, sum=None))
+    zeros = C.byref(_desc(qc, zero=P))
+    assert L.qc_w4_linear(P, 3, 64, 0.02, 100, none, None, 4, None, 0, None) == 0
+    assert L.qc_w4_gated(P, 3, 64, 0.02, 100, none, none, None, None, 0, 4, None, 0, None) == 0
+    assert L.qc_w4_gated(P, 3, 64, 0.02, 100, none, C.byref(_desc(qc, N=0, zero=P)), None, None, 0, 4, None, 0, None) == 0
+    for a, b in ((none, zeros), (zeros, none)):
+        assert L.qc_w4_linear_grad(P, 0, 8, a, P, 8, b, 0, P, 64, None) == 0
