@@ -164,12 +164,10 @@ int qc_w4_linear_grad(const void *dy, int type, int64_t lddy, const qc_w4_weight
   QC_TRY(check_weight(w, "w"));
   QC_TRY(check_type(type, false));
   QC_TRY(check_rows_of_call(M, w->K));
-  QC_TRY(check_rows_of_call(M, w->N));
   QC_TRY(check_rows(dy, "dy", lddy, M, w->N, type, bytes_of(type)));
   if (w2) {
     QC_TRY(check_weight(w2, "w2"));
     QC_TRY(check_pair(w, w2, false));
-    QC_TRY(check_rows_of_call(M, w2->N));
     QC_TRY(check_rows(dy2, "dy2", lddy2, M, w2->N, type, bytes_of(type)));
   }
   QC_TRY(check_rows(dx, "dx", lddx, M, w->K, type, bytes_of(type)));

@@ -160,3 +160,25 @@ def test_weights_without_rows(qc, asym):
         qc.qc_w4_linear(x, none, empty)
         qc.qc_w4_gated(x, none, none, empty)
     torch.cuda.synchronize()
+
+
+def test_more_than_2_31_gradients(qc):
+    """520 rows of 4194240 gradients: offsets beyond 2^31 elements.  Gradients and weights are positive and grow with row and column, so that a sum
+    over others would show: an accumulator adds N / 32 products of 32 at most."""
+    import torch
+    M, N, K = 520, 4194240, 32
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    q = torch.randint(0, 8, (N, K), generator=gen, device="cuda", dtype=torch.uint8)
+    scale = torch.rand((N, 1), generator=gen, device="cuda") * 0.01 + 0.01
+    W = qc.W4Weight((q[:, 0::2] | (q[:, 1::2] << 4)).contiguous(), scale, 32)
+    dy = torch.rand((M, N), generator=gen, device="cuda", dtype=torch.bfloat16)
+    for m in range(M):
+        dy[m] *= torch.linspace(0.1, 1 + m / M, N, device="cuda")
+    dx = torch.full((M, K), float("nan"), dtype=torch.bfloat16, device="cuda")
+    qc.qc_w4_linear_grad(dy, W, dx)
+    want = torch.zeros((M, K), dtype=torch.float64, device="cuda")
+    for n in range(0, N, 1 << 17):
+        part = slice(n, n + (1 << 17))
+        want += dy[:, part].double() @ (q[part].double() * scale[part].double())
+    assert bool(((dx.double() - want).abs() <= ((200 + N / 32) * E + PARTS["bf16"] + 1.01 * HALF["bf16"]) * want).all())

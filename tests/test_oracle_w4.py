@@ -173,3 +173,11 @@ def test_weights_without_rows_may_lie_nowhere(qc):
     assert L.qc_w4_gated(P, 3, 64, 0.02, 100, none, C.byref(_desc(qc, N=0, zero=P)), None, None, 0, 4, None, 0, None) == 0
     for a, b in ((none, zeros), (zeros, none)):
         assert L.qc_w4_linear_grad(P, 0, 8, a, P, 8, b, 0, P, 64, None) == 0
+
+
+def test_gradients_of_results_may_be_larger_than_results(qc):
+    """The limit of 2^31 elements is the result's, dx; the arguments are checked up to the missing dx."""
+    L, w = qc.lib, C.byref(_desc(qc, N=1 << 18, K=16))
+    assert L.qc_w4_linear_grad(P, 2, 1 << 18, w, None, 0, None, 1 << 14, None, 16, None) == -1
+    assert L.qc_w4_linear_grad(P, 2, 1 << 18, w, P, 1 << 18, w, 1 << 14, None, 16, None) == -1
+    assert L.qc_w4_linear_grad(P, 2, 8, C.byref(_desc(qc, K=1 << 18)), None, 0, None, 1 << 14, P, 1 << 18, None) == -7
