@@ -37,6 +37,13 @@
  * Limits: M below 2^24, N, K and leading dimensions below 2^22, M times a
  * result's columns and N * ceil(K / 32) below 2^31; M = 0 and N = 0 are valid
  * and do nothing (the gradients of N = 0 outputs are zero).
+ * Range: products are scaled after a group's are summed, or gradients before
+ * they are multiplied.  Inputs of magnitude below 2^120 (the products of a group,
+ * 128 of 15/16 of that, then stay in float32), scales below 2^124 and gradients
+ * times scales below 2^124 give what the definition gives; beyond, a result may
+ * be infinite or NaN where the definition's is not.  Float32 inputs, and in
+ * gradients scales and their products, below 2^-110 may lose their last bits.
+ * Infinite and NaN inputs reach the results of their row, and no others.
  */
 #ifndef QC_W4_H_
 #define QC_W4_H_
@@ -54,7 +61,7 @@ enum { QC_ACT_SILU = 0, QC_ACT_GELU = 1 };   /* v / (1 + exp(-v)); the tanh form
 
 typedef struct qc_w4_weight {
   void *q;          /* dev [N, K/2] packed codes, 16-byte aligned                                   */
-  float *scale;     /* dev [N, G], G = ceil(K / group); finite                                      */
+  float *scale;     /* dev [N, G], G = ceil(K / group); of magnitude below 2^124                     */
   uint8_t *zero;    /* dev [N, G] zero points 0..15, or NULL: 8 everywhere (symmetric)              */
   float *sum;       /* dev [N] sum over k of w[n, k]; read for QC_TYPE_I8 inputs only, else may be NULL */
   int32_t N, K;     /* K % 16 == 0                                                                  */

@@ -182,3 +182,35 @@ def test_more_than_2_31_gradients(qc):
         part = slice(n, n + (1 << 17))
         want += dy[:, part].double() @ (q[part].double() * scale[part].double())
     assert bool(((dx.double() - want).abs() <= ((200 + N / 32) * E + PARTS["bf16"] + 1.01 * HALF["bf16"]) * want).all())
+
+
+# ---------------------------------------------------------------- up to the stated range
+def _scaled(qc, rng, N, K, group, e):
+    """Codes of every value with scales just below 2^e."""
+    u, s = rng.integers(0, 16, (N, K)), (rng.uniform(0.5, 1, (N, -(-K // group))) * 2.0 ** e).astype(np.float32)
+    return O.values(u, s, np.full(s.shape, 8), group), qc.W4Weight(_dev(O.pack(u)), _dev(s), group)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("M,N,K", [(3, 100, 272), (70, 500, 272), (4100, 1300, 144)])
+@pytest.mark.parametrize("ex,es", [(120, -20), (-20, 124), (100, 10), (-109, 20), (20, -109)])
+def test_values_up_to_the_stated_range(qc, M, N, K, group, ex, es, dtype):
+    """Inputs and gradients just below 2^ex, scales just below 2^es: sums of many terms."""
+    import torch
+    rng = np.random.default_rng(M + group + ex + 200)
+    v, W = _scaled(qc, rng, N, K, group, es)
+    v64 = _dev(v)
+    for grad in (False, True):
+        a = _dev((rng.uniform(0.5, 0.99, (M, N if grad else K)) * rng.choice([-1.0, 1.0], (M, N if grad else K)) * 2.0 ** ex).astype(np.float32)).to(_type(dtype))
+        y = torch.full((M, K if grad else N), float("nan"), dtype=a.dtype, device="cuda")
+        (qc.qc_w4_linear_grad if grad else qc.qc_w4_linear)(a, W, y)
+        a64 = a.double()
+        if grad:
+            want = a64 @ v64
+            lim = _grad_limit(dtype, [a64], [v64], want)
+        else:
+            want = a64 @ v64.t()
+            tol = (200 + K / 16) * E * (a64.abs() @ v64.t().abs())
+            lim = tol + HALF[dtype] * (want.abs() + tol)
+        assert bool(((y.double() - want).abs() <= lim).all()), grad
