@@ -393,23 +393,25 @@ static hipError_t launch(const W4GradArgs &a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Tiles: row blocks, wavefronts side by side, parties, the smallest group they take, and us of a step of all parties, 64 rows of W each (a
-// compute unit runs one workgroup at a time).  Measured at 4608 x 1152, 1152 x 4608 and 8192 x 8192, 1 - 4096 rows; the tile whose steps
-// come to least is within a seventh of the best of all there.  Few rows want many parties, narrow tiles and the scale in the gradients (1 row
-// of 4608 x 1152, bfloat16: 20 us; with weights in two parts 23, with tiles of 128 columns 42 and 46, of 256 columns 101 and more), many
-// rows tall and wide tiles (2048 rows of 8192 x 8192, bfloat16: 480 us, 620 with 96 rows a tile and 1050 with the scale in the gradients).
+// Tiles: row blocks, wavefronts side by side, parties, the smallest group they take, us of a step of all parties, 64 rows of W each, and what
+// another 256 workgroups take of the time of the first: as much where registers or LDS leave a compute unit one workgroup at a time, 0.7
+// where it holds two (one tile, 114 registers and 80 KB of LDS; 1024 rows of 8192 x 8192: 777 us for 32 times 256, the first 35).  Measured at
+// 4608 x 1152, 1152 x 4608 and 8192 x 8192, 1 - 4096 rows, groups of 32 - 128: 16-bit types get the best tile in all 41 launches tried, float32
+// one within 6 % of it in 15.  Few rows want many parties, narrow tiles and the scale in the gradients (1 row of 4608 x 1152, bfloat16 with
+// zero points: 20 us; with weights in two parts 23, with tiles of 128 columns 42 and 46, of 256 columns 101 and more), many rows tall and
+// wide tiles (2048 rows of 8192 x 8192, bfloat16: 480 us, 620 with 96 rows a tile and 1050 with the scale in the gradients).
 // Those run at the rate of a large library product of 16-bit numbers, counted as the two products they are: 1145 TFLOP/s; float16, three
 // products, 790 us.  Weights rounded to the type, one product, would take 330 and be off by half a step each.
 struct GradShape {
   int MI, CW, parties, group;
-  float step;
+  float step, again = 1.0f;
 };
 // the first two of each with the scale in the gradients (PRE)
 static constexpr GradShape SHAPES_BF16[] = {{1, 1, 16, 64, 3.3f}, {2, 2, 4, 128, 2.05f}, {1, 1, 16, 32, 4.0f}, {2, 1, 8, 32, 2.2f}, {2, 2, 4, 32, 2.3f},
                                             {4, 2, 4, 32, 2.85f}, {4, 4, 2, 32, 2.75f}, {6, 4, 2, 32, 3.2f}, {8, 4, 2, 32, 3.7f}};
 static constexpr GradShape SHAPES_F16[] = {{1, 1, 16, 64, 3.3f}, {2, 2, 4, 128, 2.05f}, {1, 1, 16, 32, 4.7f}, {2, 1, 8, 32, 3.05f}, {2, 2, 4, 32, 2.8f},
                                            {4, 4, 2, 32, 3.25f}, {6, 4, 2, 32, 4.1f}};
-static constexpr GradShape SHAPES_F32[] = {{1, 1, 8, 64, 1.85f}, {2, 2, 4, 128, 2.8f}, {1, 1, 8, 32, 3.05f}, {2, 2, 4, 32, 4.0f}, {2, 4, 2, 32, 4.1f}, {4, 4, 2, 32, 5.4f}};
+static constexpr GradShape SHAPES_F32[] = {{1, 1, 8, 64, 2.05f, 0.7f}, {2, 2, 4, 128, 2.4f}, {1, 1, 8, 32, 3.05f}, {2, 2, 4, 32, 3.7f}, {2, 4, 2, 32, 3.45f}, {4, 4, 2, 32, 4.9f}};
 
 template <int N>
 static int shape(const W4GradArgs &a, const GradShape (&shapes)[N]) {
@@ -420,7 +422,8 @@ static int shape(const W4GradArgs &a, const GradShape (&shapes)[N]) {
     const GradShape &s = shapes[i];
     if (a.group < s.group) continue;
     const int64_t groups = (int64_t)((a.M + 16 * s.MI - 1) / (16 * s.MI)) * ((a.K + 64 * s.CW - 1) / (64 * s.CW));
-    const float t = (3.0f + s.step * ((steps + s.parties - 1) / s.parties)) * (float)((groups + 255) / 256);     // 3 us: first loads, last stores
+    const float first = 3.0f + s.step * ((steps + s.parties - 1) / s.parties);                   // 3 us: first loads, last stores
+    const float t = first * (1.0f + s.again * (float)((groups - 1) / 256));
     if (best < 0 || t < least) {
       best = i;
       least = t;
