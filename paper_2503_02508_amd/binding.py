@@ -232,6 +232,8 @@ class W4Weight:
 
     def __init__(self, q, scale, group, zero=None, sum=None):  # noqa: A002
         import torch
+        if q.dim() != 2:
+            raise QCError(-2, "W4Weight: codes of shape %s; a matrix is needed" % (tuple(q.shape),))
         N, K = q.shape[0], 2 * q.shape[1]
         G = -(-K // group) if group > 0 else 0
         for t, dtype, shape in ((q, torch.uint8, (N, K // 2)), (scale, torch.float32, (N, G)), (zero, torch.uint8, (N, G)),
@@ -248,6 +250,8 @@ class W4Weight:
     def empty(cls, N, K, group, asymmetric=False, device="cuda"):
         """Buffers for qc_w4_quantize."""
         import torch
+        if N < 0 or K < 2 or K % 2 or group < 1:
+            raise QCError(-2, "W4Weight: %d x %d in groups of %d" % (N, K, group))
         G = -(-K // group)
         new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
         return cls(new(N, K // 2, dtype=torch.uint8), new(N, G), group, new(N, G, dtype=torch.uint8) if asymmetric else None, new(N))
@@ -311,7 +315,7 @@ def qc_w4_expand(w, out):
 def qc_w4_linear(x, w, y, bias=None, x_scale=1.0, x_zp=128):
     """y = x w^T + bias; x [M, K] float32 / float16 / bfloat16, or int8 codes with x_scale and x_zp (y float32)."""
     t = _w4_type(x)
-    M = x.shape[0]
+    M = x.shape[0] if x.dim() else 0
     ldx = _w4_rows(x, M, w.K, x.dtype, w.device, "x")
     ldy = _w4_rows(y, M, w.N, x.dtype if t != 3 else w.scale.dtype, w.device, "y")
     _chk(lib.qc_w4_linear(x.data_ptr(), t, ldx, x_scale, x_zp, w.ref, _w4_bias(bias, w), M, y.data_ptr(), ldy, _w4_stream(w)))
@@ -320,7 +324,7 @@ def qc_w4_linear(x, w, y, bias=None, x_scale=1.0, x_zp=128):
 def qc_w4_gated(x, gate, up, h, act=QC_ACT_SILU, gate_bias=None, up_bias=None, x_scale=1.0, x_zp=128):
     """h = act(x gate^T + gate_bias) * (x up^T + up_bias)."""
     t = _w4_type(x)
-    M = x.shape[0]
+    M = x.shape[0] if x.dim() else 0
     ldx = _w4_rows(x, M, gate.K, x.dtype, gate.device, "x")
     ldh = _w4_rows(h, M, gate.N, x.dtype if t != 3 else gate.scale.dtype, gate.device, "h")
     if up.device != gate.device:
@@ -332,7 +336,7 @@ def qc_w4_gated(x, gate, up, h, act=QC_ACT_SILU, gate_bias=None, up_bias=None, x
 def qc_w4_linear_grad(dy, w, dx, dy2=None, w2=None):
     """dx = dy w (+ dy2 w2)."""
     t = _w4_type(dy)
-    M = dy.shape[0]
+    M = dy.shape[0] if dy.dim() else 0
     ld = _w4_rows(dy, M, w.N, dy.dtype, w.device, "dy")
     if (dy2 is None) != (w2 is None):
         raise QCError(-1, "dy2 and w2 belong together")
@@ -346,7 +350,7 @@ def qc_w4_linear_grad(dy, w, dx, dy2=None, w2=None):
 def qc_w4_gated_grad(x, gate, up, dh, dgate, dup, act=QC_ACT_SILU, gate_bias=None, up_bias=None):
     """dgate, dup: gradients of x gate^T + gate_bias and x up^T + up_bias, from dh."""
     t = _w4_type(x)
-    M = x.shape[0]
+    M = x.shape[0] if x.dim() else 0
     ldx = _w4_rows(x, M, gate.K, x.dtype, gate.device, "x")
     lddh = _w4_rows(dh, M, gate.N, x.dtype, gate.device, "dh")
     ldd = _w4_rows(dgate, M, gate.N, x.dtype, gate.device, "dgate")

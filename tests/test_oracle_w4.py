@@ -181,3 +181,19 @@ def test_gradients_of_results_may_be_larger_than_results(qc):
     assert L.qc_w4_linear_grad(P, 2, 1 << 18, w, None, 0, None, 1 << 14, None, 16, None) == -1
     assert L.qc_w4_linear_grad(P, 2, 1 << 18, w, P, 1 << 18, w, 1 << 14, None, 16, None) == -1
     assert L.qc_w4_linear_grad(P, 2, 8, C.byref(_desc(qc, K=1 << 18)), None, 0, None, 1 << 14, P, 1 << 18, None) == -7
+
+
+def test_tensors_of_other_dimensions_are_refused_like_other_shapes(qc):
+    import torch
+    w = qc.W4Weight.empty(4, 64, 32, device="cpu")
+    for kw in (dict(group=0), dict(group=-32), dict(K=17), dict(K=0), dict(N=-1)):
+        with pytest.raises(qc.QCError):
+            qc.W4Weight.empty(**{**dict(N=4, K=64, group=32, device="cpu"), **kw})
+    for q in (torch.zeros(32, dtype=torch.uint8), torch.zeros((), dtype=torch.uint8), torch.zeros((4, 4, 8), dtype=torch.uint8)):
+        with pytest.raises(qc.QCError):
+            qc.W4Weight(q, w.scale, 32)
+    x, one = torch.zeros(2, 64), torch.zeros(())
+    for call, args in ((qc.qc_w4_linear, (one, w, x)), (qc.qc_w4_gated, (one, w, w, x)), (qc.qc_w4_linear_grad, (one, w, x)),
+                       (qc.qc_w4_gated_grad, (one, w, w, x, x, x)), (qc.qc_w4_quantize, (one, w)), (qc.qc_w4_expand, (w, one))):
+        with pytest.raises(qc.QCError):
+            call(*args)
