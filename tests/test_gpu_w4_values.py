@@ -314,3 +314,40 @@ def test_every_tile_of_the_input_gradient(qc, M, N, K, asym, group, dtype):
         d64, v64 = [d.double() for d in dys[:n]], [v for v, _ in ws[:n]]
         want = sum(d @ v for d, v in zip(d64, v64))
         assert bool(((dx.double() - want).abs() <= _grad_limit(dtype, d64, v64, want)).all()) and _untouched(dx, buf)
+
+
+# ---------------------------------------------------------------- up to the stated sizes
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "i8"])
+@pytest.mark.parametrize("M,N,K", [((1 << 24) - 1, 5, 16), (3, (1 << 22) - 1, 16), (2, 3, (1 << 22) - 16)])
+def test_sizes_up_to_the_limits(qc, M, N, K, dtype):
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(7)
+    v, w = _quantised(qc, gen, N, K, 32, True)
+    t = "f32" if dtype == "i8" else dtype
+    if dtype == "i8":
+        x, kw = torch.randint(-128, 128, (M, K), generator=gen, device="cuda", dtype=torch.int8), dict(x_scale=1.0, x_zp=128)
+    else:
+        x, kw = torch.randn((M, K), generator=gen, device="cuda", dtype=_type(dtype)), {}
+    y = torch.full((M, N), float("nan"), dtype=_type(t), device="cuda")
+    qc.qc_w4_linear(x, w, y, **kw)
+    dx = dy = None
+    if dtype != "i8":
+        dy = torch.randn((M, N), generator=gen, device="cuda", dtype=_type(dtype))
+        dx = torch.full((M, K), float("nan"), dtype=dy.dtype, device="cuda")
+        qc.qc_w4_linear_grad(dy, w, dx)
+    step = 1 << 20
+    for m in range(0, M, step):
+        a = x[m:m + step].double()
+        want = a @ v.t()
+        tol = (200 + K / 16) * E * (a.abs() @ v.t().abs())
+        assert bool(((y[m:m + step].double() - want).abs() <= tol + HALF[t] * (want.abs() + tol)).all()), m
+        if dx is not None:
+            g = dy[m:m + step].double()
+            want = g @ v
+            assert bool(((dx[m:m + step].double() - want).abs() <= _grad_limit(dtype, [g], [v], want)).all()), m
+    if M == 2:                                         # one row of weights is as long as rows get
+        W, out = qc.W4Weight.empty(N, K, 32, True), torch.empty((N, K), device="cuda")
+        qc.qc_w4_quantize(v.float(), W)
+        qc.qc_w4_expand(W, out)
+        assert bool(((out.double() - v).abs() <= 0.501 * W.scale.double().repeat_interleave(32, 1)[:, :K] * 2).all())
