@@ -6,7 +6,7 @@
 // product is scaled in float32 as it is added: the codes themselves are exact in every type, and float32 inputs are three bfloat16
 // numbers each.  The wavefronts' sums are added in LDS in wavefront order.
 //
-// One row is bound by the weights' bytes and by the instructions that expand them: 28672 x 8192 float16 in groups of 64 with zero points
+// One row takes the weights' bytes and the instructions that expand them, and fills neither limit: 28672 x 8192 float16 in groups of 64 with zero points
 // takes 42 us, 3.2 TB/s of codes and scales, its SIMDs issuing vector instructions 64 % of the time (8-bit inputs, which need fewest,
 // 4.4 TB/s without zero points; a large copy reads and writes 5.2).  Sixteen neighbouring lanes are looked up in the cache together, a
 // line a clock: with lanes in the products' order, 16 rows in each look-up, the same took 80 us, and 16 rows of 8192 x 8192
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * rows_most(TYPE, MT, NT * (OP == W4_LINEAR ? 1 
   using F = FragOf<TYPE>;
   using T = typename W4Mem<TYPE>::T;
   constexpr int P = TYPE == QC_TYPE_F32 ? 3 : 1, ES = RowsX<TYPE>::ES, MATS = OP == W4_LINEAR ? 1 : 2, NW = MATS * NT;
-  constexpr int AHEAD = MT == 1 ? 2 : 1;         // chunks asked for before they are needed
+  constexpr int AHEAD = MT == 1 ? 2 : 1;         // chunks that registers hold: with two the next one is asked for before this one is used
   constexpr bool LATE = TYPE == QC_TYPE_F32 && MT > 1;                  // inputs a product ahead only: a chunk's are 32 MT registers
   constexpr int XJ = LATE ? 2 : 4;
   extern __shared__ float red[];                 // [wavefronts][NW][MT][64][4]
@@ -254,8 +254,9 @@ static hipError_t rows_launch(const W4Args &a, hipStream_t st) {
 // Tiles of this kernel, MT row blocks by NW column blocks of both matrices, and what a step (a chunk of every wavefront of a workgroup)
 // of theirs takes in us: alone, and for each 8 or 16 wavefronts (rows_most) that a compute unit has to run.  And what a chunk takes the
 // kernel of large tiles (w4_tile.hip), alone and with every compute unit holding as many of its workgroups as fit, `full_at` in all.
-// Measured with groups of 128 at 4608 x 1152, 1152 x 4608 and 8192 x 8192, 1 - 512 rows and, the large tiles, 4096 and 8192.  A
-// launch takes what comes to least; against the best there that loses up to a fifth, and mostly nothing.
+// Measured with groups of 128 at 4608 x 1152, 1152 x 4608 and 8192 x 8192, 1 - 512 rows and, the large tiles, 4096 and 8192; smaller groups
+// are taken to cost their kernels alike.  A launch takes what comes to least; against the best there that loses up to a fifth, and mostly
+// nothing.
 struct RowsTile {
   int MT, NW;
   float alone, full;

@@ -6,8 +6,8 @@
 // wavefronts read.  The products of one group are summed apart and scaled in float32 as they are added: the codes are exact.
 //
 // What bounds it is the issue of vector instructions: a chunk of 80 rows and 64 columns in groups of 128 (bfloat16) is 80 matrix
-// instructions of 16 clocks and 354 others of 4, most of them expansion (1.6 a weight) and scaling (1 for each result and group), so two
-// wavefronts a SIMD must share 1736 clocks each while the matrix unit needs 1280.  8192 x 8192 x 8192 bfloat16 runs at 960 TFLOP/s
+// instructions of 16 clocks and 354 others of 4 (494 with zero points), most of them expansion (1.6 a weight; 2.7) and scaling (1 for each
+// result and group), so two wavefronts a SIMD must share 1736 clocks each while the matrix unit needs 1280.  8192 x 8192 x 8192 bfloat16 runs at 960 TFLOP/s
 // (the library's product of 16-bit matrices reaches 1140), 8-bit inputs at 1490 TOP/s (1715).  Scaling the weights first would save
 // the second part and round every weight.  More row blocks a tile amortise the expansion, but a register in scratch memory makes the
 // next wait one for every load in flight: 8 row blocks of 16-bit types spilled 11 registers and took 98 us at 4096 x 4608 x 1152 where 5
@@ -317,7 +317,8 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(W4Args a, int tm, int t
   }
 }
 
-// row blocks of a tile: as many as 256 registers hold without spilling
+// row blocks of a tile: as many as 256 registers hold without spilling, float32 with zero points apart, which keeps 1 - 5 of them in scratch
+// memory (seven kernels)
 static constexpr int tile_mi_of(int type, int group) { return type == QC_TYPE_F32 ? 4 : type == QC_TYPE_I8 ? 8 : group == 128 ? 5 : 6; }
 int w4_tile_rows(const W4Args &a, int type) { return 16 * tile_mi_of(type, a.group); }
 

@@ -2,8 +2,8 @@
 //
 // Both move memory only: the quantiser reads a matrix once and writes an eighth (float32) or a quarter of its bytes, the
 // expansion does the reverse.  A workgroup takes a row, a lane 8 neighbouring values (a group of 32, 64 or 128 lies in 4, 8 or
-// 16 neighbouring lanes and is reduced without LDS).  16-bit matrices leave the quantiser bound by its own arithmetic: 8192 x 8192
-// bfloat16 take 53 us (3.2 TB/s), float32 59 us (5.2 TB/s, what a large copy reaches); with eight IEEE divisions a lane and reductions
+// 16 neighbouring lanes and is reduced without LDS).  16-bit matrices leave the quantiser between its bytes and its arithmetic: 8192 x 8192
+// bfloat16 take 52 us (3.3 TB/s), of which 22 vector instructions a value need 37 to issue and the bytes 33; float32 59 us (5.2 TB/s, what a large copy reaches); with eight IEEE divisions a lane and reductions
 // through LDS they took 65 and 70.  The expansion: 35 us (4.9 TB/s) and 67 us (4.5 TB/s).
 #include "w4_common.h"
 
