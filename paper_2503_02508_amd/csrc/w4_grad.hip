@@ -46,9 +46,6 @@ struct GradTile {
 // 16-byte unit u of row r of a plane: 16 rows of one unit lie in 16 different slots of 256 bytes
 __device__ __forceinline__ int gt_slot(int r, int u) { return r * 128 + ((u ^ ((r >> 1) & 7)) << 4); }
 
-// PRE: the tile's columns lie in one group, so that the scale of a weight row multiplies the gradients as they go to LDS, and the
-// weights are exact codes, of which nothing has to be split: three products for six (float32), two for three (float16), and few instructions a
-// weight where there are few rows to pay for it
 // a weight in two parts.  The first is cut off below the weight itself, so that the second has its sign and is not zero either: what an
 // infinite gradient gives is the weight's infinity, and NaN only where the weight is zero.
 __device__ __forceinline__ void gt_weight(float v, float p[2]) {
@@ -61,6 +58,9 @@ __device__ __forceinline__ unsigned gt_round_bf16(float lo, float hi) {
   return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{lo, hi}), b2));
 }
 
+// PRE: the tile's columns lie in one group, so that the scale of a weight row multiplies the gradients as they go to LDS, and the
+// weights are exact codes, of which nothing has to be split: three products for six (float32), two for three (float16), and few
+// instructions a weight where there are few rows to pay for it
 template <int TYPE, int MI, int CW, bool ASYM, bool PRE>
 __global__ __launch_bounds__((64 * GradTile<TYPE, MI, CW, PRE>::WV), 2) void w4_grad_kernel(W4GradArgs a, int tm, int tk) {
   using T = typename W4Mem<TYPE>::T;

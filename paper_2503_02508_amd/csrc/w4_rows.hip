@@ -6,9 +6,9 @@
 // product is scaled in float32 as it is added: the codes themselves are exact in every type, and float32 inputs are three bfloat16
 // numbers each.  The wavefronts' sums are added in LDS in wavefront order.
 //
-// One row takes the weights' bytes and the instructions that expand them, and fills neither limit: 28672 x 8192 float16 in groups of 64 with zero points
-// takes 42 us, 3.2 TB/s of codes and scales, its SIMDs issuing vector instructions 64 % of the time (8-bit inputs, which need fewest,
-// 4.4 TB/s without zero points; a large copy reads and writes 5.2).  Sixteen neighbouring lanes are looked up in the cache together, a
+// One row takes the weights' bytes and the instructions that expand them, and fills neither limit: 28672 x 8192 float16 in groups of 64
+// with zero points takes 42 us, 3.2 TB/s of codes and scales, its SIMDs issuing vector instructions 64 % of the time (8-bit inputs, which
+// need fewest, 4.4 TB/s without zero points; a large copy reads and writes 5.2).  Sixteen neighbouring lanes are looked up in the cache together, a
 // line a clock: with lanes in the products' order, 16 rows in each look-up, the same took 80 us, and 16 rows of 8192 x 8192
 // bfloat16 29 us instead of 16.  Loads that ran further ahead, whole cache lines a row and scales asked for a pair of chunks earlier
 // changed nothing or cost registers.
