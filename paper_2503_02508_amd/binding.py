@@ -16,6 +16,8 @@ __all__ = [
     "qc_tap_aggregate", "qc_tap_cluster", "qc_tap_profile_begin", "qc_tap_profile_end",
     "W4Weight", "QC_ACT_SILU", "QC_ACT_GELU", "qc_w4_quantize", "qc_w4_expand", "qc_w4_linear", "qc_w4_gated",
     "qc_w4_linear_grad", "qc_w4_gated_grad",
+    "qc_t8_norm", "qc_t8_norm_grad_bytes", "qc_t8_norm_grad", "qc_t8_quantize", "qc_t8_expand", "qc_t8_gated_grad", "qc_t8_linear",
+    "qc_t8_linear_grad_bytes", "qc_t8_linear_grad",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libqc.so")
@@ -100,6 +102,15 @@ _SIGS = {
     "qc_w4_gated": (i32, [vp, i32, i64, f32, i32, _W4, _W4, vp, vp, i32, i32, vp, i64, vp]),
     "qc_w4_linear_grad": (i32, [vp, i32, i64, _W4, vp, i64, _W4, i32, vp, i64, vp]),
     "qc_w4_gated_grad": (i32, [vp, i32, i64, _W4, _W4, vp, vp, i32, vp, i64, i32, vp, vp, i64, vp]),
+    "qc_t8_norm": (i32, [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp]),
+    "qc_t8_norm_grad_bytes": (i32, [i32, i32, C.POINTER(sz)]),
+    "qc_t8_norm_grad": (i32, [vp, i64, vp, f32, vp, i64, vp, i64, i32, i32, i32, vp, i64, vp, vp, sz, vp]),
+    "qc_t8_quantize": (i32, [vp, i64, vp, i64, i32, i32, i32, i32, vp, i64, vp, vp]),
+    "qc_t8_expand": (i32, [vp, i64, vp, i32, i32, vp, i32, i64, vp]),
+    "qc_t8_gated_grad": (i32, [vp, i64, vp, i64, i32, vp, i64, i32, i32, i32, vp, i64, vp, i64, vp]),
+    "qc_t8_linear": (i32, [vp, i64, vp, vp, i64, vp, vp, i32, i32, i32, vp, i32, i64, vp]),
+    "qc_t8_linear_grad_bytes": (i32, [i32, i32, i32, i32, C.POINTER(sz)]),
+    "qc_t8_linear_grad": (i32, [vp, i64, i32, vp, i64, vp, i32, i32, i32, vp, i64, vp, sz, vp]),
     "qc_profile_begin": (i32, [vp]),
     "qc_profile_end": (i32, [vp, i32, C.POINTER(C.c_int32), C.POINTER(f32), vp]),
 }
@@ -360,6 +371,117 @@ def qc_w4_gated_grad(x, gate, up, dh, dgate, dup, act=QC_ACT_SILU, gate_bias=Non
         raise QCError(-2, "the weights lie on different devices")
     _chk(lib.qc_w4_gated_grad(x.data_ptr(), t, ldx, gate.ref, up.ref, _w4_bias(gate_bias, gate), _w4_bias(up_bias, up), act,
                               dh.data_ptr(), lddh, M, dgate.data_ptr(), dup.data_ptr(), ldd, _w4_stream(gate)))
+
+
+# ------------------------------------------------ 8-bit layers with a scale for each token (include/qc_t8.h)
+def _t8_shape(t, name):
+    if t.dim() != 2:
+        raise QCError(-2, "%s: a tensor of shape %s; a matrix is needed" % (name, tuple(t.shape)))
+    return t.shape
+
+
+def _t8_vector(t, n, device, name):
+    if t is None:
+        return None
+    if t.dtype is not _w4_torch.float32 or t.shape != (n,) or t.device != device or (n > 1 and t.stride(0) != 1):
+        raise QCError(-2, "%s: a contiguous float32 vector of %d elements on %s is needed" % (name, n, device))
+    return t.data_ptr()
+
+
+def _t8_work(t, device):
+    if t is None:
+        return None, 0
+    if not t.is_contiguous() or t.device != device:
+        raise QCError(-2, "work: a contiguous tensor on %s is needed" % device)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _t8_stream(device):
+    # (private functions of torch 2.10, as in _stream)
+    if device.type != "cuda" or device.index != _w4_torch.cuda.current_device():
+        raise QCError(-2, "the tensors lie on %s, which is not the current GPU" % device)
+    return _w4_torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def qc_t8_norm(x, q=None, scale=None, weight=None, residual=None, h=None, y=None, eps=1e-6):
+    """Codes q with the rows' scales, and / or y, of the root-mean-square norm of h = x + residual (h = x without)."""
+    M, K = _t8_shape(x, "x")
+    t, dt, dev = _w4_type(x), x.dtype, x.device
+    if t == 3:
+        raise QCError(-7, "tensors of type %s are not supported" % dt)
+    rows = lambda v, name, d=dt: 0 if v is None else _w4_rows(v, M, K, d, dev, name)  # noqa: E731
+    _chk(lib.qc_t8_norm(x.data_ptr(), rows(x, "x"), _p(residual), rows(residual, "residual"), _t8_vector(weight, K, dev, "weight"), eps, t, M, K, _p(h),
+                        rows(h, "h"), _p(y), rows(y, "y"), _p(q), rows(q, "q", _w4_torch.int8), _t8_vector(scale, M, dev, "scale"), _t8_stream(dev)))
+
+
+def qc_t8_norm_grad_bytes(M, K) -> int:
+    out = sz()
+    _chk(lib.qc_t8_norm_grad_bytes(M, K, C.byref(out)))
+    return out.value
+
+
+def qc_t8_norm_grad(h, dy, dx, weight=None, dh=None, dweight=None, work=None, eps=1e-6):
+    """dx (of x and of the residual) and dweight, from the gradients of y and (dh) of h."""
+    M, K = _t8_shape(h, "h")
+    t, dt, dev = _w4_type(h), h.dtype, h.device
+    rows = lambda v, name: 0 if v is None else _w4_rows(v, M, K, dt, dev, name)  # noqa: E731
+    w, n = _t8_work(work, dev)
+    _chk(lib.qc_t8_norm_grad(h.data_ptr(), rows(h, "h"), _t8_vector(weight, K, dev, "weight"), eps, dy.data_ptr(), rows(dy, "dy"), _p(dh), rows(dh, "dh"), t,
+                             M, K, dx.data_ptr(), rows(dx, "dx"), _t8_vector(dweight, K, dev, "dweight"), w, n, _t8_stream(dev)))
+
+
+def qc_t8_quantize(x, q, scale, gate=None, act=QC_ACT_SILU):
+    """Codes and scales of the rows of x, or of act(gate) x."""
+    M, K = _t8_shape(x, "x")
+    t, dt, dev = _w4_type(x), x.dtype, x.device
+    ldg = 0 if gate is None else _w4_rows(gate, M, K, dt, dev, "gate")
+    _chk(lib.qc_t8_quantize(x.data_ptr(), _w4_rows(x, M, K, dt, dev, "x"), _p(gate), ldg, act, t, M, K, q.data_ptr(),
+                            _w4_rows(q, M, K, _w4_torch.int8, dev, "q"), _t8_vector(scale, M, dev, "scale"), _t8_stream(dev)))
+
+
+def qc_t8_expand(q, scale, out):
+    """out = scale q: what rows of codes stand for."""
+    M, K = _t8_shape(out, "out")
+    t, dev = _w4_type(out), out.device
+    _chk(lib.qc_t8_expand(q.data_ptr(), _w4_rows(q, M, K, _w4_torch.int8, dev, "q"), _t8_vector(scale, M, dev, "scale"), M, K, out.data_ptr(), t,
+                          _w4_rows(out, M, K, out.dtype, dev, "out"), _t8_stream(dev)))
+
+
+def qc_t8_gated_grad(x, gate, dv, dx, dgate, act=QC_ACT_SILU):
+    """Gradients of act(gate) x."""
+    M, K = _t8_shape(x, "x")
+    t, dt, dev = _w4_type(x), x.dtype, x.device
+    rows = lambda v, name: _w4_rows(v, M, K, dt, dev, name)  # noqa: E731
+    _chk(lib.qc_t8_gated_grad(x.data_ptr(), rows(x, "x"), gate.data_ptr(), rows(gate, "gate"), act, dv.data_ptr(), rows(dv, "dv"), t, M, K, dx.data_ptr(),
+                              rows(dx, "dx"), dgate.data_ptr(), rows(dgate, "dgate"), _t8_stream(dev)))
+
+
+def qc_t8_linear(qx, x_scale, qw, w_scale, y, bias=None):
+    """y = x w^T + bias of rows of codes."""
+    M, K = _t8_shape(qx, "qx")
+    N = _t8_shape(qw, "qw")[0]
+    t, dev = _w4_type(y), qx.device
+    i8 = _w4_torch.int8
+    _chk(lib.qc_t8_linear(qx.data_ptr(), _w4_rows(qx, M, K, i8, dev, "qx"), _t8_vector(x_scale, M, dev, "x_scale"), qw.data_ptr(),
+                          _w4_rows(qw, N, K, i8, dev, "qw"), _t8_vector(w_scale, N, dev, "w_scale"), _t8_vector(bias, N, dev, "bias"), M, N, K,
+                          y.data_ptr(), t, _w4_rows(y, M, N, y.dtype, dev, "y"), _t8_stream(dev)))
+
+
+def qc_t8_linear_grad_bytes(M, N, K, dtype) -> int:
+    import torch
+    out = sz()
+    _chk(lib.qc_t8_linear_grad_bytes(M, N, K, _w4_type(torch.empty(0, dtype=dtype)), C.byref(out)))
+    return out.value
+
+
+def qc_t8_linear_grad(dy, qw, w_scale, dx, work):
+    """dx = dy w."""
+    N, K = _t8_shape(qw, "qw")
+    M = _t8_shape(dy, "dy")[0]
+    t, dt, dev = _w4_type(dy), dy.dtype, dy.device
+    w, n = _t8_work(work, dev)
+    _chk(lib.qc_t8_linear_grad(dy.data_ptr(), _w4_rows(dy, M, N, dt, dev, "dy"), t, qw.data_ptr(), _w4_rows(qw, N, K, _w4_torch.int8, dev, "qw"),
+                               _t8_vector(w_scale, N, dev, "w_scale"), M, N, K, dx.data_ptr(), _w4_rows(dx, M, K, dt, dev, "dx"), w, n, _t8_stream(dev)))
 
 
 def qc_ddim_schedule(steps: int):

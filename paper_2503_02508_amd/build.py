@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libqc.so")
 SOURCES = ["api.hip", "gemm_i8.hip", "gemm_i8_big.hip", "gemm_i8_split.hip", "linear_f32.hip", "rowops.hip", "attention.hip", "tap.hip",
-           "w4_api.hip", "w4_weight.hip", "w4_rows.hip", "w4_tile.hip", "w4_grad.hip"]
+           "w4_api.hip", "w4_weight.hip", "w4_rows.hip", "w4_tile.hip", "w4_grad.hip", "t8_api.hip", "t8_rows.hip",
+           "t8_norm_grad.hip", "t8_few.hip", "t8_tile.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-fhip-fp32-correctly-rounded-divide-sqrt", "-ffp-contract=on",

@@ -1,0 +1,214 @@
+// Shared by the kernels of the 8-bit layers with a scale for each token (include/qc_t8.h).
+#pragma once
+#include "qc_t8.h"
+#include "w4_common.h"
+
+namespace qc {
+
+// rows to codes, by what is quantised (t8_rows.hip)
+enum T8Source { T8_PLAIN = 0, T8_GATED = 1, T8_NORM = 2, T8_PLANES = 3 };
+
+struct T8RowArgs {
+  const void *x;            // [M, K]; T8_PLANES: the gradients
+  int64_t ldx;
+  const void *add;          // T8_GATED: gates; T8_NORM: residual, or null
+  int64_t lda;
+  const float *w;           // [K]: the norm's weight, or null; T8_PLANES: the scales of the weights' rows
+  void *h, *y;              // T8_NORM: the sum with the residual, the normalised rows, or null
+  int64_t ldh, ldy;
+  int8_t *q;                // T8_PLANES: the planes, rows of `pitch` bytes, and behind `scale` the rows' scales
+  int64_t ldq;
+  float *scale;
+  int M, K, act;
+  float eps;
+  int planes, pitch;        // T8_PLANES
+};
+
+struct T8NormGradArgs {
+  const void *h, *dy, *dh;
+  int64_t ldh, lddy, lddh;
+  const float *w;
+  void *dx;
+  int64_t lddx;
+  float *dw, *part;         // part: [groups, K]
+  int M, K, groups;
+  float eps;
+};
+
+// T8_PLANES: bytes that stand for a gradient, and the rows of the matrix of planes.  Row m's plane p (the lowest byte is 0) is row
+// (m / 16 P + p) 16 + m % 16: the 16-row operands of a matrix instruction, a row block's planes one behind the other.
+constexpr int t8_planes(int type) { return type == QC_TYPE_F32 ? 4 : 2; }
+__host__ __device__ inline int64_t t8_plane_row(int m, int p, int planes) { return ((int64_t)(m >> 4) * planes + p) * 16 + (m & 15); }
+
+struct T8Product {
+  const int8_t *a;          // [rows, lda]: codes, or the planes of gradients
+  int64_t lda;
+  const int8_t *w;          // [N, K], rows ldw apart
+  int64_t ldw;
+  const float *xs, *ws, *bias;   // scales of the rows and of the columns (the gradient has none: null)
+  int M, N, K;              // rows and columns of the result, length of the summed axis
+  int arows;                // rows of `a` (M, or M's blocks of planes)
+  void *y;
+  int64_t ldy;
+  int tm, tn;               // grid of tiles
+  int split, per;           // parts of the summed axis, slabs of each; their sums
+  int32_t *part;
+};
+
+constexpr int T8_SLAB = 128;     // the summed axis of the planes is padded to it
+
+hipError_t launch_t8_rows(const T8RowArgs &a, int type, int source, hipStream_t st);
+hipError_t launch_t8_expand(const int8_t *q, int64_t ldq, const float *scale, int M, int K, void *out, int type, int64_t ldo, hipStream_t st);
+hipError_t launch_t8_gated_grad(const void *x, int64_t ldx, const void *g, int64_t ldg, int act, const void *dv, int64_t lddv, int type, int M, int K,
+                                void *dx, int64_t lddx, void *dg, int64_t lddg, hipStream_t st);
+int t8_norm_grad_groups(int M, int K);
+hipError_t launch_t8_norm_grad(const T8NormGradArgs &a, int type, hipStream_t st);
+hipError_t launch_t8_linear(T8Product a, int type, hipStream_t st);
+// bytes of the partial sums of a gradient (0: the summed axis is not split)
+int64_t t8_grad_part_bytes(int M, int N, int K, int type);
+hipError_t launch_t8_grad(T8Product a, int type, hipStream_t st);
+// rows of zeros: the gradient of a sum without terms
+hipError_t launch_t8_zero(void *x, int type, int M, int K, int64_t ld, hipStream_t st);
+
+// ---- vectors of 16 bytes at any alignment of their elements
+typedef w4_u4 t8_u4 __attribute__((aligned(1)));
+typedef w4_u2 t8_u2 __attribute__((aligned(1)));
+typedef unsigned t8_u1 __attribute__((aligned(1)));
+
+template <int TYPE>
+constexpr int t8_vl = TYPE == QC_TYPE_F32 ? 4 : 8;        // elements of such a vector
+
+// elements e .. of a row of K as float32, zeros beyond it
+template <int TYPE>
+__device__ __forceinline__ void t8_load(const typename W4Mem<TYPE>::T *row, int e, int K, float v[t8_vl<TYPE>]) {
+  constexpr int VL = t8_vl<TYPE>;
+  using T = typename W4Mem<TYPE>::T;
+  typedef T vec __attribute__((ext_vector_type(VL)));
+  if (e + VL <= K) {
+    const vec r = __builtin_bit_cast(vec, (w4_u4) * (const t8_u4 *)(row + e));
+#pragma unroll
+    for (int i = 0; i < VL; ++i) v[i] = W4Mem<TYPE>::get(r[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VL; ++i) v[i] = e + i < K ? W4Mem<TYPE>::get(row[e + i]) : 0.0f;
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ void t8_store(typename W4Mem<TYPE>::T *row, int e, int K, const float v[t8_vl<TYPE>]) {
+  constexpr int VL = t8_vl<TYPE>;
+  using T = typename W4Mem<TYPE>::T;
+  typedef T vec __attribute__((ext_vector_type(VL)));
+  if (e + VL <= K) {
+    vec r;
+#pragma unroll
+    for (int i = 0; i < VL; ++i) r[i] = W4Mem<TYPE>::put(v[i]);
+    *(t8_u4 *)(row + e) = __builtin_bit_cast(w4_u4, r);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VL; ++i)
+      if (e + i < K) row[e + i] = W4Mem<TYPE>::put(v[i]);
+  }
+}
+template <int VL>
+__device__ __forceinline__ void t8_load_f32(const float *w, int e, int K, float v[VL]) {
+  if (e + VL <= K) {
+#pragma unroll
+    for (int i = 0; i < VL; i += 4) {
+      const w4_f4 r = __builtin_bit_cast(w4_f4, (w4_u4) * (const t8_u4 *)(w + e + i));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i + j] = r[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VL; ++i) v[i] = e + i < K ? w[e + i] : 0.0f;
+  }
+}
+// the low bytes of VL words, as bytes e .. of a row
+template <int VL>
+__device__ __forceinline__ void t8_store_bytes(int8_t *row, int e, int K, const unsigned b[VL]) {
+  if (e + VL <= K) {
+    unsigned w[VL / 4];
+#pragma unroll
+    for (int i = 0; i < VL / 4; ++i)
+      w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x0c0c0400u), __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u),
+                                   0x05040100u);
+    if constexpr (VL == 8) *(t8_u2 *)(row + e) = w4_u2{w[0], w[1]};
+    else *(t8_u1 *)(row + e) = w[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < VL; ++i)
+      if (e + i < K) row[e + i] = (int8_t)b[i];
+  }
+}
+
+// ---- reductions over a wavefront, the same value in every lane
+template <int CTRL>
+__device__ __forceinline__ unsigned t8_dpp(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false); }
+__device__ __forceinline__ unsigned t8_wave_max(unsigned v) {
+  v = max(v, t8_dpp<0xB1>(v));
+  v = max(v, t8_dpp<0x4E>(v));
+  v = max(v, t8_dpp<0x141>(v));
+  v = max(v, t8_dpp<0x140>(v));
+  const unsigned a = max((unsigned)__builtin_amdgcn_readlane((int)v, 0), (unsigned)__builtin_amdgcn_readlane((int)v, 16));
+  return max(a, max((unsigned)__builtin_amdgcn_readlane((int)v, 32), (unsigned)__builtin_amdgcn_readlane((int)v, 48)));
+}
+// |v| as a word: ordered as the magnitudes are, infinities above them and NaN above those
+__device__ __forceinline__ unsigned t8_mag(float v) { return __builtin_bit_cast(unsigned, v) & 0x7FFFFFFFu; }
+
+// 1 / sqrt(v) in float64 and its float32 rounding: the hardware's estimate and two Newton steps (v is normal and positive;
+// infinite and NaN sums give 0 or NaN, whose rows are NaN either way)
+__device__ __forceinline__ double t8_rsqrt(double v) {
+  double y = __builtin_amdgcn_rsq(v);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) y = __builtin_fma(y * 0.5, __builtin_fma(-v * y, y, 1.0), y);
+  return y;
+}
+
+// ---- the gated block's activations
+// exact to float64: v times a logistic function, v / (1 + exp(-t)); (1 + tanh(y)) / 2 is the logistic function of 2 y
+__device__ __forceinline__ double t8_gate_exact(int act, float gate, float x) {
+  const double g = gate, t = act == QC_ACT_SILU ? g : g * (1.5957691216057307117 + 1.5957691216057307117 * 0.044715 * g * g);
+  return g / (1.0 + exp(-t)) * (double)x;
+}
+// float32: `s` the logistic function, `o` one minus it.  The exponent's argument is taken in float64 and handed on as two float32
+// numbers, so that the error does not grow with it: off by at most 9 e (e = 2^-24) of the value while that is above 2^-100; below,
+// s 2^100 (o 2^100) is returned in its place and `deep` is set.
+__device__ __forceinline__ void t8_logistic(int act, float gate, float &s, float &o, bool &deep) {
+  const double g = gate;
+  double u = act == QC_ACT_SILU ? g * 1.4426950408889634 : g * (2.302208198144325 + 0.1029432395800235 * (g * g));
+  u = fmin(fmax(u, -400.0), 400.0);                       // 2^-400 is 0 to any product below; a NaN comes back through `gate`
+  const double a = fabs(u);
+  const float hi = (float)a, lo = (float)(a - (double)hi);
+  deep = hi > 100.0f;
+  const float e = __builtin_amdgcn_exp2f(deep ? 100.0f - hi : -hi);
+  const float z = __builtin_fmaf(e, lo * -0.6931471805599453f, e);
+  const float r = deep ? 1.0f : __builtin_amdgcn_rcpf(1.0f + z);
+  s = u < 0.0 ? z * r : r;
+  o = u < 0.0 ? r : z * r;
+}
+// act(gate) x, to 13 e of its value while that is above 2^-90
+__device__ __forceinline__ float t8_gate(int act, float gate, float x) {
+  float s, o;
+  bool deep;
+  t8_logistic(act, gate, s, o, deep);
+  return gate * s * (deep && gate < 0.0f ? x * 0x1p-100f : x);
+}
+// value and derivative of the activation
+__device__ __forceinline__ float t8_act(int act, float gate, float &d) {
+  float s, o;
+  bool deep;
+  t8_logistic(act, gate, s, o, deep);
+  const bool low = deep && gate < 0.0f;                   // s is 2^100 times what it stands for; else o, which is nothing beside 1
+  if (deep && !low) o *= 0x1p-100f;
+  if (act == QC_ACT_SILU) {
+    d = __builtin_fmaf(gate * o, s, s);
+  } else {
+    const float b = fabsf(gate) > 30.0f ? copysignf(30.0f, gate) : gate;      // beyond, s o is 0 (the comparison leaves NaN as it is)
+    d = __builtin_fmaf(b * (1.5957691216057308f * (1.0f + 0.134145f * (b * b))) * o, s, s);
+  }
+  const float v = gate * s;
+  d = low ? d * 0x1p-100f : d;
+  return low ? v * 0x1p-100f : v;
+}
+
+}  // namespace qc

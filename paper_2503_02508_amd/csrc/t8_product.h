@@ -1,0 +1,46 @@
+// Parts of the products of the 8-bit layers with a scale for each token.
+#pragma once
+#include "t8_common.h"
+
+namespace qc {
+
+typedef int t8_i4 __attribute__((ext_vector_type(4)));
+typedef int t8_i2 __attribute__((ext_vector_type(2)));
+
+// 1024 bytes from memory to LDS, 16 a lane: lane after lane from `lds` on.  (m0 is a reserved register, which a clobber list cannot name:
+// nothing else in these kernels uses it, tests/test_codegen_t8_cpu.py)
+__device__ __forceinline__ void t8_to_lds(unsigned lds, unsigned off, const void *base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base));
+}
+__device__ __forceinline__ unsigned t8_lds_address(const void *p) { return (unsigned)(size_t)(__attribute__((address_space(3))) const char *)p; }
+// until at most N of this wavefront's loads are on their way (they end in order)
+template <int N>
+__device__ __forceinline__ void t8_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+template <int N>
+__device__ __forceinline__ void t8_wait_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void t8_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// A matrix instruction's 16 x 64 operand, rows of BK bytes in LDS: row r's 16-byte chunk c lies at place c ^ swz(r), so that eight rows of one
+// chunk lie in different banks
+template <int BK>
+__device__ __forceinline__ int t8_swz(int r) { return BK == 128 ? r & 7 : (r >> 1) & 3; }
+
+// y = x_scale w_scale sum + bias of four neighbouring columns
+__device__ __forceinline__ w4_f4 t8_finish(t8_i4 sum, w4_f4 ws, float xs, w4_f4 bias) {
+  w4_f4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf((float)sum[e] * ws[e], xs, bias[e]);
+  return v;
+}
+
+// Values of P planes of sums: plane p counts 256^p
+template <int P>
+__device__ __forceinline__ float t8_join(const int s[P], float scale) {
+  if constexpr (P == 2) return __builtin_fmaf((float)s[1], 256.0f, (float)s[0]) * scale;
+  double v = (double)s[P - 1];
+#pragma unroll
+  for (int p = P - 2; p >= 0; --p) v = __builtin_fma(v, 256.0, (double)s[p]);
+  return (float)(v * (double)scale);
+}
+
+}  // namespace qc

@@ -1,0 +1,422 @@
+// Rows with a scale each: the quantiser of plain rows, of gated rows and of normalised rows, the planes of gradients, and the reading of codes.
+//
+// All of them move bytes: a row is read once, held in registers as float32 while its largest value is found, and written.  One wavefront
+// takes a row of up to 256 vectors of 16 bytes, a workgroup of 2 - 16 wavefronts a longer one (or a short one where there are few rows:
+// then nothing but latency counts), and rows beyond 16 wavefronts' registers are read again for each of the steps.
+//
+// Exact decisions.  The codes are those of the definition: float32 quotients, rounded half to even.  Each is formed as v (1 / scale), which is off by
+// at most 1.2e-5 for quotients of up to 127, and where it is nearer than 2e-5 to a border the division decides.  The gated product is
+// formed in float32 to 13 e = 7.8e-7 of its value; where that is too near to a border, or to the row's largest value, float64 decides.
+#include "t8_common.h"
+
+namespace qc {
+
+constexpr float T8_MAGIC = 12582912.0f;      // 1.5 2^23: a sum with it is rounded to an integer, which its low byte holds
+constexpr float T8_NEAR = 2e-5f;
+constexpr float T8_TINY = 0x1p-60f;          // gated rows with nothing above it are decided in float64 throughout
+constexpr float T8_EMPTY = 0x1p-100f;        // gradients' rows with nothing above it are taken for zeros
+
+__device__ __forceinline__ unsigned t8_code(float v, float scale) {
+  const float n = fminf(fmaxf(__builtin_rintf(v / scale), -127.0f), 127.0f);
+  return (unsigned)(int)n;
+}
+
+// One row's reductions over the wavefronts of a workgroup.  The slots alternate from row to row and from use to use: a wavefront that
+// writes one again is at least one barrier behind the last that read it.
+struct T8Across {
+  double d[2][16];
+  unsigned u[2][2][16];
+};
+
+// FULL: a workgroup a row (else a wavefront).  C: vectors a lane.
+template <int TYPE, int SOURCE, bool FULL, int C>
+__global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a) {
+  using T = typename W4Mem<TYPE>::T;
+  constexpr int VL = t8_vl<TYPE>;
+  __shared__ T8Across across;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = FULL ? (int)blockDim.x >> 6 : 1, step = 64 * waves * VL, e0 = (FULL ? (int)threadIdx.x : lane) * VL;
+  const int width = SOURCE == T8_PLANES ? a.pitch : a.K;
+  float w[C][VL];
+  if ((SOURCE == T8_NORM && a.w) || SOURCE == T8_PLANES) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
+  }
+  int turn = 0;
+  for (int64_t row = FULL ? blockIdx.x : blockIdx.x * 4 + wave; row < a.M; row += FULL ? gridDim.x : gridDim.x * 4, turn ^= 1) {
+    const T *x = (const T *)a.x + row * a.ldx, *add = (const T *)a.add + row * a.lda;
+    float v[C][VL];
+#pragma unroll
+    for (int c = 0; c < C; ++c) t8_load<TYPE>(x, e0 + c * step, a.K, v[c]);
+    if constexpr (SOURCE == T8_NORM) {
+      if (a.add) {
+        T *h = (T *)a.h + row * a.ldh;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          float r[VL];
+          t8_load<TYPE>(add, e0 + c * step, a.K, r);
+#pragma unroll
+          for (int i = 0; i < VL; ++i) v[c][i] = W4Mem<TYPE>::get(W4Mem<TYPE>::put(v[c][i] + r[i]));
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) t8_store<TYPE>(h, e0 + c * step, a.K, v[c]);
+      }
+      double ss = 0.0;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < VL; ++i) ss = __builtin_fma((double)v[c][i], (double)v[c][i], ss);
+      ss = wave_sum_dpp(ss);
+      if constexpr (FULL) {
+        if (lane == 0) across.d[turn][wave] = ss;
+        __syncthreads();
+        ss = across.d[turn][0];
+        for (int i = 1; i < waves; ++i) ss += across.d[turn][i];
+      }
+      const float rho = (float)t8_rsqrt(ss / (double)a.K + (double)a.eps);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+          v[c][i] *= rho;
+          if (a.w) v[c][i] *= w[c][i];
+        }
+      if (a.y) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) t8_store<TYPE>((T *)a.y + row * a.ldy, e0 + c * step, a.K, v[c]);
+      }
+      if (!a.q) continue;
+    }
+    if constexpr (SOURCE == T8_GATED) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float g[VL];
+        t8_load<TYPE>(add, e0 + c * step, a.K, g);
+#pragma unroll
+        for (int i = 0; i < VL; ++i) v[c][i] = t8_gate(a.act, g[i], v[c][i]);
+      }
+    }
+    if constexpr (SOURCE == T8_PLANES) {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < VL; ++i) v[c][i] *= w[c][i];
+    }
+    unsigned top = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < VL; ++i) top = max(top, t8_mag(v[c][i]));
+    const auto over_row = [&](unsigned t, int use) {
+      t = t8_wave_max(t);
+      if constexpr (FULL) {
+        if (lane == 0) across.u[turn][use][wave] = t;
+        __syncthreads();
+        t = across.u[turn][use][0];
+        for (int i = 1; i < waves; ++i) t = max(t, across.u[turn][use][i]);
+      }
+      return t;
+    };
+    top = over_row(top, 0);
+    const bool lost = top >= 0x7F800000u;                 // an infinity or a NaN
+
+    if constexpr (SOURCE == T8_PLANES) {
+      constexpr int P = t8_planes(TYPE);
+      const float most = __builtin_bit_cast(float, top);
+      const bool empty = most < T8_EMPTY;
+      const double full = P == 2 ? 127.0 * 256.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
+      if (e0 == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / full);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        unsigned b[VL];
+        int t[VL];
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+          if constexpr (P == 2) t[i] = lost ? 0 : (int)__builtin_rintf(v[c][i] * (float)mult);
+          else t[i] = lost ? 0 : (int)__builtin_rint((double)v[c][i] * mult);
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+#pragma unroll
+          for (int i = 0; i < VL; ++i) {
+            b[i] = (unsigned)t[i];
+            t[i] = (t[i] >> 8) + ((t[i] >> 7) & 1);       // what is left when a signed byte is taken away
+          }
+          t8_store_bytes<VL>(a.q + t8_plane_row((int)row, p, P) * a.pitch, e0 + c * step, a.pitch, b);
+        }
+      }
+    } else {
+      uint32_t flags = 0;                                 // elements that float64 or the division decides: bit c VL + i
+      const auto element = [&](int bit) { return e0 + bit / VL * step + bit % VL; };
+      const auto exact = [&](int e) {
+        const float g = W4Mem<TYPE>::get(add[e]), f = W4Mem<TYPE>::get(x[e]);
+        return g == 0.0f || f == 0.0f ? 0.0f : (float)t8_gate_exact(a.act, g, f);      // rows of padding are zeros
+      };
+      const bool tiny = SOURCE == T8_GATED && __builtin_bit_cast(float, top) < T8_TINY;
+      if constexpr (SOURCE == T8_GATED) {
+        if (!lost) {
+          const float near = __builtin_bit_cast(float, top) * (1.0f - 3e-6f);
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < VL; ++i) flags |= (tiny ? e0 + c * step + i < width : fabsf(v[c][i]) >= near) ? 1u << (c * VL + i) : 0u;
+          top = 0;
+          while (flags) {
+            const int bit = __builtin_ctz(flags);
+            flags &= flags - 1;
+            top = max(top, t8_mag(exact(element(bit))));
+          }
+          top = over_row(top, 1);
+        }
+      }
+      float scale = __builtin_bit_cast(float, top) / 127.0f;
+      if (scale == 0.0f) scale = 1.0f;
+      if (e0 == 0) a.scale[row] = lost || top >= 0x7F800000u ? __builtin_nanf("") : scale;
+      const bool none = lost || top >= 0x7F800000u, all = tiny || scale < 0x1p-100f;
+      const float inv = none ? 0.0f : 1.0f / (all ? 1.0f : scale);
+      int8_t *q = a.q + row * a.ldq;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        unsigned b[VL];
+        float far = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+          const float m = __builtin_fmaf(v[c][i], inv, T8_MAGIC), n = m - T8_MAGIC, d = fabsf(__builtin_fmaf(v[c][i], inv, -n));
+          b[i] = none ? 0u : __builtin_bit_cast(unsigned, m);
+          if constexpr (SOURCE == T8_GATED) far = __builtin_fmaf(fabsf(n), 1.5e-6f, d);
+          else far = d;
+          flags |= far > 0.5f - T8_NEAR ? 1u << (c * VL + i) : 0u;
+        }
+        t8_store_bytes<VL>(q, e0 + c * step, width, b);
+      }
+      if (all) flags = ~0u >> (32 - C * VL);
+      if (none) flags = 0;
+      while (flags) {                                     // a byte behind its vector, from the same lane: in this order
+        const int bit = __builtin_ctz(flags), e = element(bit);
+        flags &= flags - 1;
+        if (e >= width) continue;
+        float t;
+        if constexpr (SOURCE == T8_GATED) {
+          t = exact(e);
+        } else if constexpr (SOURCE == T8_NORM) {
+          t = 0.0f;
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < VL; ++i)
+              if (bit == c * VL + i) t = v[c][i];
+        } else {
+          t = W4Mem<TYPE>::get(x[e]);
+        }
+        q[e] = (int8_t)t8_code(t, scale);
+      }
+    }
+  }
+}
+
+// Rows of any length, read again for each step; element after element.
+template <int TYPE, int SOURCE>
+__global__ __launch_bounds__(1024) void t8_long_rows_kernel(T8RowArgs a) {
+  using T = typename W4Mem<TYPE>::T;
+  __shared__ T8Across across;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x, turn ^= 1) {
+    const T *x = (const T *)a.x + row * a.ldx, *add = (const T *)a.add + row * a.lda;
+    float rho = 1.0f;
+    if constexpr (SOURCE == T8_NORM) {
+      double ss = 0.0;
+      T *h = (T *)a.h + row * a.ldh;
+      for (int e = threadIdx.x; e < a.K; e += 1024) {
+        float v = W4Mem<TYPE>::get(x[e]);
+        if (a.add) {
+          const T s = W4Mem<TYPE>::put(v + W4Mem<TYPE>::get(add[e]));
+          v = W4Mem<TYPE>::get(s);
+          h[e] = s;
+        }
+        ss = __builtin_fma((double)v, (double)v, ss);
+      }
+      ss = wave_sum_dpp(ss);
+      if (lane == 0) across.d[turn][wave] = ss;
+      __syncthreads();
+      ss = across.d[turn][0];
+      for (int i = 1; i < 16; ++i) ss += across.d[turn][i];
+      rho = (float)t8_rsqrt(ss / (double)a.K + (double)a.eps);
+      if (a.add) x = h;                                   // each thread reads what it wrote
+    }
+    const auto value = [&](int e) {
+      float v = W4Mem<TYPE>::get(x[e]);
+      if constexpr (SOURCE == T8_GATED) v = (float)t8_gate_exact(a.act, W4Mem<TYPE>::get(add[e]), v);
+      if constexpr (SOURCE == T8_PLANES) v *= a.w[e];
+      if constexpr (SOURCE == T8_NORM) {
+        v *= rho;
+        if (a.w) v *= a.w[e];
+      }
+      return v;
+    };
+    unsigned top = 0;
+    for (int e = threadIdx.x; e < a.K; e += 1024) {
+      const float v = value(e);
+      top = max(top, t8_mag(v));
+      if constexpr (SOURCE == T8_NORM)
+        if (a.y) ((T *)a.y)[row * a.ldy + e] = W4Mem<TYPE>::put(v);
+    }
+    if (SOURCE == T8_NORM && !a.q) continue;
+    top = t8_wave_max(top);
+    if (lane == 0) across.u[turn][0][wave] = top;
+    __syncthreads();
+    top = across.u[turn][0][0];
+    for (int i = 1; i < 16; ++i) top = max(top, across.u[turn][0][i]);
+    const bool lost = top >= 0x7F800000u;
+    if constexpr (SOURCE == T8_PLANES) {
+      constexpr int P = t8_planes(TYPE);
+      const float most = __builtin_bit_cast(float, top);
+      const bool empty = most < T8_EMPTY;
+      const double full = P == 2 ? 127.0 * 256.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
+      if (threadIdx.x == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / full);
+      for (int e = threadIdx.x; e < a.pitch; e += 1024) {
+        int t = 0;
+        if (!lost && e < a.K) t = P == 2 ? (int)__builtin_rintf(value(e) * (float)mult) : (int)__builtin_rint((double)value(e) * mult);
+        for (int p = 0; p < P; ++p) {
+          a.q[t8_plane_row((int)row, p, P) * a.pitch + e] = (int8_t)t;
+          t = (t >> 8) + ((t >> 7) & 1);
+        }
+      }
+    } else {
+      float scale = __builtin_bit_cast(float, top) / 127.0f;
+      if (scale == 0.0f) scale = 1.0f;
+      if (threadIdx.x == 0) a.scale[row] = lost ? __builtin_nanf("") : scale;
+      for (int e = threadIdx.x; e < a.K; e += 1024) a.q[row * a.ldq + e] = lost ? (int8_t)0 : (int8_t)t8_code(value(e), scale);
+    }
+  }
+}
+
+// wavefronts that keep the chip busy; more rows than these take are walked by the same ones
+constexpr int T8_WAVES = 256 * 16;
+
+template <int TYPE, int SOURCE>
+static hipError_t rows_launch(const T8RowArgs &a, hipStream_t st) {
+  constexpr int VL = t8_vl<TYPE>;
+  const int vectors = ((SOURCE == T8_PLANES ? a.pitch : a.K) + VL - 1) / VL;
+  if (vectors > 64 * 16 * 4) {
+    t8_long_rows_kernel<TYPE, SOURCE><<<(unsigned)std::min(a.M, 1024), 1024, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  int waves = 1;
+  while (vectors > 64 * 4 * waves || (waves < 16 && vectors > 64 * waves && (int64_t)a.M * waves < T8_WAVES / 4)) waves *= 2;
+  const int c = (vectors + 64 * waves - 1) / (64 * waves);
+  if (waves == 1) {
+    const unsigned grid = (unsigned)std::min((a.M + 3) / 4, T8_WAVES / 4);
+    if (c == 1) t8_rows_kernel<TYPE, SOURCE, false, 1><<<grid, 256, 0, st>>>(a);
+    else if (c == 2) t8_rows_kernel<TYPE, SOURCE, false, 2><<<grid, 256, 0, st>>>(a);
+    else t8_rows_kernel<TYPE, SOURCE, false, 4><<<grid, 256, 0, st>>>(a);
+  } else {
+    const unsigned grid = (unsigned)std::min(a.M, T8_WAVES / waves);
+    if (c == 1) t8_rows_kernel<TYPE, SOURCE, true, 1><<<grid, 64 * waves, 0, st>>>(a);
+    else if (c == 2) t8_rows_kernel<TYPE, SOURCE, true, 2><<<grid, 64 * waves, 0, st>>>(a);
+    else t8_rows_kernel<TYPE, SOURCE, true, 4><<<grid, 64 * waves, 0, st>>>(a);
+  }
+  return hipGetLastError();
+}
+
+template <int TYPE>
+static hipError_t rows_source(const T8RowArgs &a, int source, hipStream_t st) {
+  if (source == T8_PLAIN) return rows_launch<TYPE, T8_PLAIN>(a, st);
+  if (source == T8_GATED) return rows_launch<TYPE, T8_GATED>(a, st);
+  if (source == T8_NORM) return rows_launch<TYPE, T8_NORM>(a, st);
+  return rows_launch<TYPE, T8_PLANES>(a, st);
+}
+
+hipError_t launch_t8_rows(const T8RowArgs &a, int type, int source, hipStream_t st) {
+  if (type == QC_TYPE_F32) return rows_source<QC_TYPE_F32>(a, source, st);
+  if (type == QC_TYPE_F16) return rows_source<QC_TYPE_F16>(a, source, st);
+  return rows_source<QC_TYPE_BF16>(a, source, st);
+}
+
+// ---------------------------------------------------------------- codes to values; the gates' gradient
+// Elementwise: a workgroup takes `rows` whole rows (as many as make some thousand elements), or one a part of a row at a time.
+template <int TYPE>
+__global__ __launch_bounds__(256) void t8_expand_kernel(const int8_t *q, int64_t ldq, const float *scale, int M, int K, typename W4Mem<TYPE>::T *out, int64_t ldo,
+                                                        int rows, int vectors) {
+  const int64_t first = (int64_t)blockIdx.x * rows;
+  const int count = (int)min((int64_t)rows, M - first) * vectors;
+  for (int t = blockIdx.y * 256 + threadIdx.x; t < count; t += gridDim.y * 256) {
+    const int r = t / vectors, e = (t - r * vectors) * 8;
+    const int64_t row = first + r;
+    const float s = scale[row];
+    const int8_t *from = q + row * ldq;
+    typename W4Mem<TYPE>::T *to = out + row * ldo;
+    float v[8];
+    if (e + 8 <= K) {
+      const w4_u2 b = *(const t8_u2 *)(from + e);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(b[i / 4] >> (8 * (i % 4))) * s;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = e + i < K ? (float)from[e + i] * s : 0.0f;
+    }
+    constexpr int VL = t8_vl<TYPE>;
+#pragma unroll
+    for (int i = 0; i < 8; i += VL)
+      if (e + i < K) t8_store<TYPE>(to, e + i, K, v + i);
+  }
+}
+
+hipError_t launch_t8_expand(const int8_t *q, int64_t ldq, const float *scale, int M, int K, void *out, int type, int64_t ldo, hipStream_t st) {
+  const int vectors = (K + 7) / 8, rows = std::max(1, 1024 / vectors);
+  const dim3 grid((unsigned)((M + rows - 1) / rows), (unsigned)std::max(1, std::min(16, vectors / 1024)));
+  if (type == QC_TYPE_F32) t8_expand_kernel<QC_TYPE_F32><<<grid, 256, 0, st>>>(q, ldq, scale, M, K, (float *)out, ldo, rows, vectors);
+  else if (type == QC_TYPE_F16) t8_expand_kernel<QC_TYPE_F16><<<grid, 256, 0, st>>>(q, ldq, scale, M, K, (_Float16 *)out, ldo, rows, vectors);
+  else t8_expand_kernel<QC_TYPE_BF16><<<grid, 256, 0, st>>>(q, ldq, scale, M, K, (__bf16 *)out, ldo, rows, vectors);
+  return hipGetLastError();
+}
+
+// Every element is read before any of the same thread's results is written, so that results may take their inputs' place.
+template <int TYPE>
+__global__ __launch_bounds__(256) void t8_gated_grad_kernel(const void *x, int64_t ldx, const void *g, int64_t ldg, const void *dv, int64_t lddv, int act,
+                                                            int64_t M, int K, void *dx, int64_t lddx, void *dg, int64_t lddg, int rows, int vectors) {
+  using T = typename W4Mem<TYPE>::T;
+  constexpr int VL = t8_vl<TYPE>;
+  const int64_t first = (int64_t)blockIdx.x * rows;
+  const int count = (int)min((int64_t)rows, M - first) * vectors;
+  for (int t = blockIdx.y * 256 + threadIdx.x; t < count; t += gridDim.y * 256) {
+    const int r = t / vectors, e = (t - r * vectors) * VL;
+    const int64_t row = first + r;
+    float xv[VL], gv[VL], d[VL], rx[VL], rg[VL];
+    t8_load<TYPE>((const T *)x + row * ldx, e, K, xv);
+    t8_load<TYPE>((const T *)g + row * ldg, e, K, gv);
+    t8_load<TYPE>((const T *)dv + row * lddv, e, K, d);
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      float slope;
+      rx[i] = d[i] * t8_act(act, gv[i], slope);
+      rg[i] = d[i] * xv[i] * slope;
+    }
+    t8_store<TYPE>((T *)dx + row * lddx, e, K, rx);
+    t8_store<TYPE>((T *)dg + row * lddg, e, K, rg);
+  }
+}
+
+hipError_t launch_t8_gated_grad(const void *x, int64_t ldx, const void *g, int64_t ldg, int act, const void *dv, int64_t lddv, int type, int M, int K, void *dx,
+                                int64_t lddx, void *dg, int64_t lddg, hipStream_t st) {
+  const int vl = type == QC_TYPE_F32 ? 4 : 8, vectors = (K + vl - 1) / vl, rows = std::max(1, 512 / vectors);
+  const dim3 grid((unsigned)((M + rows - 1) / rows), (unsigned)std::max(1, std::min(32, vectors / 512)));
+  if (type == QC_TYPE_F32) t8_gated_grad_kernel<QC_TYPE_F32><<<grid, 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, act, M, K, dx, lddx, dg, lddg, rows, vectors);
+  else if (type == QC_TYPE_F16) t8_gated_grad_kernel<QC_TYPE_F16><<<grid, 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, act, M, K, dx, lddx, dg, lddg, rows, vectors);
+  else t8_gated_grad_kernel<QC_TYPE_BF16><<<grid, 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, act, M, K, dx, lddx, dg, lddg, rows, vectors);
+  return hipGetLastError();
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(256) void t8_zero_kernel(typename W4Mem<TYPE>::T *x, int K, int64_t ld) {
+  for (int k = threadIdx.x; k < K; k += 256) x[(int64_t)blockIdx.x * ld + k] = W4Mem<TYPE>::put(0.0f);
+}
+
+hipError_t launch_t8_zero(void *x, int type, int M, int K, int64_t ld, hipStream_t st) {
+  if (type == QC_TYPE_F32) t8_zero_kernel<QC_TYPE_F32><<<M, 256, 0, st>>>((float *)x, K, ld);
+  else if (type == QC_TYPE_F16) t8_zero_kernel<QC_TYPE_F16><<<M, 256, 0, st>>>((_Float16 *)x, K, ld);
+  else t8_zero_kernel<QC_TYPE_BF16><<<M, 256, 0, st>>>((__bf16 *)x, K, ld);
+  return hipGetLastError();
+}
+
+}  // namespace qc
