@@ -132,7 +132,7 @@ int qc_t8_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, co
   T8RowArgs a{};
   a.x = x; a.ldx = row_step(ldx, M, K);
   a.add = residual; a.lda = row_step(ldr, M, K);
-  a.w = weight; a.eps = eps;
+  a.w = weight; a.eps = eps; a.share = 1.0 / K;
   a.h = h; a.ldh = row_step(ldh, M, K);
   a.y = y; a.ldy = row_step(ldy, M, K);
   a.q = q; a.ldq = row_step(ldq, M, K);
@@ -167,7 +167,7 @@ int qc_t8_norm_grad(const void *h, int64_t ldh, const float *weight, float eps, 
   a.dy = dy; a.lddy = row_step(lddy, M, K);
   a.dh = dh; a.lddh = row_step(lddh, M, K);
   a.dx = dx; a.lddx = row_step(lddx, M, K);
-  a.w = weight; a.eps = eps;
+  a.w = weight; a.eps = eps; a.share = 1.0 / K;
   a.dw = dweight; a.part = static_cast<float *>(work);
   a.M = M; a.K = K;
   QC_HIP(launch_t8_norm_grad(a, type, static_cast<hipStream_t>(stream)));

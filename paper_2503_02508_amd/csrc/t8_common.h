@@ -21,6 +21,7 @@ struct T8RowArgs {
   float *scale;
   int M, K, act;
   float eps;
+  double share;             // 1 / K
   int planes, pitch;        // T8_PLANES
 };
 
@@ -33,6 +34,8 @@ struct T8NormGradArgs {
   float *dw, *part;         // part: [groups, K]
   int M, K, groups;
   float eps;
+  double share;             // 1 / K
+  int waves;                // of a row
 };
 
 // T8_PLANES: bytes that stand for a gradient, and the rows of the matrix of planes.  Row m's plane p (the lowest byte is 0) is row
@@ -78,20 +81,29 @@ typedef unsigned t8_u1 __attribute__((aligned(1)));
 template <int TYPE>
 constexpr int t8_vl = TYPE == QC_TYPE_F32 ? 4 : 8;        // elements of such a vector
 
-// elements e .. of a row of K as float32, zeros beyond it
+// elements e .. of a row of K, zeros beyond it, and their float32 values
 template <int TYPE>
-__device__ __forceinline__ void t8_load(const typename W4Mem<TYPE>::T *row, int e, int K, float v[t8_vl<TYPE>]) {
+__device__ __forceinline__ w4_u4 t8_raw(const typename W4Mem<TYPE>::T *row, int e, int K) {
   constexpr int VL = t8_vl<TYPE>;
   using T = typename W4Mem<TYPE>::T;
   typedef T vec __attribute__((ext_vector_type(VL)));
-  if (e + VL <= K) {
-    const vec r = __builtin_bit_cast(vec, (w4_u4) * (const t8_u4 *)(row + e));
+  if (e + VL <= K) return (w4_u4) * (const t8_u4 *)(row + e);
+  vec r;
 #pragma unroll
-    for (int i = 0; i < VL; ++i) v[i] = W4Mem<TYPE>::get(r[i]);
-  } else {
+  for (int i = 0; i < VL; ++i) r[i] = e + i < K ? row[e + i] : (T)0.0f;
+  return __builtin_bit_cast(w4_u4, r);
+}
+template <int TYPE>
+__device__ __forceinline__ void t8_values(w4_u4 raw, float v[t8_vl<TYPE>]) {
+  constexpr int VL = t8_vl<TYPE>;
+  typedef typename W4Mem<TYPE>::T vec __attribute__((ext_vector_type(VL)));
+  const vec r = __builtin_bit_cast(vec, raw);
 #pragma unroll
-    for (int i = 0; i < VL; ++i) v[i] = e + i < K ? W4Mem<TYPE>::get(row[e + i]) : 0.0f;
-  }
+  for (int i = 0; i < VL; ++i) v[i] = W4Mem<TYPE>::get(r[i]);
+}
+template <int TYPE>
+__device__ __forceinline__ void t8_load(const typename W4Mem<TYPE>::T *row, int e, int K, float v[t8_vl<TYPE>]) {
+  t8_values<TYPE>(t8_raw<TYPE>(row, e, K), v);
 }
 template <int TYPE>
 __device__ __forceinline__ void t8_store(typename W4Mem<TYPE>::T *row, int e, int K, const float v[t8_vl<TYPE>]) {
@@ -192,6 +204,24 @@ __device__ __forceinline__ float t8_gate(int act, float gate, float x) {
   bool deep;
   t8_logistic(act, gate, s, o, deep);
   return gate * s * (deep && gate < 0.0f ? x * 0x1p-100f : x);
+}
+// The same where the exponent's argument is at most 100 (else `most` says that it is not): 1 + exp(-t) then neither overflows nor
+// loses the smaller term.  SiLU's argument is a product of float32 numbers with what the product and log2(e) lose, to 2^-45 of it.
+template <int ACT>
+__device__ __forceinline__ float t8_gate_near(float gate, float x, float &most) {
+  float hi, lo;
+  if constexpr (ACT == QC_ACT_SILU) {
+    hi = gate * -1.44269502162933349609375f;
+    lo = __builtin_fmaf(gate, -1.44269502162933349609375f, -hi);
+    lo = __builtin_fmaf(gate, -1.9259629911266174681e-8f, lo);
+  } else {
+    const double g = gate, u = g * (-2.302208198144325 - 0.1029432395800235 * (g * g));
+    hi = (float)u;
+    lo = (float)(u - (double)hi);
+  }
+  most = fmaxf(most, fabsf(hi));
+  const float e = __builtin_amdgcn_exp2f(hi);
+  return gate * __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, lo * 0.6931471805599453f, e)) * x;
 }
 // value and derivative of the activation
 __device__ __forceinline__ float t8_act(int act, float gate, float &d) {

@@ -7,88 +7,116 @@
 
 namespace qc {
 
-// FULL: a workgroup a row (else a wavefront); C: vectors a lane
-template <int TYPE, bool FULL, int C>
-__global__ __launch_bounds__(FULL ? 1024 : 256) void t8_norm_grad_kernel(T8NormGradArgs a) {
+// `waves` wavefronts a row, as many rows a workgroup as make 16 of them; they walk in step.  C: vectors a lane.
+template <int TYPE, int C>
+__global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
   using T = typename W4Mem<TYPE>::T;
   constexpr int VL = t8_vl<TYPE>;
   __shared__ double red[2][2][16];                          // alternating, as in t8_rows.hip
-  __shared__ float join[FULL ? 1 : 4 * 64 * C * VL];
+  extern __shared__ float join[];                           // [rows of a workgroup, width]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int waves = FULL ? (int)blockDim.x >> 6 : 1, step = 64 * waves * VL, e0 = (FULL ? (int)threadIdx.x : lane) * VL;
+  const int waves = a.waves, rows = ((int)blockDim.x >> 6) / waves, sub = wave / waves, first = sub * waves;
+  const int step = 64 * waves * VL, e0 = ((wave - first) * 64 + lane) * VL;
   float dw[C][VL] = {};
-  int turn = 0;
-  for (int64_t row = FULL ? blockIdx.x : blockIdx.x * 4 + wave; row < a.M; row += FULL ? gridDim.x : gridDim.x * 4, turn ^= 1) {
-    float h[C][VL], g[C][VL];
+  constexpr bool AHEAD = C < 4;                             // the next row is on its way while this one is at work (registers)
+  w4_u4 nh[C], ng[C];
+  const auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      t8_load<TYPE>((const T *)a.h + row * a.ldh, e0 + c * step, a.K, h[c]);
-      t8_load<TYPE>((const T *)a.dy + row * a.lddy, e0 + c * step, a.K, g[c]);
+      nh[c] = t8_raw<TYPE>((const T *)a.h + row * a.ldh, e0 + c * step, a.K);
+      ng[c] = t8_raw<TYPE>((const T *)a.dy + row * a.lddy, e0 + c * step, a.K);
     }
+  };
+  int64_t row = (int64_t)blockIdx.x * rows + sub;
+  const int64_t ahead = (int64_t)gridDim.x * rows;
+  if (AHEAD && row < a.M) fetch(row);
+  int turn = 0;
+  for (int64_t base = (int64_t)blockIdx.x * rows; base < a.M; base += ahead, row += ahead, turn ^= 1) {
+    const bool there = row < a.M;
+    w4_u4 ch[C], cg[C], cd[C];
+    if (!AHEAD && there) fetch(row);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      ch[c] = nh[c];
+      cg[c] = ng[c];
+    }
+    if (a.dh && there) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) cd[c] = t8_raw<TYPE>((const T *)a.dh + row * a.lddh, e0 + c * step, a.K);
+    }
+    if (AHEAD && row + ahead < a.M) fetch(row + ahead);
     double ss = 0.0;
     float gh = 0.0f;
+    if (there) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      float w[VL];
-      if (a.w) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w);
+      for (int c = 0; c < C; ++c) {
+        float h[VL], g[VL], w[VL];
+        t8_values<TYPE>(ch[c], h);
+        t8_values<TYPE>(cg[c], g);
+        if (a.w) {
+          t8_load_f32<VL>(a.w, e0 + c * step, a.K, w);
 #pragma unroll
-      for (int i = 0; i < VL; ++i) {
-        ss = __builtin_fma((double)h[c][i], (double)h[c][i], ss);
-        gh = __builtin_fmaf(a.w ? g[c][i] * w[i] : g[c][i], h[c][i], gh);
+          for (int i = 0; i < VL; ++i) g[i] *= w[i];
+        }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+          ss = __builtin_fma((double)h[i], (double)h[i], ss);
+          gh = __builtin_fmaf(g[i], h[i], gh);
+        }
       }
     }
     ss = wave_sum_dpp(ss);
     double dot = wave_sum_dpp((double)gh);
-    if constexpr (FULL) {
+    if (waves > 1) {
       if (lane == 0) {
         red[turn][0][wave] = ss;
         red[turn][1][wave] = dot;
       }
-      __syncthreads();
-      ss = red[turn][0][0];
-      dot = red[turn][1][0];
+      // (not __syncthreads(), which would wait for the next row too)
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      ss = red[turn][0][first];
+      dot = red[turn][1][first];
       for (int i = 1; i < waves; ++i) {
-        ss += red[turn][0][i];
-        dot += red[turn][1][i];
+        ss += red[turn][0][first + i];
+        dot += red[turn][1][first + i];
       }
     }
-    const double r = t8_rsqrt(ss / (double)a.K + (double)a.eps);
-    const float rho = (float)r, along = (float)(r * r * r * (dot / (double)a.K));
+    if (!there) continue;
+    const double r = t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
+    const float rho = (float)r, along = (float)(r * r * r * (dot * a.share));
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float w[VL], add[VL], d[VL];
+      float h[VL], g[VL], w[VL], d[VL];
+      t8_values<TYPE>(ch[c], h);
+      t8_values<TYPE>(cg[c], g);
       if (a.w) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w);
-      if (a.dh) t8_load<TYPE>((const T *)a.dh + row * a.lddh, e0 + c * step, a.K, add);
 #pragma unroll
       for (int i = 0; i < VL; ++i) {
-        d[i] = __builtin_fmaf(-h[c][i], along, rho * (a.w ? g[c][i] * w[i] : g[c][i]));
-        if (a.dh) d[i] += add[i];
-        dw[c][i] = __builtin_fmaf(g[c][i], h[c][i] * rho, dw[c][i]);
+        dw[c][i] = __builtin_fmaf(g[i], h[i] * rho, dw[c][i]);
+        if (a.w) g[i] *= w[i];
+        d[i] = __builtin_fmaf(-h[i], along, rho * g[i]);
+      }
+      if (a.dh) {
+        float add[VL];
+        t8_values<TYPE>(cd[c], add);
+#pragma unroll
+        for (int i = 0; i < VL; ++i) d[i] += add[i];
       }
       t8_store<TYPE>((T *)a.dx + row * a.lddx, e0 + c * step, a.K, d);
     }
   }
   if (!a.dw) return;
   float *part = a.part + (size_t)blockIdx.x * a.K;
-  if constexpr (FULL) {
+  const int width = step * C;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
+  for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int i = 0; i < VL; ++i)
-        if (e0 + c * step + i < a.K) part[e0 + c * step + i] = dw[c][i];
-    }
-  } else {
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int i = 0; i < VL; ++i) join[wave * 64 * C * VL + e0 + c * step + i] = dw[c][i];
-    __syncthreads();
-    for (int e = threadIdx.x; e < a.K; e += 256) {
-      float t = join[e];
-#pragma unroll
-      for (int i = 1; i < 4; ++i) t += join[i * 64 * C * VL + e];
-      part[e] = t;
-    }
+    for (int i = 0; i < VL; ++i) join[sub * width + e0 + c * step + i] = dw[c][i];
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.K; e += blockDim.x) {
+    float t = join[e];
+    for (int i = 1; i < rows; ++i) t += join[i * width + e];
+    part[e] = t;
   }
 }
 
@@ -124,8 +152,8 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_long_kernel(T8NormGradArgs 
       ss += red[turn][0][i];
       dot += red[turn][1][i];
     }
-    const double r = t8_rsqrt(ss / (double)a.K + (double)a.eps);
-    const float rho = (float)r, along = (float)(r * r * r * (dot / (double)a.K));
+    const double r = t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
+    const float rho = (float)r, along = (float)(r * r * r * (dot * a.share));
     for (int e = threadIdx.x; e < a.K; e += 1024) {
       const float v = Mem::get(h[e]), g = Mem::get(dy[e]);
       float d = __builtin_fmaf(-v, along, rho * (a.w ? g * a.w[e] : g));
@@ -136,53 +164,64 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_long_kernel(T8NormGradArgs 
   }
 }
 
-// dweight: 64 columns a workgroup, its 16 wavefronts every sixteenth group, float64 sums in the groups' order
+// dweight: 16 columns a workgroup, 64 groups at a time, float64 sums in the groups' order
 __global__ __launch_bounds__(1024) void t8_weight_grad_kernel(const float *part, int groups, int K, float *dw) {
-  __shared__ double red[16][64];
-  const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+  __shared__ double red[64][17];
+  const int col = blockIdx.x * 16 + (threadIdx.x & 15), first = threadIdx.x >> 4;
   double t = 0.0;
   if (col < K)
-    for (int g = wave; g < groups; g += 16) t += (double)part[(size_t)g * K + col];
-  red[wave][threadIdx.x & 63] = t;
+    for (int g = first; g < groups; g += 64) t += (double)part[(size_t)g * K + col];
+  red[first][threadIdx.x & 15] = t;
   __syncthreads();
-  if (wave == 0 && col < K) {
-    for (int i = 1; i < 16; ++i) t += red[i][threadIdx.x];
+  if (first == 0 && col < K) {
+    for (int i = 1; i < 64; ++i) t += red[i][threadIdx.x];
     dw[col] = (float)t;
   }
 }
 
 struct NormGradShape {
-  int waves, c, groups;      // waves 0: the kernel of long rows
+  int waves, rows, c, groups;      // waves 0: the kernel of long rows
 };
-// One rule for every type, so that the workspace does not depend on it: vectors of 4 elements would be 8 of the 16-bit types'.
-static NormGradShape norm_grad_shape(int M, int K, int vl) {
-  const int vectors = (K + vl - 1) / vl;
+constexpr int NORM_GRAD_GROUPS = 256;
+static NormGradShape norm_grad_shape(int M, int K, int type) {
+  const int vl = type == QC_TYPE_F32 ? 4 : 8, most = type == QC_TYPE_F32 ? 4 : 2, vectors = (K + vl - 1) / vl;
   NormGradShape s{};
-  s.groups = std::min(M, 512);
-  if (vectors > 64 * 16 * 2) return s;
-  s.waves = 1;
-  while (vectors > 64 * 2 * s.waves || (s.waves < 16 && vectors > 64 * s.waves && (int64_t)M * s.waves < 1024)) s.waves *= 2;
+  s.groups = std::min(M, NORM_GRAD_GROUPS);
+  if (vectors > 64 * 16 * most) return s;
+  s.waves = (vectors + 64 * most - 1) / (64 * most);
+  while (s.waves < 16 && vectors > 64 * s.waves && (int64_t)M * s.waves < 1024) ++s.waves;
   s.c = (vectors + 64 * s.waves - 1) / (64 * s.waves);
-  if (s.waves == 1) s.groups = std::min((M + 3) / 4, 512);
+  s.rows = 16 / s.waves;
+  // workgroups for every compute unit come before rows that share one
+  while (s.rows > 1 && (M + s.rows - 1) / s.rows < NORM_GRAD_GROUPS) --s.rows;
+  s.groups = std::min((M + s.rows - 1) / s.rows, NORM_GRAD_GROUPS);
   return s;
 }
 
-int t8_norm_grad_groups(int M, int K) { return std::max(norm_grad_shape(M, K, 4).groups, norm_grad_shape(M, K, 8).groups); }
+int t8_norm_grad_groups(int M, int K) { return std::min(M, NORM_GRAD_GROUPS); }
 
 template <int TYPE>
 static hipError_t norm_grad_launch(T8NormGradArgs a, hipStream_t st) {
-  const NormGradShape s = norm_grad_shape(a.M, a.K, t8_vl<TYPE>);
+  const NormGradShape s = norm_grad_shape(a.M, a.K, TYPE);
   a.groups = s.groups;
+  a.waves = s.waves;
   if (a.M > 0) {
+    const int threads = 64 * s.waves * s.rows, lds = threads * s.c * t8_vl<TYPE> * 4;      // 64 KB at most
     if (s.waves == 0) t8_norm_grad_long_kernel<TYPE><<<s.groups, 1024, 0, st>>>(a);
-    else if (s.waves == 1 && s.c == 1) t8_norm_grad_kernel<TYPE, false, 1><<<s.groups, 256, 0, st>>>(a);
-    else if (s.waves == 1) t8_norm_grad_kernel<TYPE, false, 2><<<s.groups, 256, 0, st>>>(a);
-    else if (s.c == 1) t8_norm_grad_kernel<TYPE, true, 1><<<s.groups, 64 * s.waves, 0, st>>>(a);
-    else t8_norm_grad_kernel<TYPE, true, 2><<<s.groups, 64 * s.waves, 0, st>>>(a);
+    else {
+      constexpr int MOST = TYPE == QC_TYPE_F32 ? 4 : 2;
+      const auto kern = s.c == 1 ? t8_norm_grad_kernel<TYPE, 1> : s.c == 2 ? t8_norm_grad_kernel<TYPE, 2> : t8_norm_grad_kernel<TYPE, MOST>;
+      static std::atomic<unsigned long long> done[3];
+      if (lds > 65536 - 1024) {
+        const hipError_t e = allow_lds((const void *)kern, 65536, done[std::min(s.c, 3) - 1]);
+        if (e != hipSuccess) return e;
+      }
+      kern<<<s.groups, threads, lds, st>>>(a);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.dw) t8_weight_grad_kernel<<<(a.K + 63) / 64, 1024, 0, st>>>(a.part, s.groups, a.K, a.dw);
+  if (a.dw) t8_weight_grad_kernel<<<(a.K + 15) / 16, 1024, 0, st>>>(a.part, s.groups, a.K, a.dw);
   return hipGetLastError();
 }
 

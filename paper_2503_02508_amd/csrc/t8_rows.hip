@@ -37,29 +37,32 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = FULL ? (int)blockDim.x >> 6 : 1, step = 64 * waves * VL, e0 = (FULL ? (int)threadIdx.x : lane) * VL;
   const int width = SOURCE == T8_PLANES ? a.pitch : a.K;
-  float w[C][VL];
-  if ((SOURCE == T8_NORM && a.w) || SOURCE == T8_PLANES) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
-  }
   int turn = 0;
   for (int64_t row = FULL ? blockIdx.x : blockIdx.x * 4 + wave; row < a.M; row += FULL ? gridDim.x : gridDim.x * 4, turn ^= 1) {
     const T *x = (const T *)a.x + row * a.ldx, *add = (const T *)a.add + row * a.lda;
-    float v[C][VL];
+    float v[C][VL], w[C][VL];
+    w4_u4 second[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) t8_load<TYPE>(x, e0 + c * step, a.K, v[c]);
+    if (SOURCE == T8_GATED || (SOURCE == T8_NORM && a.add)) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) second[c] = t8_raw<TYPE>(add, e0 + c * step, a.K);
+    }
+    if (SOURCE == T8_PLANES || (SOURCE == T8_NORM && a.w)) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
+    }
     if constexpr (SOURCE == T8_NORM) {
       if (a.add) {
         T *h = (T *)a.h + row * a.ldh;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           float r[VL];
-          t8_load<TYPE>(add, e0 + c * step, a.K, r);
+          t8_values<TYPE>(second[c], r);
 #pragma unroll
           for (int i = 0; i < VL; ++i) v[c][i] = W4Mem<TYPE>::get(W4Mem<TYPE>::put(v[c][i] + r[i]));
+          t8_store<TYPE>(h, e0 + c * step, a.K, v[c]);
         }
-#pragma unroll
-        for (int c = 0; c < C; ++c) t8_store<TYPE>(h, e0 + c * step, a.K, v[c]);
       }
       double ss = 0.0;
 #pragma unroll
@@ -73,14 +76,16 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
         ss = across.d[turn][0];
         for (int i = 1; i < waves; ++i) ss += across.d[turn][i];
       }
-      const float rho = (float)t8_rsqrt(ss / (double)a.K + (double)a.eps);
+      const float rho = (float)t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
 #pragma unroll
-      for (int c = 0; c < C; ++c)
+      for (int c = 0; c < C; ++c) {
 #pragma unroll
-        for (int i = 0; i < VL; ++i) {
-          v[c][i] *= rho;
-          if (a.w) v[c][i] *= w[c][i];
+        for (int i = 0; i < VL; ++i) v[c][i] *= rho;
+        if (a.w) {
+#pragma unroll
+          for (int i = 0; i < VL; ++i) v[c][i] *= w[c][i];
         }
+      }
       if (a.y) {
 #pragma unroll
         for (int c = 0; c < C; ++c) t8_store<TYPE>((T *)a.y + row * a.ldy, e0 + c * step, a.K, v[c]);
@@ -90,10 +95,22 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
     if constexpr (SOURCE == T8_GATED) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        float g[VL];
-        t8_load<TYPE>(add, e0 + c * step, a.K, g);
+        float g[VL], most = 0.0f, r[VL];
+        t8_values<TYPE>(second[c], g);
+        if (a.act == QC_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < VL; ++i) v[c][i] = t8_gate(a.act, g[i], v[c][i]);
+          for (int i = 0; i < VL; ++i) r[i] = t8_gate_near<QC_ACT_SILU>(g[i], v[c][i], most);
+        } else {
+#pragma unroll
+          for (int i = 0; i < VL; ++i) r[i] = t8_gate_near<QC_ACT_GELU>(g[i], v[c][i], most);
+        }
+        if (most > 100.0f) {
+#pragma unroll
+          for (int i = 0; i < VL; ++i) v[c][i] = t8_gate(a.act, g[i], v[c][i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < VL; ++i) v[c][i] = r[i];
+        }
       }
     }
     if constexpr (SOURCE == T8_PLANES) {
@@ -102,11 +119,14 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
 #pragma unroll
         for (int i = 0; i < VL; ++i) v[c][i] *= w[c][i];
     }
-    unsigned top = 0;
+    unsigned top = 0, tops[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+      tops[c] = 0;
 #pragma unroll
-      for (int i = 0; i < VL; ++i) top = max(top, t8_mag(v[c][i]));
+      for (int i = 0; i < VL; ++i) tops[c] = max(tops[c], t8_mag(v[c][i]));
+      top = max(top, tops[c]);
+    }
     const auto over_row = [&](unsigned t, int use) {
       t = t8_wave_max(t);
       if constexpr (FULL) {
@@ -146,7 +166,8 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
         }
       }
     } else {
-      uint32_t flags = 0;                                 // elements that float64 or the division decides: bit c VL + i
+      // elements that float64 or the division decides, as a word of bits (c VL + i), read again; few
+      uint32_t flags = 0;
       const auto element = [&](int bit) { return e0 + bit / VL * step + bit % VL; };
       const auto exact = [&](int e) {
         const float g = W4Mem<TYPE>::get(add[e]), f = W4Mem<TYPE>::get(x[e]);
@@ -158,8 +179,10 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
           const float near = __builtin_bit_cast(float, top) * (1.0f - 3e-6f);
 #pragma unroll
           for (int c = 0; c < C; ++c)
+            if (__builtin_bit_cast(float, tops[c]) >= near) {
 #pragma unroll
-            for (int i = 0; i < VL; ++i) flags |= (tiny ? e0 + c * step + i < width : fabsf(v[c][i]) >= near) ? 1u << (c * VL + i) : 0u;
+              for (int i = 0; i < VL; ++i) flags |= (tiny ? e0 + c * step + i < width : fabsf(v[c][i]) >= near) ? 1u << (c * VL + i) : 0u;
+            }
           top = 0;
           while (flags) {
             const int bit = __builtin_ctz(flags);
@@ -171,9 +194,9 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
       }
       float scale = __builtin_bit_cast(float, top) / 127.0f;
       if (scale == 0.0f) scale = 1.0f;
-      if (e0 == 0) a.scale[row] = lost || top >= 0x7F800000u ? __builtin_nanf("") : scale;
       const bool none = lost || top >= 0x7F800000u, all = tiny || scale < 0x1p-100f;
-      const float inv = none ? 0.0f : 1.0f / (all ? 1.0f : scale);
+      if (e0 == 0) a.scale[row] = none ? __builtin_nanf("") : scale;
+      const float inv = 1.0f / (all ? 1.0f : scale);
       int8_t *q = a.q + row * a.ldq;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -181,13 +204,23 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
         float far = 0.0f;
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
-          const float m = __builtin_fmaf(v[c][i], inv, T8_MAGIC), n = m - T8_MAGIC, d = fabsf(__builtin_fmaf(v[c][i], inv, -n));
-          b[i] = none ? 0u : __builtin_bit_cast(unsigned, m);
-          if constexpr (SOURCE == T8_GATED) far = __builtin_fmaf(fabsf(n), 1.5e-6f, d);
-          else far = d;
-          flags |= far > 0.5f - T8_NEAR ? 1u << (c * VL + i) : 0u;
+          const float m = __builtin_fmaf(v[c][i], inv, T8_MAGIC), n = m - T8_MAGIC, d = __builtin_fmaf(v[c][i], inv, -n);
+          b[i] = __builtin_bit_cast(unsigned, m);
+          if constexpr (SOURCE == T8_GATED) far = fmaxf(far, __builtin_fmaf(fabsf(n), 1.5e-6f, fabsf(d)));
+          else far = fmaxf(far, fabsf(d));
+        }
+        if (none) {
+#pragma unroll
+          for (int i = 0; i < VL; ++i) b[i] = 0;
         }
         t8_store_bytes<VL>(q, e0 + c * step, width, b);
+        if (far > 0.5f - T8_NEAR) {
+#pragma unroll
+          for (int i = 0; i < VL; ++i) {
+            const float n = __builtin_fmaf(v[c][i], inv, T8_MAGIC) - T8_MAGIC, d = fabsf(__builtin_fmaf(v[c][i], inv, -n));
+            flags |= (SOURCE == T8_GATED ? __builtin_fmaf(fabsf(n), 1.5e-6f, d) : d) > 0.5f - T8_NEAR ? 1u << (c * VL + i) : 0u;
+          }
+        }
       }
       if (all) flags = ~0u >> (32 - C * VL);
       if (none) flags = 0;
@@ -241,7 +274,7 @@ __global__ __launch_bounds__(1024) void t8_long_rows_kernel(T8RowArgs a) {
       __syncthreads();
       ss = across.d[turn][0];
       for (int i = 1; i < 16; ++i) ss += across.d[turn][i];
-      rho = (float)t8_rsqrt(ss / (double)a.K + (double)a.eps);
+      rho = (float)t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
       if (a.add) x = h;                                   // each thread reads what it wrote
     }
     const auto value = [&](int e) {
@@ -291,9 +324,8 @@ __global__ __launch_bounds__(1024) void t8_long_rows_kernel(T8RowArgs a) {
   }
 }
 
-// wavefronts that keep the chip busy; more rows than these take are walked by the same ones
-constexpr int T8_WAVES = 256 * 16;
-
+// Up to 4 vectors a lane: what a wavefront does once a row (its reductions, root and division) costs as much as one or two of them.
+// Where the rows are fewer than the chip has wavefronts, one a lane.
 template <int TYPE, int SOURCE>
 static hipError_t rows_launch(const T8RowArgs &a, hipStream_t st) {
   constexpr int VL = t8_vl<TYPE>;
@@ -302,18 +334,20 @@ static hipError_t rows_launch(const T8RowArgs &a, hipStream_t st) {
     t8_long_rows_kernel<TYPE, SOURCE><<<(unsigned)std::min(a.M, 1024), 1024, 0, st>>>(a);
     return hipGetLastError();
   }
-  int waves = 1;
-  while (vectors > 64 * 4 * waves || (waves < 16 && vectors > 64 * waves && (int64_t)a.M * waves < T8_WAVES / 4)) waves *= 2;
+  int waves = (vectors + 255) / 256;
+  while (waves < 16 && vectors > 64 * waves && (int64_t)a.M * waves < 2048) ++waves;
   const int c = (vectors + 64 * waves - 1) / (64 * waves);
   if (waves == 1) {
-    const unsigned grid = (unsigned)std::min((a.M + 3) / 4, T8_WAVES / 4);
+    const unsigned grid = (unsigned)std::min((a.M + 3) / 4, 1 << 20);
     if (c == 1) t8_rows_kernel<TYPE, SOURCE, false, 1><<<grid, 256, 0, st>>>(a);
     else if (c == 2) t8_rows_kernel<TYPE, SOURCE, false, 2><<<grid, 256, 0, st>>>(a);
+    else if (c == 3) t8_rows_kernel<TYPE, SOURCE, false, 3><<<grid, 256, 0, st>>>(a);
     else t8_rows_kernel<TYPE, SOURCE, false, 4><<<grid, 256, 0, st>>>(a);
   } else {
-    const unsigned grid = (unsigned)std::min(a.M, T8_WAVES / waves);
+    const unsigned grid = (unsigned)std::min(a.M, 1 << 20);
     if (c == 1) t8_rows_kernel<TYPE, SOURCE, true, 1><<<grid, 64 * waves, 0, st>>>(a);
     else if (c == 2) t8_rows_kernel<TYPE, SOURCE, true, 2><<<grid, 64 * waves, 0, st>>>(a);
+    else if (c == 3) t8_rows_kernel<TYPE, SOURCE, true, 3><<<grid, 64 * waves, 0, st>>>(a);
     else t8_rows_kernel<TYPE, SOURCE, true, 4><<<grid, 64 * waves, 0, st>>>(a);
   }
   return hipGetLastError();
