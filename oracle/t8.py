@@ -66,7 +66,8 @@ def gated_grad(x, gate, name, dv):
 
 
 def linear(qx, xs, qw, ws, bias=None):
-    y = (np.asarray(qx, np.int64) @ np.asarray(qw, np.int64).T) * (np.asarray(xs, np.float64)[:, None] * np.asarray(ws, np.float64))
+    """The sums are whole numbers below 2^53: exact."""
+    y = (np.asarray(qx, np.float64) @ np.asarray(qw, np.float64).T) * (np.asarray(xs, np.float64)[:, None] * np.asarray(ws, np.float64))
     return y if bias is None else y + np.asarray(bias, np.float64)
 
 

@@ -54,6 +54,7 @@ struct T8Product {
   void *y;
   int64_t ldy;
   int tm, tn;               // grid of tiles
+  int stream;               // whether the result's stores pass the caches
   int split, per;           // parts of the summed axis, slabs of each; their sums
   int32_t *part;
 };

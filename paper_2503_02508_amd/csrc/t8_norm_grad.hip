@@ -184,11 +184,11 @@ struct NormGradShape {
 };
 constexpr int NORM_GRAD_GROUPS = 256;
 static NormGradShape norm_grad_shape(int M, int K, int type) {
-  const int vl = type == QC_TYPE_F32 ? 4 : 8, most = type == QC_TYPE_F32 ? 4 : 2, vectors = (K + vl - 1) / vl;
+  const int vl = type == QC_TYPE_F32 ? 4 : 8, most = type == QC_TYPE_F32 ? 4 : 2, vectors = (K + vl - 1) / vl;      // most: vectors a lane
   NormGradShape s{};
   s.groups = std::min(M, NORM_GRAD_GROUPS);
   if (vectors > 64 * 16 * most) return s;
-  s.waves = (vectors + 64 * most - 1) / (64 * most);
+  s.waves = std::min((vectors + 127) / 128, 16);
   while (s.waves < 16 && vectors > 64 * s.waves && (int64_t)M * s.waves < 1024) ++s.waves;
   s.c = (vectors + 64 * s.waves - 1) / (64 * s.waves);
   s.rows = 16 / s.waves;
@@ -206,7 +206,7 @@ static hipError_t norm_grad_launch(T8NormGradArgs a, hipStream_t st) {
   a.groups = s.groups;
   a.waves = s.waves;
   if (a.M > 0) {
-    const int threads = 64 * s.waves * s.rows, lds = threads * s.c * t8_vl<TYPE> * 4;      // 64 KB at most
+    const int threads = 64 * s.waves * s.rows, lds = threads * (s.c == 3 ? 4 : s.c) * t8_vl<TYPE> * 4;      // (the kernel's C; 64 KB at most)
     if (s.waves == 0) t8_norm_grad_long_kernel<TYPE><<<s.groups, 1024, 0, st>>>(a);
     else {
       constexpr int MOST = TYPE == QC_TYPE_F32 ? 4 : 2;

@@ -12,6 +12,9 @@ typedef int t8_i2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void t8_to_lds(unsigned lds, unsigned off, const void *base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base));
 }
+__device__ __forceinline__ void t8_word_to_lds(unsigned lds, unsigned off, const void *base) {      // 256 bytes, 4 a lane
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base));
+}
 __device__ __forceinline__ unsigned t8_lds_address(const void *p) { return (unsigned)(size_t)(__attribute__((address_space(3))) const char *)p; }
 // until at most N of this wavefront's loads are on their way (they end in order)
 template <int N>
@@ -24,14 +27,6 @@ __device__ __forceinline__ void t8_barrier() { asm volatile("s_waitcnt lgkmcnt(0
 // chunk lie in different banks
 template <int BK>
 __device__ __forceinline__ int t8_swz(int r) { return BK == 128 ? r & 7 : (r >> 1) & 3; }
-
-// y = x_scale w_scale sum + bias of four neighbouring columns
-__device__ __forceinline__ w4_f4 t8_finish(t8_i4 sum, w4_f4 ws, float xs, w4_f4 bias) {
-  w4_f4 v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf((float)sum[e] * ws[e], xs, bias[e]);
-  return v;
-}
 
 // Values of P planes of sums: plane p counts 256^p
 template <int P>

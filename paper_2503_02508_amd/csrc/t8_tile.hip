@@ -1,221 +1,414 @@
 // Products of the 8-bit layers with a scale for each token, many rows: y = x W^T and, on the byte planes of gradients, dx = dy W.
 //
-// A workgroup makes a tile of the result; slabs of BK bytes of the summed axis go from memory straight to LDS, ST of them in a ring, one
-// barrier a slab.  Wavefronts read 16 x 64 operands of v_mfma_i32_16x16x64_i8 from there.  The weights' rows run along the summed axis in the
-// forward product; in the gradient they run across it, and ds_read_b64_tr_b8 turns 8 rows x 16 bytes on their way to the registers.  Operands
-// are exchanged (weights first), so that a lane holds four neighbouring columns of one row; the epilogue turns 16 rows at a time through the
-// wavefront's own part of LDS and writes whole cache lines.
+// Slabs of 128 bytes of the summed axis (whole cache lines: slabs of 64 made 4096 x 8192 x 8192 a quarter slower) go from memory straight to one of
+// two places in LDS.  Wavefronts read 16 x 64 operands of v_mfma_i32_16x16x64_i8 from there half a slab ahead into registers: behind a
+// slab's barrier its products start at once, the next operands come in under them, and the place of the slab that was read is filled again.
+// The weights' rows run along the summed axis in the forward product; in the gradient they run across it, and ds_read_b64_tr_b8 turns 8 rows x
+// 16 bytes on their way to the registers.
+// Workgroups stay and walk over the tiles: the slabs of the next tile are on their way while the last of this one are multiplied.
+// In the forward product a lane's columns are neighbours (block j's lane l reads weight row 4 l + j), so that 16 lanes write whole lines of a
+// row without any exchange: trading words between lanes took 16384 x 4608 x 1152 from 88 to 100 us.  The transposed reads of the gradient cannot
+// permute columns; its operands are exchanged (weights first) and lanes trade words instead.
+// What bounds it: the large tile's LDS traffic (96 KB read, 32 written for 1024 clocks of products) is as long as its products, and what ends a tile
+// is not overlapped: 4.4 us of 20 at K = 1152.  4096 x 8192 x 8192 runs at 2.5 POP/s (a loop of nothing but products: 4.1).
 #include "t8_product.h"
 
 namespace qc {
 
-template <int BK, int ST, int WM, int WN, int MI, int NI>
+constexpr int T8_BK = 128, T8_ST = 2;
+
+template <int WM, int WN, int MI, int NI>
 struct T8Tile {
   static constexpr int W = WM * WN, TM = WM * MI * 16, TN = WN * NI * 16;
-  static constexpr int ABYTES = TM * BK, BBYTES = TN * BK, STAGE = ABYTES + BBYTES;
-  static constexpr int LA = ABYTES / 1024 / W, LB = BBYTES / 1024 / W;   // loads of a wavefront
-  static constexpr int TURN = 16 * (NI * 16 * 4 + 16);                   // bytes of a wavefront's part in the epilogue
-  static constexpr int LDS = ST * STAGE > W * TURN ? ST * STAGE : W * TURN;
+  static constexpr int ABYTES = TM * T8_BK, BBYTES = TN * T8_BK, STAGE = ABYTES + BBYTES, RING = T8_ST * STAGE;
+  static constexpr int SCALES = (TM + 2 * TN) * 4, LDS = RING + 2 * SCALES;              // of two tiles: scales of rows and columns, biases
+  static constexpr int LA = ABYTES / 1024 / W, LB = BBYTES / 1024 / W, L = LA + LB;      // loads of a wavefront
+  static constexpr int PER_CU = 160 * 1024 / LDS < 2 ? 1 : 2;
   static_assert(ABYTES % (1024 * W) == 0 && BBYTES % (1024 * W) == 0, "whole loads");
 };
 
-// Four columns' values of 16 rows, turned through LDS, to rows of y
-template <int TYPE, int NI>
-__device__ __forceinline__ void t8_rows_out(char *turn, const w4_f4 v[NI], int lane, typename W4Mem<TYPE>::T *y, int64_t ldy, int rows, int cols) {
+// lanes m and m + 8 of 16 trade: afterwards lanes 0 - 7 hold the first words of rows 0 - 7 (a) and 8 - 15 (b), lanes 8 - 15 the second words
+__device__ __forceinline__ void t8_trade8(unsigned &a, unsigned &b) {
+  const unsigned first = (unsigned)__builtin_amdgcn_update_dpp((int)a, (int)b, 0x128, 0xF, 0xC, false);    // row_ror:8 to lanes 8 - 15
+  b = (unsigned)__builtin_amdgcn_update_dpp((int)b, (int)a, 0x128, 0xF, 0x3, false);                       // to lanes 0 - 7
+  a = first;
+}
+
+// 16 bytes of a row's columns from `col` on, of which `cols` exist
+template <int TYPE, bool WHOLE>
+__device__ __forceinline__ void t8_put16(typename W4Mem<TYPE>::T *row, int col, int cols, w4_u4 r) {
   using T = typename W4Mem<TYPE>::T;
-  typedef T vec __attribute__((ext_vector_type(4)));
-  constexpr int ES = sizeof(T), PITCH = NI * 16 * ES + 16, U = NI * ES, VE = 16 / ES;
-  const int m = lane & 15, g = lane >> 4;
+  constexpr int VE = 16 / sizeof(T);
+  if (WHOLE || col + VE <= cols) {
+    *(t8_u4 *)(row + col) = r;
+  } else {
+    typedef T all __attribute__((ext_vector_type(VE)));
+    const all q = __builtin_bit_cast(all, r);
 #pragma unroll
-  for (int j = 0; j < NI; ++j) {
-    vec r;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = W4Mem<TYPE>::put(v[j][e]);
-    *(vec *)(turn + m * PITCH + (j * 16 + 4 * g) * ES) = r;
+    for (int i = 0; i < VE; ++i)
+      if (col + i < cols) row[col + i] = q[i];
   }
+}
+
+// WHOLE: all of them exist.  16 rows' values, lane l's of row l % 16 and columns 16 j + 4 (l / 16) + e, to rows of y (its first row and column)
+template <int TYPE, int NI, bool WHOLE>
+__device__ __forceinline__ void t8_rows_out(const w4_f4 v[NI], int lane, typename W4Mem<TYPE>::T *y, int64_t ldy, int rows, int cols) {
+  using T = typename W4Mem<TYPE>::T;
+  typedef T four __attribute__((ext_vector_type(4)));
+  static_assert(NI % 4 == 0, "whole lines");
+  const int m = lane & 15, g = lane >> 4, low = m & 7, high = m >> 3;
+  T *first = y + low * ldy, *second = first + 8 * ldy;
+  if constexpr (sizeof(T) == 4) {
+    // blocks 2 j and 2 j + 1: a line
 #pragma unroll
-  for (int t = 0; t < U / 4; ++t) {
-    const int at = t * 64 + lane, row = at / U, u = at % U;
-    const w4_u4 r = *(const w4_u4 *)(turn + row * PITCH + u * 16);
-    T *to = y + row * ldy + u * VE;
-    if (row < rows) {
-      if (u * VE + VE <= cols) {
-        *(t8_u4 *)to = r;
-      } else {
-        typedef T all __attribute__((ext_vector_type(VE)));
-        const all q = __builtin_bit_cast(all, r);
+    for (int j = 0; j < NI; j += 2) {
+      w4_u4 a = __builtin_bit_cast(w4_u4, v[j]), b = __builtin_bit_cast(w4_u4, v[j + 1]);
 #pragma unroll
-        for (int i = 0; i < VE; ++i)
-          if (u * VE + i < cols) to[i] = q[i];
+      for (int e = 0; e < 4; ++e) {
+        unsigned p = a[e], q = b[e];
+        t8_trade8(p, q);
+        a[e] = p;
+        b[e] = q;
       }
+      const int col = (j + high) * 16 + 4 * g;
+      if (WHOLE || low < rows) t8_put16<TYPE, WHOLE>(first, col, cols, a);
+      if (WHOLE || low + 8 < rows) t8_put16<TYPE, WHOLE>(second, col, cols, b);
+    }
+  } else {
+    // four blocks: a line.  Lanes of even g take a block's 8 columns from their neighbours 16 on, of odd g the next block's
+    typedef unsigned u2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int j = 0; j < NI; j += 4) {
+      w4_u4 u[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        four p, q;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = W4Mem<TYPE>::put(v[j + 2 * h][e]);
+          q[e] = W4Mem<TYPE>::put(v[j + 2 * h + 1][e]);
+        }
+        const u2 pw = __builtin_bit_cast(u2, p), qw = __builtin_bit_cast(u2, q);
+        const u2 s0 = __builtin_amdgcn_permlane16_swap(pw[0], qw[0], false, false), s1 = __builtin_amdgcn_permlane16_swap(pw[1], qw[1], false, false);
+        u[h] = w4_u4{s0[0], s1[0], s0[1], s1[1]};
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        unsigned p = u[0][e], q = u[1][e];
+        t8_trade8(p, q);
+        u[0][e] = p;
+        u[1][e] = q;
+      }
+      const int col = j * 16 + 32 * high + 16 * (g & 1) + 8 * (g >> 1);
+      if (WHOLE || low < rows) t8_put16<TYPE, WHOLE>(first, col, cols, u[0]);
+      if (WHOLE || low + 8 < rows) t8_put16<TYPE, WHOLE>(second, col, cols, u[1]);
     }
   }
 }
 
 // P: 0 the forward product, else planes of a gradient.  PART: sums to the workspace.
-template <int TYPE, int P, bool PART, int BK, int ST, int WM, int WN, int MI, int NI>
-__global__ __launch_bounds__(64 * WM * WN, 2) void t8_tile_kernel(T8Product a) {
-  using S = T8Tile<BK, ST, WM, WN, MI, NI>;
-  constexpr int W = S::W, TM = S::TM, TN = S::TN, CH = BK / 16, RA = 1024 / BK;
+template <int TYPE, int P, bool PART, int WM, int WN, int MI, int NI>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_kernel(T8Product a) {
+  using S = T8Tile<WM, WN, MI, NI>;
+  constexpr int W = S::W, TM = S::TM, TN = S::TN, BK = T8_BK, ST = T8_ST, L = S::L;
   constexpr bool GRAD = P > 0;
   constexpr int CB = TN / 16, RB = 1024 / TN;              // gradient: chunks of a row of weights, rows of a load
   static_assert(P == 0 || MI % P == 0, "whole blocks of planes");
   extern __shared__ __align__(1024) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
-  int tile = blockIdx.x, part = 0;
-  const int total = a.tm * a.tn;
-  if (PART) {
-    part = tile / total;
-    tile -= part * total;
-  }
-  int ti, tj;
-  tile_at(tile, total, a.tm, a.tn, 8, ti, tj);
-  const int m0 = __builtin_amdgcn_readfirstlane(ti * TM), n0 = __builtin_amdgcn_readfirstlane(tj * TN);
+  const int wm = wave / WN * MI * 16, wn = wave % WN * NI * 16;
   const int cols = GRAD ? a.K : a.N, depth = GRAD ? (a.N + T8_SLAB - 1) / T8_SLAB * T8_SLAB : a.K;
-  const int all = (depth + BK - 1) / BK, s0 = PART ? part * a.per : 0, ns = PART ? min(a.per, all - s0) : all;
+  const int all = (depth + BK - 1) / BK, tiles = a.tm * a.tn;
 
-  // this lane's places in a wavefront's loads: row and chunk of what belongs there
-  const int lr = lane / CH, lc = (lane % CH) ^ t8_swz<BK>(lr);
-  unsigned ao[S::LA], bo[S::LB];
-#pragma unroll
-  for (int i = 0; i < S::LA; ++i) ao[i] = (unsigned)(min(m0 + (wave * S::LA + i) * RA + lr, a.arows - 1) - m0) * (unsigned)a.lda + lc * 16;
-#pragma unroll
-  for (int i = 0; i < S::LB; ++i) {
-    if constexpr (GRAD) {
-      const int r = (wave * S::LB + i) * RB + lane / CB, c = (lane % CB) ^ (r & (CB - 1));
-      bo[i] = (unsigned)min(n0 + c * 16, a.K - 16) - n0;
+  // The walk over the tiles: the workgroups of one XCD (every eighth) have a range of them, groups of 8 tile rows column by column, and take every
+  // step-th.  (Not more than one division, but in the last rows.)
+  struct At {
+    int m0, n0, s0, ns, part;
+  };
+  struct Walk {
+    int left, group, rows, in;                             // tiles of the range from this one on; group, its rows, place in it
+  };
+  const int step = ((int)gridDim.x + 7) >> 3;              // at least one, and no tile twice where the grid is the tiles
+  const auto begin = [&]() {
+    Walk w;
+    int t = blockIdx.x;
+    if (PART) {
+      t %= tiles;                                          // one a workgroup
+      w.left = 1;
     } else {
-      bo[i] = (unsigned)(min(n0 + (wave * S::LB + i) * RA + lr, a.N - 1) - n0) * (unsigned)a.ldw + lc * 16;
+      const int x = t & 7, q = tiles >> 3, r = tiles & 7;
+      w.left = q + (x < r) - (t >> 3);
+      t = x * q + min(x, r) + (t >> 3);
     }
-  }
-  // forward: chunks of the last slab beyond K re-read its end, and lie in LDS as zeros on the activations' side
-  const unsigned back = GRAD ? 0u : (unsigned)max((all - 1) * BK + lc * 16 + 16 - a.K, 0);
-  const int8_t *abase = a.a + (int64_t)m0 * a.lda, *bbase = a.w + (GRAD ? (int64_t)n0 : (int64_t)n0 * a.ldw);
+    w.group = t / (8 * a.tn);
+    w.in = t - w.group * 8 * a.tn;
+    w.rows = min(8, a.tm - w.group * 8);
+    return w;
+  };
+  const auto advance = [&](Walk &w) {
+    w.left -= step;
+    w.in += step;
+    if (w.left > 0)
+      while (w.in >= w.rows * a.tn) {
+        w.in -= w.rows * a.tn;
+        ++w.group;
+        w.rows = min(8, a.tm - w.group * 8);
+      }
+  };
+  const auto at = [&](const Walk &w) {
+    At r;
+    const int nj = w.rows == 8 ? w.in >> 3 : w.in / w.rows, mi = w.in - nj * w.rows;
+    r.m0 = __builtin_amdgcn_readfirstlane((w.group * 8 + mi) * TM);
+    r.n0 = __builtin_amdgcn_readfirstlane(nj * TN);
+    r.part = PART ? (int)blockIdx.x / tiles : 0;
+    r.s0 = PART ? r.part * a.per : 0;
+    r.ns = PART ? min(a.per, all - r.s0) : all;
+    return r;
+  };
+
+  // ---- slabs to LDS: this lane's places in a wavefront's loads, row and chunk of what belongs there
+  const int lr = lane / 8, lc = (lane % 8) ^ t8_swz<BK>(lr);
+  // forward: chunks of the last slab beyond K re-read its end, and become zeros on the activations' side
+  const auto back = [&](int c) { return (unsigned)max((all - 1) * BK + c * 16 + 16 - a.K, 0); };
+  // of the forward product's weights, block j's lane l reads row NI l + j, so that a lane's columns are neighbours: swizzled by l
+  const auto wc = [&](int i) { return (lane % 8) ^ (((wave * S::LB + i) * 8 + lr) / NI & 7); };
   const unsigned lds0 = t8_lds_address(smem);
-  const auto fetch = [&](int s, int stage) {               // s: slab of all
-    const bool last = s == all - 1;
-    const int row = min(s * BK, a.N - 1);                  // gradient: rows beyond the last meet zeros, and are the last
-    const unsigned to = lds0 + stage * S::STAGE;
+  unsigned ao[S::LA], bo[S::LB];
+  const int8_t *abase, *bbase;
+  Walk fw = begin();                                       // tile, slab and place of the next load
+  int fs = 0, fstage = 0;
+  At fat = at(fw);
+  const auto aim = [&]() {
 #pragma unroll
-    for (int i = 0; i < S::LA; ++i) t8_to_lds(to + (wave * S::LA + i) * 1024, ao[i] - (last ? back : 0u), abase + (int64_t)s * BK);
+    for (int i = 0; i < S::LA; ++i) ao[i] = (unsigned)(min(fat.m0 + (wave * S::LA + i) * 8 + lr, a.arows - 1) - fat.m0) * (unsigned)a.lda + lc * 16;
+#pragma unroll
+    for (int i = 0; i < S::LB; ++i) {
+      if constexpr (GRAD) {
+        const int r = (wave * S::LB + i) * RB + lane / CB, c = (lane % CB) ^ (r & (CB - 1));
+        bo[i] = (unsigned)(min(fat.n0 + c * 16, a.K - 16) - fat.n0);
+      } else {
+        bo[i] = (unsigned)(min(fat.n0 + (wave * S::LB + i) * 8 + lr, a.N - 1) - fat.n0) * (unsigned)a.ldw + wc(i) * 16;
+      }
+    }
+    abase = a.a + (int64_t)fat.m0 * a.lda;
+    bbase = a.w + (GRAD ? (int64_t)fat.n0 : (int64_t)fat.n0 * a.ldw);
+  };
+  aim();
+  const auto fetch = [&]() {
+    if (fw.left <= 0) return;
+    const int s = fat.s0 + fs;
+    const bool last = !GRAD && s == all - 1;
+    const int row = min(s * BK, a.N - 1);                  // gradient: rows beyond the last meet zeros, and are the last
+    const unsigned to = lds0 + fstage * S::STAGE;
+#pragma unroll
+    for (int i = 0; i < S::LA; ++i) t8_to_lds(to + (wave * S::LA + i) * 1024, ao[i] - (last ? back(lc) : 0u), abase + (int64_t)s * BK);
 #pragma unroll
     for (int i = 0; i < S::LB; ++i) {
       if constexpr (GRAD) {
         const int r = (wave * S::LB + i) * RB + lane / CB;
         t8_to_lds(to + S::ABYTES + (wave * S::LB + i) * 1024, bo[i] + (unsigned)min(r, a.N - 1 - row) * (unsigned)a.ldw, bbase + (int64_t)row * a.ldw);
       } else {
-        t8_to_lds(to + S::ABYTES + (wave * S::LB + i) * 1024, bo[i] - (last ? back : 0u), bbase + (int64_t)s * BK);
+        t8_to_lds(to + S::ABYTES + (wave * S::LB + i) * 1024, bo[i] - (last ? back(wc(i)) : 0u), bbase + (int64_t)s * BK);
+      }
+    }
+    fstage = fstage == ST - 1 ? 0 : fstage + 1;
+    if (++fs == fat.ns) {
+      fs = 0;
+      advance(fw);
+      if (fw.left > 0) {
+        fat = at(fw);
+        aim();
       }
     }
   };
 
-  t8_i4 acc[MI][NI];
+  t8_i4 acc[MI][NI], af[MI], bf[2][NI];
+  const auto clear = [&]() {
 #pragma unroll
-  for (int i = 0; i < MI; ++i)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-    for (int j = 0; j < NI; ++j) acc[i][j] = t8_i4{0, 0, 0, 0};
-  const int wm = wave / WN * MI * 16, wn = wave % WN * NI * 16;
+      for (int j = 0; j < NI; ++j) acc[i][j] = t8_i4{0, 0, 0, 0};
+  };
+  // the last slab of a K that is no whole slabs: zeros beyond it
+  const auto blank = [&](int stage) {
+    char *as = smem + stage * S::STAGE;
+    const int valid = a.K % BK / 16;
+    for (int t = threadIdx.x; t < TM * 8; t += 64 * W) {
+      const int r = t / 8, c = t % 8;
+      if (c >= valid) *(w4_u4 *)(as + r * BK + ((c ^ t8_swz<BK>(r)) << 4)) = w4_u4{};
+    }
+    t8_barrier();
+  };
+  // operands of half `kk` of the slab at `stage`
+  const auto read_w = [&](t8_i4 (&w)[NI], int stage, int kk) {
+    const char *bs = smem + stage * S::STAGE + S::ABYTES;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      if constexpr (GRAD) {
+        // lane l of 16 gives the place of row l / 2, half l % 2 of 16 columns, and gets column l of 8 rows
+        const int r = kk * 64 + g * 16 + (r16 >> 1), c = (wn >> 4) + j;
+        typedef __attribute__((address_space(3))) t8_i2 lds_i2;
+        const t8_i2 lo = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2 *)(bs + r * TN + ((c ^ (r & (CB - 1))) << 4) + (r16 & 1) * 8));
+        const t8_i2 hi = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2 *)(bs + (r + 8) * TN + ((c ^ ((r + 8) & (CB - 1))) << 4) + (r16 & 1) * 8));
+        w[j] = t8_i4{lo[0], lo[1], hi[0], hi[1]};
+      } else {
+        const int r = wn + r16 * NI + j;
+        w[j] = *(const t8_i4 *)(bs + r * BK + (((kk * 4 + g) ^ (r / NI & 7)) << 4));
+      }
+    }
+  };
+  const auto read_x = [&](int stage, int kk, int i) {
+    const int r = wm + i * 16 + r16;
+    return *(const t8_i4 *)(smem + stage * S::STAGE + r * BK + (((kk * 4 + g) ^ t8_swz<BK>(r)) << 4));
+  };
 
-  constexpr int L = S::LA + S::LB;
-#pragma unroll
-  for (int i = 0; i < ST - 1; ++i)
-    if (i < ns) fetch(s0 + i, i);
-  int stage = 0;
-  for (int s = 0; s < ns; ++s) {
-    if (ST > 2 && s + 1 < ns) t8_wait_barrier<(ST - 2) * L>();
-    else t8_wait_barrier<0>();
-    if (s + ST - 1 < ns) fetch(s0 + s + ST - 1, stage == 0 ? ST - 1 : stage - 1);
-    char *as = smem + stage * S::STAGE, *bs = as + S::ABYTES;
-    if (!GRAD && s == ns - 1 && a.K % BK) {
-      const int valid = a.K % BK / 16;
-      for (int t = threadIdx.x; t < TM * CH; t += 64 * W) {
-        const int r = t / CH, c = t % CH;
-        if (c >= valid) *(w4_u4 *)(as + r * BK + ((c ^ t8_swz<BK>(r)) << 4)) = w4_u4{};
-      }
-      t8_barrier();
-    }
-#pragma unroll
-    for (int kk = 0; kk < BK / 64; ++kk) {
-      t8_i4 af[MI], bf[NI];
-#pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        const int r = wm + i * 16 + r16;
-        af[i] = *(const t8_i4 *)(as + r * BK + (((kk * 4 + g) ^ t8_swz<BK>(r)) << 4));
-      }
-#pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        if constexpr (GRAD) {
-          // lane l of 16 gives the place of row l / 2, half l % 2 of 16 columns, and gets column l of 8 rows
-          const int r = kk * 64 + g * 16 + (r16 >> 1), c = (wn >> 4) + j;
-          typedef __attribute__((address_space(3))) t8_i2 lds_i2;
-          const t8_i2 lo = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2 *)(bs + r * TN + ((c ^ (r & (CB - 1))) << 4) + (r16 & 1) * 8));
-          const t8_i2 hi = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2 *)(bs + (r + 8) * TN + ((c ^ ((r + 8) & (CB - 1))) << 4) + (r16 & 1) * 8));
-          bf[j] = t8_i4{lo[0], lo[1], hi[0], hi[1]};
-        } else {
-          const int r = wn + j * 16 + r16;
-          bf[j] = *(const t8_i4 *)(bs + r * BK + (((kk * 4 + g) ^ t8_swz<BK>(r)) << 4));
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[j], af[i], acc[i][j], 0, 0, 0);
-    }
-    stage = stage == ST - 1 ? 0 : stage + 1;
-  }
-
-  const int col0 = n0 + wn;
-  if constexpr (PART) {
-    int32_t *to = a.part + (int64_t)part * a.arows * a.K;
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int r = m0 + wm + i * 16 + r16;
-#pragma unroll
-      for (int j = 0; j < NI; ++j)
-        if (r < a.arows && col0 + j * 16 < a.K) *(t8_i4 *)(to + (int64_t)r * a.K + col0 + j * 16 + 4 * g) = acc[i][j];
-    }
-    return;
-  }
-  t8_barrier();                                            // every wavefront has read its last operands
-  if (col0 >= cols) return;
   using T = typename W4Mem<TYPE>::T;
-  char *turn = smem + wave * S::TURN;
-  w4_f4 v[NI];
-  if constexpr (GRAD) {
-    if constexpr (P > 0) {
+  // scales and biases of a tile, 4 bytes a lane; their place alternates from tile to tile
+  const auto scales = [&](const At &p, int turn) {
+    if constexpr (!GRAD) {
+      const unsigned to = lds0 + S::RING + turn * S::SCALES;
+      for (int t = wave; t < TM / 64; t += W) t8_word_to_lds(to + t * 256, (unsigned)min(t * 64 + lane, a.M - 1 - p.m0) * 4, a.xs + p.m0);
+      for (int t = wave; t < TN / 64; t += W) {
+        const unsigned off = (unsigned)min(t * 64 + lane, a.N - 1 - p.n0) * 4;
+        t8_word_to_lds(to + TM * 4 + t * 256, off, a.ws + p.n0);
+        if (a.bias) t8_word_to_lds(to + (TM + TN) * 4 + t * 256, off, a.bias + p.n0);
+      }
+    }
+  };
+  const auto rows_of = [&](const At &p, int turn, auto whole, auto stream) {
+    constexpr bool WHOLE = decltype(whole)::value, STREAM = decltype(stream)::value;
+    const int col0 = p.n0 + wn;
+    w4_f4 v[NI];
+    if constexpr (GRAD) {
 #pragma unroll
-      for (int q = 0; q < MI / P; ++q) {
-        const int mb = ((m0 + wm) / 16 / P + q) * 16, m = mb + r16;
-        const float scale = a.xs[min(m, a.M - 1)];
+      for (int q = 0; q < MI / (P ? P : 1); ++q) {
+        const int mb = ((p.m0 + wm) / 16 / P + q) * 16;
+        const float scale = a.xs[WHOLE ? mb + r16 : min(mb + r16, a.M - 1)];
 #pragma unroll
         for (int j = 0; j < NI; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            int s[P];
+            int s[P ? P : 1];
 #pragma unroll
-            for (int p = 0; p < P; ++p) s[p] = acc[q * P + p][j][e];
+            for (int b = 0; b < P; ++b) s[b] = acc[q * P + b][j][e];
             v[j][e] = t8_join<P>(s, scale);
           }
-        t8_rows_out<TYPE, NI>(turn, v, lane, (T *)a.y + (int64_t)mb * a.ldy + col0, a.ldy, a.M - mb, cols - col0);
+        t8_rows_out<TYPE, NI, WHOLE>(v, lane, (T *)a.y + (int64_t)mb * a.ldy + col0, a.ldy, a.M - mb, cols - col0);
+      }
+    } else {
+      // a lane's rows 4 g + e of a block, and NI neighbouring columns: 16 lanes write whole lines
+      typedef T some __attribute__((ext_vector_type(NI)));
+      typedef some some_at __attribute__((aligned(sizeof(T))));
+      const float *xs = (const float *)(smem + S::RING + turn * S::SCALES), *ws = xs + TM, *bias = ws + TN;
+      float cs[NI], cb[NI];
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        cs[j] = ws[wn + r16 * NI + j];
+        cb[j] = a.bias ? bias[wn + r16 * NI + j] : 0.0f;
+      }
+      const int mb = p.m0 + wm + 4 * g, col = col0 + r16 * NI;
+      T *to = (T *)a.y + (int64_t)mb * a.ldy + col;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const w4_f4 scale = *(const w4_f4 *)(xs + wm + i * 16 + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          some r;
+#pragma unroll
+          for (int j = 0; j < NI; ++j) r[j] = W4Mem<TYPE>::put(__builtin_fmaf((float)acc[i][j][e] * cs[j], scale[e], cb[j]));
+          T *row = to + (int64_t)(i * 16 + e) * a.ldy;
+          if (WHOLE) {
+            if (STREAM) __builtin_nontemporal_store(r, (some_at *)row);
+            else *(some_at *)row = r;
+          } else if (mb + i * 16 + e < a.M) {
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+              if (col + j < cols) row[j] = r[j];
+          }
+        }
       }
     }
-  } else {
-    w4_f4 ws[NI], bias[NI];
+  };
+  const auto finish = [&](const At &p, int turn) {
+    const int col0 = p.n0 + wn;
+    if constexpr (PART) {
+      int32_t *to = a.part + (int64_t)p.part * a.arows * a.K;
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
+      for (int i = 0; i < MI; ++i) {
+        const int r = p.m0 + wm + i * 16 + r16;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = min(col0 + j * 16 + 4 * g + e, a.N - 1);
-        ws[j][e] = a.ws[n];
-        bias[j][e] = a.bias ? a.bias[n] : 0.0f;
+        for (int j = 0; j < NI; ++j)
+          if (r < a.arows && col0 + j * 16 < a.K) *(t8_i4 *)(to + (int64_t)r * a.K + col0 + j * 16 + 4 * g) = acc[i][j];
       }
+    } else if ((P ? (p.m0 + TM) / (P ? P : 1) : p.m0 + TM) <= a.M && p.n0 + TN <= cols) {
+      if (!GRAD && a.stream) rows_of(p, turn, std::true_type(), std::true_type());
+      else rows_of(p, turn, std::true_type(), std::false_type());
+    } else if (col0 < cols) {
+      rows_of(p, turn, std::false_type(), std::false_type());
+    }
+    clear();
+  };
+
+  // ---- slab after slab, tile after tile
+  if (fw.left <= 0) return;
+  const bool ragged = !GRAD && a.K % BK;
+  Walk cw = fw;
+  At cat = fat;
+  int cs = 0, stage = 0, turn = 0;                         // slab of the tile, place, and place of the scales of what is multiplied
+  // products of the operands in af and w, under which others come in: each row block's in the place of those just used
+  const auto half = [&](const t8_i4 (&w)[NI], t8_i4 (&nw)[NI], int from, int kk) {
+    read_w(nw, from, kk);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const int mb = m0 + wm + i * 16;
-      const float xs = a.xs[min(mb + r16, a.M - 1)];
 #pragma unroll
-      for (int j = 0; j < NI; ++j) v[j] = t8_finish(acc[i][j], ws[j], xs, bias[j]);
-      t8_rows_out<TYPE, NI>(turn, v, lane, (T *)a.y + (int64_t)mb * a.ldy + col0, a.ldy, a.M - mb, cols - col0);
+      for (int j = 0; j < NI; ++j)
+        acc[i][j] = GRAD ? __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], af[i], acc[i][j], 0, 0, 0) : __builtin_amdgcn_mfma_i32_16x16x64_i8(af[i], w[j], acc[i][j], 0, 0, 0);
+      af[i] = read_x(from, kk, i);
+    }
+    // in this order
+    __builtin_amdgcn_sched_group_barrier(0x100, GRAD ? 2 * NI : NI, 0);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x8, NI, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+  };
+  clear();
+  fetch();
+  const bool two = fw.left > 0;                            // a second slab, of this tile or another
+  fetch();
+  if (two) t8_wait_barrier<L>();
+  else t8_wait_barrier<0>();
+  if (ragged && cat.ns == 1) blank(0);
+  read_w(bf[0], 0, 0);
+#pragma unroll
+  for (int i = 0; i < MI; ++i) af[i] = read_x(0, 0, i);
+  for (;;) {
+    if (cs == 0) scales(cat, turn);
+    half(bf[0], bf[1], stage, 1);
+    const bool ends = cs + 1 == cat.ns;
+    const At p = cat;
+    if (ends) {
+      cs = 0;
+      advance(cw);
+      if (cw.left > 0) cat = at(cw);
+    } else {
+      ++cs;
+    }
+    const bool more = cw.left > 0;
+    // the next slab is there, and this one's operands are in registers
+    t8_wait_barrier<0>();
+    fetch();
+    stage ^= 1;
+    if (ragged && more && cs + 1 == cat.ns) blank(stage);
+    half(bf[1], bf[0], stage, 0);                          // (behind the last slab: some operands that nothing uses)
+    if (ends) {                                            // the epilogue takes the operands' registers: they are read again
+      finish(p, turn);
+      turn ^= 1;
+      if (!more) break;
+      read_w(bf[0], stage, 0);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) af[i] = read_x(stage, 0, i);
     }
   }
 }
@@ -244,37 +437,62 @@ __global__ __launch_bounds__(256) void t8_join_kernel(T8Product a) {
   }
 }
 
-template <int TYPE, int P, bool PART, int BK, int ST, int WM, int WN, int MI, int NI>
+template <int TYPE, int P, bool PART, int WM, int WN, int MI, int NI>
 static hipError_t tile_launch(T8Product a, hipStream_t st) {
-  using S = T8Tile<BK, ST, WM, WN, MI, NI>;
+  using S = T8Tile<WM, WN, MI, NI>;
   a.tm = (a.arows + S::TM - 1) / S::TM;
   a.tn = ((P ? a.K : a.N) + S::TN - 1) / S::TN;
+  // results that outgrow the L2 caches stream past them (16384 x 4608 x 1152 bfloat16, 151 MB: 103 -> 97 us; 4096 rows, 38 MB: 32.7 -> 28.7)
+  a.stream = (int64_t)a.M * a.N * (TYPE == QC_TYPE_F32 ? 4 : 2) > (32 << 20);
   static std::atomic<unsigned long long> done;
-  const auto kern = t8_tile_kernel<TYPE, P, PART, BK, ST, WM, WN, MI, NI>;
+  const auto kern = t8_tile_kernel<TYPE, P, PART, WM, WN, MI, NI>;
   if (S::LDS > 65536) {
     const hipError_t e = allow_lds((const void *)kern, S::LDS, done);
     if (e != hipSuccess) return e;
   }
-  kern<<<(unsigned)a.tm * (unsigned)a.tn * (unsigned)(PART ? a.split : 1), 64 * S::W, S::LDS, st>>>(a);
+  const int64_t tiles = (int64_t)a.tm * a.tn;
+  kern<<<(unsigned)(PART ? tiles * a.split : std::min<int64_t>(tiles, 256 * S::PER_CU)), 64 * S::W, S::LDS, st>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_t8_tile(const T8Product &a, int type, hipStream_t st) {
-  if (type == QC_TYPE_F32) return tile_launch<QC_TYPE_F32, 0, false, 64, 3, 1, 4, 8, 4>(a, st);
-  if (type == QC_TYPE_F16) return tile_launch<QC_TYPE_F16, 0, false, 64, 3, 1, 4, 8, 4>(a, st);
-  return tile_launch<QC_TYPE_BF16, 0, false, 64, 3, 1, 4, 8, 4>(a, st);
+// ---- Tiles: 256 x 256 by eight wavefronts, one workgroup a compute unit, or 128 x 128 by four, two.  The large one reads LDS half as often for a
+// product, the small one leaves fewer compute units without a tile.  us of a slab and of a tile's ends, by how much of the chip is taken
+// (measured at 16384 x 4608 x 128 - 4608, 16384 x 1152 x 4608 and 4096 x 8192 x 8192):
+struct TileCost {
+  int rows, cols, slots;
+  float slab, ends, slab_rest, ends_rest;                  // all slots taken; half of them or fewer
+};
+constexpr TileCost LARGE = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL = {128, 128, 512, 0.93f, 3.2f, 0.6f, 2.5f};
+
+static float tile_time(const TileCost &c, int64_t rows, int cols, int slabs) {
+  const int64_t tiles = ((rows + c.rows - 1) / c.rows) * ((cols + c.cols - 1) / c.cols), rest = tiles % c.slots;
+  const float full = c.slab * slabs + c.ends, last = rest == 0 ? 0.0f : rest > c.slots / 2 ? full : c.slab_rest * slabs + c.ends_rest;
+  return (float)(tiles / c.slots) * full + last;
+}
+static bool large_tiles(int64_t rows, int cols, int slabs) { return tile_time(LARGE, rows, cols, slabs) < tile_time(SMALL, rows, cols, slabs); }
+
+template <int TYPE, int P, bool PART>
+static hipError_t tile_of(const T8Product &a, hipStream_t st) {
+  if (!PART && large_tiles(a.arows, P ? a.K : a.N, ((P ? a.N : a.K) + T8_BK - 1) / T8_BK)) return tile_launch<TYPE, P, false, 2, 4, 8, 4>(a, st);
+  return tile_launch<TYPE, P, PART, 2, 2, 4, 4>(a, st);
 }
 
-// ---- the gradient: tiles of 128 rows of planes by 256 columns; fewer than fill the chip split the summed axis
+hipError_t launch_t8_tile(const T8Product &a, int type, hipStream_t st) {
+  if (type == QC_TYPE_F32) return tile_of<QC_TYPE_F32, 0, false>(a, st);
+  if (type == QC_TYPE_F16) return tile_of<QC_TYPE_F16, 0, false>(a, st);
+  return tile_of<QC_TYPE_BF16, 0, false>(a, st);
+}
+
+// ---- the gradient: launches of fewer tiles than fill the chip split the summed axis
 struct GradShape {
   int arows, split, per;
 };
 static GradShape grad_shape(int M, int N, int K, int type) {
   GradShape s;
-  const int P = t8_planes(type), slabs = (N + T8_SLAB - 1) / T8_SLAB * (T8_SLAB / 64);
+  const int P = t8_planes(type), slabs = (N + T8_BK - 1) / T8_BK;
   s.arows = (M + 15) / 16 * 16 * P;
-  const int64_t tiles = (int64_t)((s.arows + 127) / 128) * ((K + 255) / 256);
-  int split = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, slabs / 4));
+  const int64_t tiles = (int64_t)((s.arows + 127) / 128) * ((K + 127) / 128);
+  const int split = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, slabs / 2));
   s.per = (slabs + split - 1) / split;
   s.split = (slabs + s.per - 1) / s.per;
   return s;
@@ -292,8 +510,8 @@ static hipError_t grad_launch(T8Product a, hipStream_t st) {
   a.arows = s.arows;
   a.split = s.split;
   a.per = s.per;
-  if (s.split == 1) return tile_launch<TYPE, P, false, 64, 3, 1, 4, 8, 4>(a, st);
-  const hipError_t e = tile_launch<TYPE, P, true, 64, 3, 1, 4, 8, 4>(a, st);
+  if (s.split == 1) return tile_of<TYPE, P, false>(a, st);
+  const hipError_t e = tile_of<TYPE, P, true>(a, st);
   if (e != hipSuccess) return e;
   t8_join_kernel<TYPE><<<(unsigned)(((int64_t)a.M * (a.K / 4) + 255) / 256), 256, 0, st>>>(a);
   return hipGetLastError();

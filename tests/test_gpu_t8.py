@@ -78,7 +78,7 @@ def _same_codes(q, scale, v, what):
 
 
 # rows, width: one element, one row, odd everything, a vector and a bit, several rows a wavefront, wide rows, rows that are read again
-SHAPES = [(1, 1), (1, 8192), (3, 7), (5, 64), (2, 1153), (77, 1152), (9, 3081), (515, 40), (130, 513), (6000, 72), (17000, 33), (1030, 4608), (3, 16384),
+SHAPES = [(1, 1), (1, 8192), (3, 7), (5, 64), (2, 1153), (77, 1152), (9, 3081), (515, 40), (130, 513), (6000, 72), (17000, 33), (1500, 1153), (2100, 700), (1030, 4608), (2000, 9001), (3, 16384),
           (2, 16390), (1, 40000), (2, 131071)]
 
 
@@ -308,7 +308,9 @@ def test_gated_grad(qc, M, K, t, act):
 # M, N, K
 PRODUCTS = [(1, 1, 16), (1, 17, 48), (2, 33, 144), (5, 100, 1168), (1, 700, 4608), (16, 48, 384), (17, 64, 272), (33, 31, 656), (64, 130, 1152),
             (77, 257, 1040), (128, 128, 128), (129, 200, 912), (300, 384, 1152), (513, 261, 400), (600, 300, 64), (1030, 515, 80), (1, 40, 14336),
-            (2000, 1152, 208)]
+            (2000, 1152, 208),
+            # more tiles than workgroups, tiles of both sizes, ragged in every direction, one slab a tile, whole tiles
+            (4090, 4085, 272), (9000, 4608, 144), (2500, 8000, 48), (5000, 5120, 128), (8192, 1000, 1152)]
 
 
 def _codes(rng, M, K, pad):
