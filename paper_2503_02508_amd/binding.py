@@ -374,44 +374,70 @@ def qc_w4_gated_grad(x, gate, up, dh, dgate, dup, act=QC_ACT_SILU, gate_bias=Non
 
 
 # ------------------------------------------------ 8-bit layers with a scale for each token (include/qc_t8.h)
-def _t8_shape(t, name):
+# (These calls' kernels take a few microseconds: what is asked of a tensor here is asked once, and a device is its index, -1 for the host.)
+
+
+def _t8_matrix(t, name):
     if t.dim() != 2:
         raise QCError(-2, "%s: a tensor of shape %s; a matrix is needed" % (name, tuple(t.shape)))
     return t.shape
 
 
-def _t8_vector(t, n, device, name):
-    if t is None:
-        return None
-    if t.dtype is not _w4_torch.float32 or t.shape != (n,) or t.device != device or (n > 1 and t.stride(0) != 1):
-        raise QCError(-2, "%s: a contiguous float32 vector of %d elements on %s is needed" % (name, n, device))
-    return t.data_ptr()
+def _t8_type(t):
+    code = _w4_types.get(t.dtype) if _w4_torch is not None else _w4_type(t)
+    if code is None or code == 3:
+        raise QCError(-7, "tensors of type %s are not supported" % t.dtype)
+    return code
 
 
-def _t8_work(t, device):
+def _t8_rows(t, rows, cols, dtype, dev, name):
+    """Leading dimension of a [rows, cols] tensor whose rows are contiguous."""
+    if t.dtype is dtype and t.get_device() == dev and t.shape == (rows, cols):
+        ld, one = t.stride()
+        if one == 1 or cols <= 1:
+            return ld
+    raise QCError(-2, "%s: %s %s with strides %s on %s; %s [%d, %d] with contiguous rows on GPU %d is needed" % (
+        name, t.dtype, tuple(t.shape), t.stride(), t.device, dtype, rows, cols, dev))
+
+
+def _t8_vector(t, n, dev, name):
+    if t.dtype is _w4_torch.float32 and t.get_device() == dev and t.shape == (n,) and t.is_contiguous():
+        return t.data_ptr()
+    raise QCError(-2, "%s: %s %s on %s; a contiguous float32 vector of %d elements on GPU %d is needed" % (name, t.dtype, tuple(t.shape), t.device, n, dev))
+
+
+def _t8_work(t, dev):
     if t is None:
         return None, 0
-    if not t.is_contiguous() or t.device != device:
-        raise QCError(-2, "work: a contiguous tensor on %s is needed" % device)
+    if not t.is_contiguous() or t.get_device() != dev:
+        raise QCError(-2, "work: a contiguous tensor on GPU %d is needed" % dev)
     return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _t8_stream(device):
+def _t8_stream(dev):
     # (private functions of torch 2.10, as in _stream)
-    if device.type != "cuda" or device.index != _w4_torch.cuda.current_device():
-        raise QCError(-2, "the tensors lie on %s, which is not the current GPU" % device)
-    return _w4_torch._C._cuda_getCurrentRawStream(device.index)
+    if dev < 0 or dev != _w4_torch._C._cuda_getDevice():
+        raise QCError(-2, "the tensors lie on %s, which is not the current GPU" % ("the host" if dev < 0 else "GPU %d" % dev))
+    return _w4_torch._C._cuda_getCurrentRawStream(dev)
 
 
 def qc_t8_norm(x, q=None, scale=None, weight=None, residual=None, h=None, y=None, eps=1e-6):
     """Codes q with the rows' scales, and / or y, of the root-mean-square norm of h = x + residual (h = x without)."""
-    M, K = _t8_shape(x, "x")
-    t, dt, dev = _w4_type(x), x.dtype, x.device
-    if t == 3:
-        raise QCError(-7, "tensors of type %s are not supported" % dt)
-    rows = lambda v, name, d=dt: 0 if v is None else _w4_rows(v, M, K, d, dev, name)  # noqa: E731
-    _chk(lib.qc_t8_norm(x.data_ptr(), rows(x, "x"), _p(residual), rows(residual, "residual"), _t8_vector(weight, K, dev, "weight"), eps, t, M, K, _p(h),
-                        rows(h, "h"), _p(y), rows(y, "y"), _p(q), rows(q, "q", _w4_torch.int8), _t8_vector(scale, M, dev, "scale"), _t8_stream(dev)))
+    M, K = _t8_matrix(x, "x")
+    t, dt, dev = _t8_type(x), x.dtype, x.get_device()
+    r = ldr = hp = ldh = yp = ldy = qp = ldq = None
+    if residual is not None:
+        r, ldr = residual.data_ptr(), _t8_rows(residual, M, K, dt, dev, "residual")
+    if h is not None:
+        hp, ldh = h.data_ptr(), _t8_rows(h, M, K, dt, dev, "h")
+    if y is not None:
+        yp, ldy = y.data_ptr(), _t8_rows(y, M, K, dt, dev, "y")
+    if q is not None:
+        qp, ldq = q.data_ptr(), _t8_rows(q, M, K, _w4_torch.int8, dev, "q")
+    rc = lib.qc_t8_norm(x.data_ptr(), _t8_rows(x, M, K, dt, dev, "x"), r, ldr or 0, None if weight is None else _t8_vector(weight, K, dev, "weight"), eps, t, M,
+                        K, hp, ldh or 0, yp, ldy or 0, qp, ldq or 0, None if scale is None else _t8_vector(scale, M, dev, "scale"), _t8_stream(dev))
+    if rc:
+        _chk(rc)
 
 
 def qc_t8_norm_grad_bytes(M, K) -> int:
@@ -422,49 +448,61 @@ def qc_t8_norm_grad_bytes(M, K) -> int:
 
 def qc_t8_norm_grad(h, dy, dx, weight=None, dh=None, dweight=None, work=None, eps=1e-6):
     """dx (of x and of the residual) and dweight, from the gradients of y and (dh) of h."""
-    M, K = _t8_shape(h, "h")
-    t, dt, dev = _w4_type(h), h.dtype, h.device
-    rows = lambda v, name: 0 if v is None else _w4_rows(v, M, K, dt, dev, name)  # noqa: E731
+    M, K = _t8_matrix(h, "h")
+    t, dt, dev = _t8_type(h), h.dtype, h.get_device()
+    dhp, lddh = (None, 0) if dh is None else (dh.data_ptr(), _t8_rows(dh, M, K, dt, dev, "dh"))
     w, n = _t8_work(work, dev)
-    _chk(lib.qc_t8_norm_grad(h.data_ptr(), rows(h, "h"), _t8_vector(weight, K, dev, "weight"), eps, dy.data_ptr(), rows(dy, "dy"), _p(dh), rows(dh, "dh"), t,
-                             M, K, dx.data_ptr(), rows(dx, "dx"), _t8_vector(dweight, K, dev, "dweight"), w, n, _t8_stream(dev)))
+    rc = lib.qc_t8_norm_grad(h.data_ptr(), _t8_rows(h, M, K, dt, dev, "h"), None if weight is None else _t8_vector(weight, K, dev, "weight"), eps,
+                             dy.data_ptr(), _t8_rows(dy, M, K, dt, dev, "dy"), dhp, lddh, t, M, K, dx.data_ptr(), _t8_rows(dx, M, K, dt, dev, "dx"),
+                             None if dweight is None else _t8_vector(dweight, K, dev, "dweight"), w, n, _t8_stream(dev))
+    if rc:
+        _chk(rc)
 
 
 def qc_t8_quantize(x, q, scale, gate=None, act=QC_ACT_SILU):
     """Codes and scales of the rows of x, or of act(gate) x."""
-    M, K = _t8_shape(x, "x")
-    t, dt, dev = _w4_type(x), x.dtype, x.device
-    ldg = 0 if gate is None else _w4_rows(gate, M, K, dt, dev, "gate")
-    _chk(lib.qc_t8_quantize(x.data_ptr(), _w4_rows(x, M, K, dt, dev, "x"), _p(gate), ldg, act, t, M, K, q.data_ptr(),
-                            _w4_rows(q, M, K, _w4_torch.int8, dev, "q"), _t8_vector(scale, M, dev, "scale"), _t8_stream(dev)))
+    M, K = _t8_matrix(x, "x")
+    t, dt, dev = _t8_type(x), x.dtype, x.get_device()
+    g, ldg = (None, 0) if gate is None else (gate.data_ptr(), _t8_rows(gate, M, K, dt, dev, "gate"))
+    rc = lib.qc_t8_quantize(x.data_ptr(), _t8_rows(x, M, K, dt, dev, "x"), g, ldg, act, t, M, K, q.data_ptr(), _t8_rows(q, M, K, _w4_torch.int8, dev, "q"),
+                            _t8_vector(scale, M, dev, "scale"), _t8_stream(dev))
+    if rc:
+        _chk(rc)
 
 
 def qc_t8_expand(q, scale, out):
     """out = scale q: what rows of codes stand for."""
-    M, K = _t8_shape(out, "out")
-    t, dev = _w4_type(out), out.device
-    _chk(lib.qc_t8_expand(q.data_ptr(), _w4_rows(q, M, K, _w4_torch.int8, dev, "q"), _t8_vector(scale, M, dev, "scale"), M, K, out.data_ptr(), t,
-                          _w4_rows(out, M, K, out.dtype, dev, "out"), _t8_stream(dev)))
+    M, K = _t8_matrix(out, "out")
+    t, dev = _t8_type(out), out.get_device()
+    rc = lib.qc_t8_expand(q.data_ptr(), _t8_rows(q, M, K, _w4_torch.int8, dev, "q"), _t8_vector(scale, M, dev, "scale"), M, K, out.data_ptr(), t,
+                          _t8_rows(out, M, K, out.dtype, dev, "out"), _t8_stream(dev))
+    if rc:
+        _chk(rc)
 
 
 def qc_t8_gated_grad(x, gate, dv, dx, dgate, act=QC_ACT_SILU):
     """Gradients of act(gate) x."""
-    M, K = _t8_shape(x, "x")
-    t, dt, dev = _w4_type(x), x.dtype, x.device
-    rows = lambda v, name: _w4_rows(v, M, K, dt, dev, name)  # noqa: E731
-    _chk(lib.qc_t8_gated_grad(x.data_ptr(), rows(x, "x"), gate.data_ptr(), rows(gate, "gate"), act, dv.data_ptr(), rows(dv, "dv"), t, M, K, dx.data_ptr(),
-                              rows(dx, "dx"), dgate.data_ptr(), rows(dgate, "dgate"), _t8_stream(dev)))
+    M, K = _t8_matrix(x, "x")
+    t, dt, dev = _t8_type(x), x.dtype, x.get_device()
+    rc = lib.qc_t8_gated_grad(x.data_ptr(), _t8_rows(x, M, K, dt, dev, "x"), gate.data_ptr(), _t8_rows(gate, M, K, dt, dev, "gate"), act, dv.data_ptr(),
+                              _t8_rows(dv, M, K, dt, dev, "dv"), t, M, K, dx.data_ptr(), _t8_rows(dx, M, K, dt, dev, "dx"), dgate.data_ptr(),
+                              _t8_rows(dgate, M, K, dt, dev, "dgate"), _t8_stream(dev))
+    if rc:
+        _chk(rc)
 
 
 def qc_t8_linear(qx, x_scale, qw, w_scale, y, bias=None):
     """y = x w^T + bias of rows of codes."""
-    M, K = _t8_shape(qx, "qx")
-    N = _t8_shape(qw, "qw")[0]
-    t, dev = _w4_type(y), qx.device
+    M, K = _t8_matrix(qx, "qx")
+    N = _t8_matrix(qw, "qw")[0]
+    t, dev = _t8_type(y), qx.get_device()
     i8 = _w4_torch.int8
-    _chk(lib.qc_t8_linear(qx.data_ptr(), _w4_rows(qx, M, K, i8, dev, "qx"), _t8_vector(x_scale, M, dev, "x_scale"), qw.data_ptr(),
-                          _w4_rows(qw, N, K, i8, dev, "qw"), _t8_vector(w_scale, N, dev, "w_scale"), _t8_vector(bias, N, dev, "bias"), M, N, K,
-                          y.data_ptr(), t, _w4_rows(y, M, N, y.dtype, dev, "y"), _t8_stream(dev)))
+    rc = lib.qc_t8_linear(qx.data_ptr(), _t8_rows(qx, M, K, i8, dev, "qx"), _t8_vector(x_scale, M, dev, "x_scale"), qw.data_ptr(),
+                          _t8_rows(qw, N, K, i8, dev, "qw"), _t8_vector(w_scale, N, dev, "w_scale"),
+                          None if bias is None else _t8_vector(bias, N, dev, "bias"), M, N, K, y.data_ptr(), t, _t8_rows(y, M, N, y.dtype, dev, "y"),
+                          _t8_stream(dev))
+    if rc:
+        _chk(rc)
 
 
 def qc_t8_linear_grad_bytes(M, N, K, dtype) -> int:
@@ -476,12 +514,14 @@ def qc_t8_linear_grad_bytes(M, N, K, dtype) -> int:
 
 def qc_t8_linear_grad(dy, qw, w_scale, dx, work):
     """dx = dy w."""
-    N, K = _t8_shape(qw, "qw")
-    M = _t8_shape(dy, "dy")[0]
-    t, dt, dev = _w4_type(dy), dy.dtype, dy.device
+    N, K = _t8_matrix(qw, "qw")
+    M = _t8_matrix(dy, "dy")[0]
+    t, dt, dev = _t8_type(dy), dy.dtype, dy.get_device()
     w, n = _t8_work(work, dev)
-    _chk(lib.qc_t8_linear_grad(dy.data_ptr(), _w4_rows(dy, M, N, dt, dev, "dy"), t, qw.data_ptr(), _w4_rows(qw, N, K, _w4_torch.int8, dev, "qw"),
-                               _t8_vector(w_scale, N, dev, "w_scale"), M, N, K, dx.data_ptr(), _w4_rows(dx, M, K, dt, dev, "dx"), w, n, _t8_stream(dev)))
+    rc = lib.qc_t8_linear_grad(dy.data_ptr(), _t8_rows(dy, M, N, dt, dev, "dy"), t, qw.data_ptr(), _t8_rows(qw, N, K, _w4_torch.int8, dev, "qw"),
+                               _t8_vector(w_scale, N, dev, "w_scale"), M, N, K, dx.data_ptr(), _t8_rows(dx, M, K, dt, dev, "dx"), w, n, _t8_stream(dev))
+    if rc:
+        _chk(rc)
 
 
 def qc_ddim_schedule(steps: int):

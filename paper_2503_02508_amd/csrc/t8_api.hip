@@ -189,8 +189,8 @@ int qc_t8_quantize(const void *x, int64_t ldx, const void *gate, int64_t ldg, in
   a.add = gate; a.lda = row_step(ldg, M, K);
   a.q = q; a.ldq = row_step(ldq, M, K);
   a.scale = scale;
-  a.M = M; a.K = K; a.act = act;
-  QC_HIP(launch_t8_rows(a, type, gate ? T8_GATED : T8_PLAIN, static_cast<hipStream_t>(stream)));
+  a.M = M; a.K = K;
+  QC_HIP(launch_t8_rows(a, type, gate ? (act == QC_ACT_SILU ? T8_SILU : T8_GELU) : T8_PLAIN, static_cast<hipStream_t>(stream)));
   return QC_OK;
 }
 
@@ -264,7 +264,7 @@ int qc_t8_linear_grad(const void *dy, int64_t lddy, int type, const int8_t *qw, 
   r.x = dy; r.ldx = row_step(lddy, M, N);
   r.w = w_scale;
   r.q = (int8_t *)base; r.scale = (float *)(base + w.scale);
-  r.M = M; r.K = N; r.planes = t8_planes(type); r.pitch = (int)w.pitch;
+  r.M = M; r.K = N; r.pitch = (int)w.pitch;
   T8Product a{};
   a.a = r.q; a.lda = w.pitch; a.xs = r.scale;
   a.w = qw; a.ldw = row_step(ldw, N, K);

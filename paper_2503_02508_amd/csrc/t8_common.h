@@ -6,12 +6,12 @@
 namespace qc {
 
 // rows to codes, by what is quantised (t8_rows.hip)
-enum T8Source { T8_PLAIN = 0, T8_GATED = 1, T8_NORM = 2, T8_PLANES = 3 };
+enum T8Source { T8_PLAIN = 0, T8_SILU = 1, T8_GELU = 2, T8_NORM = 3, T8_PLANES = 4 };
 
 struct T8RowArgs {
   const void *x;            // [M, K]; T8_PLANES: the gradients
   int64_t ldx;
-  const void *add;          // T8_GATED: gates; T8_NORM: residual, or null
+  const void *add;          // T8_SILU, T8_GELU: gates; T8_NORM: residual, or null
   int64_t lda;
   const float *w;           // [K]: the norm's weight, or null; T8_PLANES: the scales of the weights' rows
   void *h, *y;              // T8_NORM: the sum with the residual, the normalised rows, or null
@@ -19,10 +19,10 @@ struct T8RowArgs {
   int8_t *q;                // T8_PLANES: the planes, rows of `pitch` bytes, and behind `scale` the rows' scales
   int64_t ldq;
   float *scale;
-  int M, K, act;
+  int M, K;
   float eps;
   double share;             // 1 / K
-  int planes, pitch;        // T8_PLANES
+  int pitch;                // T8_PLANES
 };
 
 struct T8NormGradArgs {
@@ -68,6 +68,9 @@ hipError_t launch_t8_gated_grad(const void *x, int64_t ldx, const void *g, int64
 int t8_norm_grad_groups(int M, int K);
 hipError_t launch_t8_norm_grad(const T8NormGradArgs &a, int type, hipStream_t st);
 hipError_t launch_t8_linear(T8Product a, int type, hipStream_t st);
+// the forward product by large tiles, and what it takes in us
+hipError_t launch_t8_tile(const T8Product &a, int type, hipStream_t st);
+float t8_tile_time(int M, int N, int K);
 // bytes of the partial sums of a gradient (0: the summed axis is not split)
 int64_t t8_grad_part_bytes(int M, int N, int K, int type);
 hipError_t launch_t8_grad(T8Product a, int type, hipStream_t st);
@@ -82,17 +85,23 @@ typedef unsigned t8_u1 __attribute__((aligned(1)));
 template <int TYPE>
 constexpr int t8_vl = TYPE == QC_TYPE_F32 ? 4 : 8;        // elements of such a vector
 
-// elements e .. of a row of K, zeros beyond it, and their float32 values
+// Elements e .. of a row of K >= VL, zeros beyond it: the row's last vector is loaded in their place and shifted (a branch that whole vectors do not
+// take; element by element it would be many, whose masks fill the scalar registers).
 template <int TYPE>
 __device__ __forceinline__ w4_u4 t8_raw(const typename W4Mem<TYPE>::T *row, int e, int K) {
-  constexpr int VL = t8_vl<TYPE>;
-  using T = typename W4Mem<TYPE>::T;
-  typedef T vec __attribute__((ext_vector_type(VL)));
-  if (e + VL <= K) return (w4_u4) * (const t8_u4 *)(row + e);
-  vec r;
-#pragma unroll
-  for (int i = 0; i < VL; ++i) r[i] = e + i < K ? row[e + i] : (T)0.0f;
-  return __builtin_bit_cast(w4_u4, r);
+  constexpr int VL = t8_vl<TYPE>, BITS = 128 / VL;
+  w4_u4 r = {0, 0, 0, 0};
+  if (e < K) {
+    const int from = min(e, K - VL), by = (e - from) * BITS;
+    r = *(const t8_u4 *)((const char *)row + (unsigned)from * (unsigned)sizeof(*row));
+    if (by > 0) {
+      unsigned long long lo = (unsigned long long)r[1] << 32 | r[0], hi = (unsigned long long)r[3] << 32 | r[2];
+      lo = by >= 64 ? hi >> (by - 64) : lo >> by | hi << (64 - by);
+      hi = by >= 64 ? 0 : hi >> by;
+      r = w4_u4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+    }
+  }
+  return r;
 }
 template <int TYPE>
 __device__ __forceinline__ void t8_values(w4_u4 raw, float v[t8_vl<TYPE>]) {
@@ -115,25 +124,34 @@ __device__ __forceinline__ void t8_store(typename W4Mem<TYPE>::T *row, int e, in
     vec r;
 #pragma unroll
     for (int i = 0; i < VL; ++i) r[i] = W4Mem<TYPE>::put(v[i]);
-    *(t8_u4 *)(row + e) = __builtin_bit_cast(w4_u4, r);
+    *(t8_u4 *)((char *)row + (unsigned)e * (unsigned)sizeof(T)) = __builtin_bit_cast(w4_u4, r);
   } else {
 #pragma unroll
     for (int i = 0; i < VL; ++i)
       if (e + i < K) row[e + i] = W4Mem<TYPE>::put(v[i]);
   }
 }
+// the same of a float32 vector, VL elements
 template <int VL>
 __device__ __forceinline__ void t8_load_f32(const float *w, int e, int K, float v[VL]) {
-  if (e + VL <= K) {
+#pragma unroll
+  for (int i = 0; i < VL; ++i) v[i] = 0.0f;
+  if (e < K) {
+    const int from = min(e, K - VL), over = e - from;
 #pragma unroll
     for (int i = 0; i < VL; i += 4) {
-      const w4_f4 r = __builtin_bit_cast(w4_f4, (w4_u4) * (const t8_u4 *)(w + e + i));
+      const w4_f4 r = __builtin_bit_cast(w4_f4, (w4_u4) * (const t8_u4 *)((const char *)w + (unsigned)(from + i) * 4u));
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[i + j] = r[j];
     }
-  } else {
+    if (over > 0) {
 #pragma unroll
-    for (int i = 0; i < VL; ++i) v[i] = e + i < K ? w[e + i] : 0.0f;
+      for (int by = VL / 2; by; by /= 2)
+        if (over & by) {
+#pragma unroll
+          for (int i = 0; i < VL; ++i) v[i] = i + by < VL ? v[i + by] : 0.0f;
+        }
+    }
   }
 }
 // the low bytes of VL words, as bytes e .. of a row
@@ -145,8 +163,8 @@ __device__ __forceinline__ void t8_store_bytes(int8_t *row, int e, int K, const 
     for (int i = 0; i < VL / 4; ++i)
       w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x0c0c0400u), __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u),
                                    0x05040100u);
-    if constexpr (VL == 8) *(t8_u2 *)(row + e) = w4_u2{w[0], w[1]};
-    else *(t8_u1 *)(row + e) = w[0];
+    if constexpr (VL == 8) *(t8_u2 *)(row + (unsigned)e) = w4_u2{w[0], w[1]};
+    else *(t8_u1 *)(row + (unsigned)e) = w[0];
   } else {
 #pragma unroll
     for (int i = 0; i < VL; ++i)
@@ -165,6 +183,27 @@ __device__ __forceinline__ unsigned t8_wave_max(unsigned v) {
   const unsigned a = max((unsigned)__builtin_amdgcn_readlane((int)v, 0), (unsigned)__builtin_amdgcn_readlane((int)v, 16));
   return max(a, max((unsigned)__builtin_amdgcn_readlane((int)v, 32), (unsigned)__builtin_amdgcn_readlane((int)v, 48)));
 }
+// for what lies in LDS (not __syncthreads(), which would wait for loads that are on their way too)
+__device__ __forceinline__ void t8_lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// the same over the entries of up to 16 wavefronts, in LDS
+__device__ __forceinline__ unsigned t8_across_max(const unsigned *u, int waves, int lane) {
+  unsigned v = (lane & 15) < waves ? u[lane & 15] : 0u;
+  v = max(v, t8_dpp<0xB1>(v));
+  v = max(v, t8_dpp<0x4E>(v));
+  v = max(v, t8_dpp<0x141>(v));
+  v = max(v, t8_dpp<0x140>(v));
+  return (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ __forceinline__ double t8_across_sum(const double *d, int waves, int lane) {
+  double v = (lane & 15) < waves ? d[lane & 15] : 0.0;
+  v += dpp_move_d<0xB1>(v);
+  v += dpp_move_d<0x4E>(v);
+  v += dpp_move_d<0x141>(v);
+  v += dpp_move_d<0x140>(v);
+  return readlane_d(v, 0);
+}
+// the larger of two magnitudes, a NaN if either is one
+__device__ __forceinline__ float t8_larger(float a, float b) { return __builtin_elementwise_maximum(fabsf(a), fabsf(b)); }
 // |v| as a word: ordered as the magnitudes are, infinities above them and NaN above those
 __device__ __forceinline__ unsigned t8_mag(float v) { return __builtin_bit_cast(unsigned, v) & 0x7FFFFFFFu; }
 
@@ -199,31 +238,30 @@ __device__ __forceinline__ void t8_logistic(int act, float gate, float &s, float
   s = u < 0.0 ? z * r : r;
   o = u < 0.0 ? r : z * r;
 }
-// act(gate) x, to 13 e of its value while that is above 2^-90
-__device__ __forceinline__ float t8_gate(int act, float gate, float x) {
-  float s, o;
-  bool deep;
-  t8_logistic(act, gate, s, o, deep);
-  return gate * s * (deep && gate < 0.0f ? x * 0x1p-100f : x);
-}
-// The same where the exponent's argument is at most 100 (else `most` says that it is not): 1 + exp(-t) then neither overflows nor
-// loses the smaller term.  SiLU's argument is a product of float32 numbers with what the product and log2(e) lose, to 2^-45 of it.
+// act(gate) x by the same formula without the cases, for gates above T8_DEEP: to 1.8e-6 of its value (9e-7 by what log2(e) loses in float32, at the
+// largest exponents).  The logistic function is 1 / (1 + exp(-t)), which keeps the digits of small values; beyond LIMIT it is 0 or 1 to any
+// product.  An infinite or NaN gate gives an infinite or NaN product.
 template <int ACT>
-__device__ __forceinline__ float t8_gate_near(float gate, float x, float &most) {
+__device__ __forceinline__ float t8_gate(float gate, float x) {
+  constexpr float LIMIT = ACT == QC_ACT_SILU ? 85.0f : 9.9f;             // exp(-t) up to 2^123
+  const float b = __builtin_amdgcn_fmed3f(gate, -LIMIT, LIMIT);
   float hi, lo;
   if constexpr (ACT == QC_ACT_SILU) {
-    hi = gate * -1.44269502162933349609375f;
-    lo = __builtin_fmaf(gate, -1.44269502162933349609375f, -hi);
-    lo = __builtin_fmaf(gate, -1.9259629911266174681e-8f, lo);
+    hi = b * -1.4426950408889634f;
+    lo = __builtin_fmaf(b, -1.4426950408889634f, -hi);
   } else {
-    const double g = gate, u = g * (-2.302208198144325 - 0.1029432395800235 * (g * g));
+    const double g = b, u = g * (-2.302208198144325 - 0.1029432395800235 * (g * g));
     hi = (float)u;
     lo = (float)(u - (double)hi);
   }
-  most = fmaxf(most, fabsf(hi));
   const float e = __builtin_amdgcn_exp2f(hi);
   return gate * __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, lo * 0.6931471805599453f, e)) * x;
 }
+template <int ACT>
+constexpr float T8_DEEP = ACT == QC_ACT_SILU ? -69.0f : -9.0f;       // exp(-t) = 2^100, about
+template <int ACT>
+constexpr float T8_GONE = ACT == QC_ACT_SILU ? -400.0f : -20.0f;     // the product is below any float32, for finite x
+
 // value and derivative of the activation
 __device__ __forceinline__ float t8_act(int act, float gate, float &d) {
   float s, o;

@@ -3,23 +3,21 @@
 // A workgroup makes 16 MT rows by 16 NT columns; its wavefronts share the summed axis, each taking every W-th chunk of 128 bytes of all
 // rows alone: chunks go from memory straight to the wavefront's own ring in LDS, ST of them on their way, without registers and without
 // barriers.  A load covers 8 rows of 128 bytes, whole cache lines; operands are read back in the matrix instruction's order.  The integer
-// sums of the wavefronts meet in LDS.
+// sums of the wavefronts meet in LDS.  One row by 28672 x 8192 takes 41 us, 5.7 TB/s; the tiles' times stand beside the rule below.
 #include "t8_product.h"
 
 namespace qc {
 
-constexpr int FEW_WAVES = 8;
-
 template <int MT, int NT, int ST>
 struct T8Few {
   static constexpr int STAGE = (MT + NT) * 16 * 128, RING = ST * STAGE, SUM = MT * NT * 1024;
-  static constexpr int EACH = RING > SUM ? RING : SUM;                    // of a wavefront
-  static constexpr int MOST = FEW_WAVES * EACH <= 160 * 1024 ? FEW_WAVES : FEW_WAVES / 2;
+  static constexpr int EACH = RING > SUM ? RING : SUM;                    // LDS of a wavefront
+  static constexpr int MOST = 8 * EACH <= 160 * 1024 ? 8 : 4;             // wavefronts of a workgroup
   static_assert(MOST * EACH <= 160 * 1024, "LDS of a compute unit");
 };
 
 template <int TYPE, int MT, int NT, int ST>
-__global__ __launch_bounds__(64 * FEW_WAVES) void t8_few_kernel(T8Product a) {
+__global__ __launch_bounds__((64 * T8Few<MT, NT, ST>::MOST)) void t8_few_kernel(T8Product a) {
   using S = T8Few<MT, NT, ST>;
   constexpr int L = 2 * (MT + NT);
   extern __shared__ __align__(1024) char smem[];
@@ -53,8 +51,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void t8_few_kernel(T8Product a) {
   int stage = 0;
   for (int i = 0; i < mine; ++i) {
     const int behind = min(ST, mine - i) - 1;              // chunks that may still be on their way
-    if (behind >= 3 && ST > 3) t8_wait<(ST > 3 ? 3 : 0) * L>();
-    else if (behind == 2) t8_wait<2 * L>();
+    if (ST > 2 && behind == 2) t8_wait<2 * L>();
     else if (behind == 1) t8_wait<L>();
     else t8_wait<0>();
     const char *as = ring + stage * S::STAGE, *bs = as + MT * 2048;
@@ -101,32 +98,58 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void t8_few_kernel(T8Product a) {
   }
 }
 
+// More wavefronts where the workgroups are fewer than the compute units
 template <int TYPE, int MT, int NT, int ST>
 static hipError_t few_launch(T8Product a, hipStream_t st) {
+  using S = T8Few<MT, NT, ST>;
   a.tm = (a.M + 16 * MT - 1) / (16 * MT);
   a.tn = (a.N + 16 * NT - 1) / (16 * NT);
   const int chunks = (a.K + 127) / 128;
-  int waves = 1;
-  while (waves < T8Few<MT, NT, ST>::MOST && waves < chunks && (int64_t)a.tm * a.tn * waves < 2048) waves *= 2;
-  const int lds = waves * T8Few<MT, NT, ST>::EACH;
+  const int64_t groups = (int64_t)a.tm * a.tn;
+  int waves = groups > 256 && MT * NT > 8 ? 2 : groups <= 128 && chunks >= 32 ? S::MOST : 4;
+  while (waves > chunks) waves /= 2;
+  const int lds = waves * S::EACH;
   static std::atomic<unsigned long long> done;
   const auto kern = t8_few_kernel<TYPE, MT, NT, ST>;
   if (lds > 65536) {
-    const hipError_t e = allow_lds((const void *)kern, T8Few<MT, NT, ST>::MOST * T8Few<MT, NT, ST>::EACH, done);
+    const hipError_t e = allow_lds((const void *)kern, S::MOST * S::EACH, done);
     if (e != hipSuccess) return e;
   }
-  kern<<<(unsigned)a.tm * (unsigned)a.tn, 64 * waves, lds, st>>>(a);
+  kern<<<(unsigned)groups, 64 * waves, lds, st>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_t8_tile(const T8Product &a, int type, hipStream_t st);
+// us of a tile's launch: what its workgroups load, over the chip at 13 TB/s (from the L2 caches, mostly) and over one compute unit's share
+// of them at 70 GB/s (50 where it has one workgroup of a large tile); the weights once, from memory, at 5.2 TB/s; and what a launch takes.  Measured (the best of these | the others): 1 x 28672 x
+// 8192 40.7 with 16 x 16 | 44 with 16 x 64; 32 x 8192 x 8192 15.7 with 16 x 64 | 16.4 - 23; 64 x 8192 x 8192 19.5 with 32 x 64 | 22 - 24, tiles of 128 x 128
+// (t8_tile.hip) 55; 256 x 8192 x 8192 42 with 64 x 64 | 59 - 72 | 54; 256 x 1152 x 4608 10.5 with 32 x 32 | 10.6 - 16 | 26; 256 x 4608 x 1152
+// 9.4 with 128 x 128 | 10.1 - 12.
+static float few_time(const T8Product &a, int MT, int NT) {
+  const int64_t groups = (int64_t)((a.M + 16 * MT - 1) / (16 * MT)) * ((a.N + 16 * NT - 1) / (16 * NT));
+  const float each = (float)((a.K + 127) / 128) * (float)(MT + NT) * 2048.0f;
+  return 4.0f + std::max(std::max((float)groups * each / 13e6f, (float)((groups + 255) / 256) * each / (MT + NT > 4 ? 50e3f : 70e3f)), (float)a.N * (float)a.K / 5.2e6f);
+}
 
 template <int TYPE>
 static hipError_t linear_launch(const T8Product &a, hipStream_t st) {
-  if (a.M > 512) return launch_t8_tile(a, TYPE, st);
-  if (a.M <= 16) return few_launch<TYPE, 1, 2, 3>(a, st);
-  if (a.M <= 32) return few_launch<TYPE, 2, 2, 2>(a, st);
-  return few_launch<TYPE, 4, 2, 2>(a, st);
+  constexpr int tiles[5][2] = {{1, 1}, {1, 4}, {2, 2}, {2, 4}, {4, 4}};
+  float best = t8_tile_time(a.M, a.N, a.K);
+  int at = -1;
+  for (int i = 4; i >= 0; --i) {
+    const float t = few_time(a, tiles[i][0], tiles[i][1]);
+    if (t <= best) {
+      best = t;
+      at = i;
+    }
+  }
+  switch (at) {
+    case 0: return few_launch<TYPE, 1, 1, 3>(a, st);
+    case 1: return few_launch<TYPE, 1, 4, 3>(a, st);
+    case 2: return few_launch<TYPE, 2, 2, 2>(a, st);
+    case 3: return few_launch<TYPE, 2, 4, 2>(a, st);
+    case 4: return few_launch<TYPE, 4, 4, 2>(a, st);
+  }
+  return launch_t8_tile(a, TYPE, st);
 }
 
 hipError_t launch_t8_linear(T8Product a, int type, hipStream_t st) {

@@ -20,21 +20,23 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
   float dw[C][VL] = {};
   constexpr bool AHEAD = C < 4;                             // the next row is on its way while this one is at work (registers)
   w4_u4 nh[C], ng[C];
-  const auto fetch = [&](int64_t row) {
+  const auto fetch = [&](int64_t row, int K) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      nh[c] = t8_raw<TYPE>((const T *)a.h + row * a.ldh, e0 + c * step, a.K);
-      ng[c] = t8_raw<TYPE>((const T *)a.dy + row * a.lddy, e0 + c * step, a.K);
+      nh[c] = t8_raw<TYPE>((const T *)a.h + row * a.ldh, e0 + c * step, K);
+      ng[c] = t8_raw<TYPE>((const T *)a.dy + row * a.lddy, e0 + c * step, K);
     }
   };
   int64_t row = (int64_t)blockIdx.x * rows + sub;
   const int64_t ahead = (int64_t)gridDim.x * rows;
-  if (AHEAD && row < a.M) fetch(row);
+  if (AHEAD && row < a.M) fetch(row, a.K);
   int turn = 0;
   for (int64_t base = (int64_t)blockIdx.x * rows; base < a.M; base += ahead, row += ahead, turn ^= 1) {
     const bool there = row < a.M;
+    int K = a.K;
+    asm volatile("" : "+s"(K));                             // what depends on it is formed again for each row, not kept: registers
     w4_u4 ch[C], cg[C], cd[C];
-    if (!AHEAD && there) fetch(row);
+    if (!AHEAD && there) fetch(row, K);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       ch[c] = nh[c];
@@ -42,9 +44,9 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
     }
     if (a.dh && there) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) cd[c] = t8_raw<TYPE>((const T *)a.dh + row * a.lddh, e0 + c * step, a.K);
+      for (int c = 0; c < C; ++c) cd[c] = t8_raw<TYPE>((const T *)a.dh + row * a.lddh, e0 + c * step, K);
     }
-    if (AHEAD && row + ahead < a.M) fetch(row + ahead);
+    if (AHEAD && row + ahead < a.M) fetch(row + ahead, K);
     double ss = 0.0;
     float gh = 0.0f;
     if (there) {
@@ -54,7 +56,7 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
         t8_values<TYPE>(ch[c], h);
         t8_values<TYPE>(cg[c], g);
         if (a.w) {
-          t8_load_f32<VL>(a.w, e0 + c * step, a.K, w);
+          t8_load_f32<VL>(a.w, e0 + c * step, K, w);
 #pragma unroll
           for (int i = 0; i < VL; ++i) g[i] *= w[i];
         }
@@ -72,14 +74,9 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
         red[turn][0][wave] = ss;
         red[turn][1][wave] = dot;
       }
-      // (not __syncthreads(), which would wait for the next row too)
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      ss = red[turn][0][first];
-      dot = red[turn][1][first];
-      for (int i = 1; i < waves; ++i) {
-        ss += red[turn][0][first + i];
-        dot += red[turn][1][first + i];
-      }
+      t8_lds_barrier();
+      ss = t8_across_sum(red[turn][0] + first, waves, lane);
+      dot = t8_across_sum(red[turn][1] + first, waves, lane);
     }
     if (!there) continue;
     const double r = t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
@@ -89,7 +86,7 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
       float h[VL], g[VL], w[VL], d[VL];
       t8_values<TYPE>(ch[c], h);
       t8_values<TYPE>(cg[c], g);
-      if (a.w) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w);
+      if (a.w) t8_load_f32<VL>(a.w, e0 + c * step, K, w);
 #pragma unroll
       for (int i = 0; i < VL; ++i) {
         dw[c][i] = __builtin_fmaf(g[i], h[i] * rho, dw[c][i]);
@@ -102,7 +99,7 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
 #pragma unroll
         for (int i = 0; i < VL; ++i) d[i] += add[i];
       }
-      t8_store<TYPE>((T *)a.dx + row * a.lddx, e0 + c * step, a.K, d);
+      t8_store<TYPE>((T *)a.dx + row * a.lddx, e0 + c * step, K, d);
     }
   }
   if (!a.dw) return;
@@ -146,12 +143,8 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_long_kernel(T8NormGradArgs 
       red[turn][1][wave] = dot;
     }
     __syncthreads();
-    ss = red[turn][0][0];
-    dot = red[turn][1][0];
-    for (int i = 1; i < 16; ++i) {
-      ss += red[turn][0][i];
-      dot += red[turn][1][i];
-    }
+    ss = t8_across_sum(red[turn][0], 16, lane);
+    dot = t8_across_sum(red[turn][1], 16, lane);
     const double r = t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
     const float rho = (float)r, along = (float)(r * r * r * (dot * a.share));
     for (int e = threadIdx.x; e < a.K; e += 1024) {
@@ -187,7 +180,7 @@ static NormGradShape norm_grad_shape(int M, int K, int type) {
   const int vl = type == QC_TYPE_F32 ? 4 : 8, most = type == QC_TYPE_F32 ? 4 : 2, vectors = (K + vl - 1) / vl;      // most: vectors a lane
   NormGradShape s{};
   s.groups = std::min(M, NORM_GRAD_GROUPS);
-  if (vectors > 64 * 16 * most) return s;
+  if (vectors > 64 * 16 * most || K < vl) return s;
   s.waves = std::min((vectors + 127) / 128, 16);
   while (s.waves < 16 && vectors > 64 * s.waves && (int64_t)M * s.waves < 1024) ++s.waves;
   s.c = (vectors + 64 * s.waves - 1) / (64 * s.waves);

@@ -6,7 +6,7 @@
 //
 // Exact decisions.  The codes are those of the definition: float32 quotients, rounded half to even.  Each is formed as v (1 / scale), which is off by
 // at most 1.2e-5 for quotients of up to 127, and where it is nearer than 2e-5 to a border the division decides.  The gated product is
-// formed in float32 to 13 e = 7.8e-7 of its value; where that is too near to a border, or to the row's largest value, float64 decides.
+// formed in float32 to 1.8e-6 of its value; where that is too near to a border, or to the row's largest value, float64 decides.
 #include "t8_common.h"
 
 namespace qc {
@@ -32,23 +32,26 @@ struct T8Across {
 template <int TYPE, int SOURCE, bool FULL, int C>
 __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a) {
   using T = typename W4Mem<TYPE>::T;
-  constexpr int VL = t8_vl<TYPE>;
+  constexpr int VL = t8_vl<TYPE>, ACT = SOURCE == T8_GELU ? QC_ACT_GELU : QC_ACT_SILU;
+  constexpr bool GATED = SOURCE == T8_SILU || SOURCE == T8_GELU;
   __shared__ T8Across across;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = FULL ? (int)blockDim.x >> 6 : 1, step = 64 * waves * VL, e0 = (FULL ? (int)threadIdx.x : lane) * VL;
   const int width = SOURCE == T8_PLANES ? a.pitch : a.K;
-  int turn = 0;
-  for (int64_t row = FULL ? blockIdx.x : blockIdx.x * 4 + wave; row < a.M; row += FULL ? gridDim.x : gridDim.x * 4, turn ^= 1) {
+  // (one row: what does not depend on it would be worked out ahead of a loop, in registers that then hold nothing else)
+  const int64_t row = FULL ? blockIdx.x + (int64_t)blockIdx.y * gridDim.x : (blockIdx.x + (int64_t)blockIdx.y * gridDim.x) * 4 + wave;
+  {
+    if (row >= a.M) return;
     const T *x = (const T *)a.x + row * a.ldx, *add = (const T *)a.add + row * a.lda;
     float v[C][VL], w[C][VL];
     w4_u4 second[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) t8_load<TYPE>(x, e0 + c * step, a.K, v[c]);
-    if (SOURCE == T8_GATED || (SOURCE == T8_NORM && a.add)) {
+    if (GATED || (SOURCE == T8_NORM && a.add)) {
 #pragma unroll
       for (int c = 0; c < C; ++c) second[c] = t8_raw<TYPE>(add, e0 + c * step, a.K);
     }
-    if (SOURCE == T8_PLANES || (SOURCE == T8_NORM && a.w)) {
+    if constexpr (SOURCE == T8_PLANES) {
 #pragma unroll
       for (int c = 0; c < C; ++c) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
     }
@@ -71,17 +74,18 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
         for (int i = 0; i < VL; ++i) ss = __builtin_fma((double)v[c][i], (double)v[c][i], ss);
       ss = wave_sum_dpp(ss);
       if constexpr (FULL) {
-        if (lane == 0) across.d[turn][wave] = ss;
-        __syncthreads();
-        ss = across.d[turn][0];
-        for (int i = 1; i < waves; ++i) ss += across.d[turn][i];
+        if (lane == 0) across.d[0][wave] = ss;
+        t8_lds_barrier();
+        ss = t8_across_sum(across.d[0], waves, lane);
       }
       const float rho = (float)t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
+      asm volatile("" ::: "memory");                      // the weight is not loaded sooner: registers, and with them wavefronts
 #pragma unroll
       for (int c = 0; c < C; ++c) {
 #pragma unroll
         for (int i = 0; i < VL; ++i) v[c][i] *= rho;
         if (a.w) {
+          t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
 #pragma unroll
           for (int i = 0; i < VL; ++i) v[c][i] *= w[c][i];
         }
@@ -90,26 +94,22 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
 #pragma unroll
         for (int c = 0; c < C; ++c) t8_store<TYPE>((T *)a.y + row * a.ldy, e0 + c * step, a.K, v[c]);
       }
-      if (!a.q) continue;
+      if (!a.q) return;
     }
-    if constexpr (SOURCE == T8_GATED) {
+    uint32_t deep = 0;                                    // elements (c VL + i) whose gate is far below zero: float64 decides them
+    if constexpr (GATED) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        float g[VL], most = 0.0f, r[VL];
+        float g[VL], least = 0.0f;
         t8_values<TYPE>(second[c], g);
-        if (a.act == QC_ACT_SILU) {
 #pragma unroll
-          for (int i = 0; i < VL; ++i) r[i] = t8_gate_near<QC_ACT_SILU>(g[i], v[c][i], most);
-        } else {
-#pragma unroll
-          for (int i = 0; i < VL; ++i) r[i] = t8_gate_near<QC_ACT_GELU>(g[i], v[c][i], most);
+        for (int i = 0; i < VL; ++i) {
+          v[c][i] = t8_gate<ACT>(g[i], v[c][i]);
+          least = fminf(least, g[i]);
         }
-        if (most > 100.0f) {
+        if (least < T8_DEEP<ACT>) {
 #pragma unroll
-          for (int i = 0; i < VL; ++i) v[c][i] = t8_gate(a.act, g[i], v[c][i]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < VL; ++i) v[c][i] = r[i];
+          for (int i = 0; i < VL; ++i) deep |= g[i] < T8_DEEP<ACT> ? 1u << (c * VL + i) : 0u;
         }
       }
     }
@@ -119,21 +119,22 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
 #pragma unroll
         for (int i = 0; i < VL; ++i) v[c][i] *= w[c][i];
     }
-    unsigned top = 0, tops[C];
+    float tops[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      tops[c] = 0;
+      tops[c] = fabsf(v[c][0]);
 #pragma unroll
-      for (int i = 0; i < VL; ++i) tops[c] = max(tops[c], t8_mag(v[c][i]));
-      top = max(top, tops[c]);
+      for (int i = 1; i < VL; ++i) tops[c] = t8_larger(tops[c], v[c][i]);
     }
+    unsigned top = t8_mag(tops[0]);
+#pragma unroll
+    for (int c = 1; c < C; ++c) top = max(top, t8_mag(tops[c]));
     const auto over_row = [&](unsigned t, int use) {
       t = t8_wave_max(t);
       if constexpr (FULL) {
-        if (lane == 0) across.u[turn][use][wave] = t;
-        __syncthreads();
-        t = across.u[turn][use][0];
-        for (int i = 1; i < waves; ++i) t = max(t, across.u[turn][use][i]);
+        if (lane == 0) across.u[0][use][wave] = t;
+        t8_lds_barrier();
+        t = t8_across_max(across.u[0][use], waves, lane);
       }
       return t;
     };
@@ -167,19 +168,19 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
       }
     } else {
       // elements that float64 or the division decides, as a word of bits (c VL + i), read again; few
-      uint32_t flags = 0;
+      uint32_t flags = deep;
       const auto element = [&](int bit) { return e0 + bit / VL * step + bit % VL; };
       const auto exact = [&](int e) {
         const float g = W4Mem<TYPE>::get(add[e]), f = W4Mem<TYPE>::get(x[e]);
-        return g == 0.0f || f == 0.0f ? 0.0f : (float)t8_gate_exact(a.act, g, f);      // rows of padding are zeros
+        return g == 0.0f || f == 0.0f || g < T8_GONE<ACT> ? 0.0f : (float)t8_gate_exact(ACT, g, f);      // rows of padding are zeros
       };
-      const bool tiny = SOURCE == T8_GATED && __builtin_bit_cast(float, top) < T8_TINY;
-      if constexpr (SOURCE == T8_GATED) {
+      const bool tiny = GATED && __builtin_bit_cast(float, top) < T8_TINY;
+      if constexpr (GATED) {
         if (!lost) {
-          const float near = __builtin_bit_cast(float, top) * (1.0f - 3e-6f);
+          const float near = __builtin_bit_cast(float, top) * (1.0f - 5e-6f);
 #pragma unroll
           for (int c = 0; c < C; ++c)
-            if (__builtin_bit_cast(float, tops[c]) >= near) {
+            if (tops[c] >= near) {
 #pragma unroll
               for (int i = 0; i < VL; ++i) flags |= (tiny ? e0 + c * step + i < width : fabsf(v[c][i]) >= near) ? 1u << (c * VL + i) : 0u;
             }
@@ -191,6 +192,7 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
           }
           top = over_row(top, 1);
         }
+        flags = deep;
       }
       float scale = __builtin_bit_cast(float, top) / 127.0f;
       if (scale == 0.0f) scale = 1.0f;
@@ -206,7 +208,7 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
         for (int i = 0; i < VL; ++i) {
           const float m = __builtin_fmaf(v[c][i], inv, T8_MAGIC), n = m - T8_MAGIC, d = __builtin_fmaf(v[c][i], inv, -n);
           b[i] = __builtin_bit_cast(unsigned, m);
-          if constexpr (SOURCE == T8_GATED) far = fmaxf(far, __builtin_fmaf(fabsf(n), 1.5e-6f, fabsf(d)));
+          if constexpr (GATED) far = fmaxf(far, __builtin_fmaf(fabsf(n), 2.5e-6f, fabsf(d)));
           else far = fmaxf(far, fabsf(d));
         }
         if (none) {
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
 #pragma unroll
           for (int i = 0; i < VL; ++i) {
             const float n = __builtin_fmaf(v[c][i], inv, T8_MAGIC) - T8_MAGIC, d = fabsf(__builtin_fmaf(v[c][i], inv, -n));
-            flags |= (SOURCE == T8_GATED ? __builtin_fmaf(fabsf(n), 1.5e-6f, d) : d) > 0.5f - T8_NEAR ? 1u << (c * VL + i) : 0u;
+            flags |= (GATED ? __builtin_fmaf(fabsf(n), 2.5e-6f, d) : d) > 0.5f - T8_NEAR ? 1u << (c * VL + i) : 0u;
           }
         }
       }
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
         flags &= flags - 1;
         if (e >= width) continue;
         float t;
-        if constexpr (SOURCE == T8_GATED) {
+        if constexpr (GATED) {
           t = exact(e);
         } else if constexpr (SOURCE == T8_NORM) {
           t = 0.0f;
@@ -251,6 +253,7 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
 template <int TYPE, int SOURCE>
 __global__ __launch_bounds__(1024) void t8_long_rows_kernel(T8RowArgs a) {
   using T = typename W4Mem<TYPE>::T;
+  constexpr bool GATED = SOURCE == T8_SILU || SOURCE == T8_GELU;
   __shared__ T8Across across;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int turn = 0;
@@ -272,14 +275,13 @@ __global__ __launch_bounds__(1024) void t8_long_rows_kernel(T8RowArgs a) {
       ss = wave_sum_dpp(ss);
       if (lane == 0) across.d[turn][wave] = ss;
       __syncthreads();
-      ss = across.d[turn][0];
-      for (int i = 1; i < 16; ++i) ss += across.d[turn][i];
+      ss = t8_across_sum(across.d[turn], 16, lane);
       rho = (float)t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
       if (a.add) x = h;                                   // each thread reads what it wrote
     }
     const auto value = [&](int e) {
       float v = W4Mem<TYPE>::get(x[e]);
-      if constexpr (SOURCE == T8_GATED) v = (float)t8_gate_exact(a.act, W4Mem<TYPE>::get(add[e]), v);
+      if constexpr (GATED) v = (float)t8_gate_exact(SOURCE == T8_GELU ? QC_ACT_GELU : QC_ACT_SILU, W4Mem<TYPE>::get(add[e]), v);
       if constexpr (SOURCE == T8_PLANES) v *= a.w[e];
       if constexpr (SOURCE == T8_NORM) {
         v *= rho;
@@ -298,8 +300,7 @@ __global__ __launch_bounds__(1024) void t8_long_rows_kernel(T8RowArgs a) {
     top = t8_wave_max(top);
     if (lane == 0) across.u[turn][0][wave] = top;
     __syncthreads();
-    top = across.u[turn][0][0];
-    for (int i = 1; i < 16; ++i) top = max(top, across.u[turn][0][i]);
+    top = t8_across_max(across.u[turn][0], 16, lane);
     const bool lost = top >= 0x7F800000u;
     if constexpr (SOURCE == T8_PLANES) {
       constexpr int P = t8_planes(TYPE);
@@ -330,21 +331,21 @@ template <int TYPE, int SOURCE>
 static hipError_t rows_launch(const T8RowArgs &a, hipStream_t st) {
   constexpr int VL = t8_vl<TYPE>;
   const int vectors = ((SOURCE == T8_PLANES ? a.pitch : a.K) + VL - 1) / VL;
-  if (vectors > 64 * 16 * 4) {
+  if (vectors > 64 * 16 * 4 || a.K < VL) {
     t8_long_rows_kernel<TYPE, SOURCE><<<(unsigned)std::min(a.M, 1024), 1024, 0, st>>>(a);
     return hipGetLastError();
   }
   int waves = (vectors + 255) / 256;
   while (waves < 16 && vectors > 64 * waves && (int64_t)a.M * waves < 2048) ++waves;
   const int c = (vectors + 64 * waves - 1) / (64 * waves);
+  const int groups = waves == 1 ? (a.M + 3) / 4 : a.M;
+  const dim3 grid((unsigned)std::min(groups, 1 << 20), (unsigned)((groups + (1 << 20) - 1) >> 20));
   if (waves == 1) {
-    const unsigned grid = (unsigned)std::min((a.M + 3) / 4, 1 << 20);
     if (c == 1) t8_rows_kernel<TYPE, SOURCE, false, 1><<<grid, 256, 0, st>>>(a);
     else if (c == 2) t8_rows_kernel<TYPE, SOURCE, false, 2><<<grid, 256, 0, st>>>(a);
     else if (c == 3) t8_rows_kernel<TYPE, SOURCE, false, 3><<<grid, 256, 0, st>>>(a);
     else t8_rows_kernel<TYPE, SOURCE, false, 4><<<grid, 256, 0, st>>>(a);
   } else {
-    const unsigned grid = (unsigned)std::min(a.M, 1 << 20);
     if (c == 1) t8_rows_kernel<TYPE, SOURCE, true, 1><<<grid, 64 * waves, 0, st>>>(a);
     else if (c == 2) t8_rows_kernel<TYPE, SOURCE, true, 2><<<grid, 64 * waves, 0, st>>>(a);
     else if (c == 3) t8_rows_kernel<TYPE, SOURCE, true, 3><<<grid, 64 * waves, 0, st>>>(a);
@@ -356,7 +357,8 @@ static hipError_t rows_launch(const T8RowArgs &a, hipStream_t st) {
 template <int TYPE>
 static hipError_t rows_source(const T8RowArgs &a, int source, hipStream_t st) {
   if (source == T8_PLAIN) return rows_launch<TYPE, T8_PLAIN>(a, st);
-  if (source == T8_GATED) return rows_launch<TYPE, T8_GATED>(a, st);
+  if (source == T8_SILU) return rows_launch<TYPE, T8_SILU>(a, st);
+  if (source == T8_GELU) return rows_launch<TYPE, T8_GELU>(a, st);
   if (source == T8_NORM) return rows_launch<TYPE, T8_NORM>(a, st);
   return rows_launch<TYPE, T8_PLANES>(a, st);
 }
@@ -431,13 +433,44 @@ __global__ __launch_bounds__(256) void t8_gated_grad_kernel(const void *x, int64
   }
 }
 
+// rows that are shorter than a vector
+template <int TYPE>
+__global__ __launch_bounds__(256) void t8_gated_grad_narrow_kernel(const void *x, int64_t ldx, const void *g, int64_t ldg, const void *dv, int64_t lddv, int act,
+                                                                   int64_t M, int K, void *dx, int64_t lddx, void *dg, int64_t lddg) {
+  using T = typename W4Mem<TYPE>::T;
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, row = t / K, e = t % K;
+  if (row >= M) return;
+  const float xv = W4Mem<TYPE>::get(((const T *)x)[row * ldx + e]), gv = W4Mem<TYPE>::get(((const T *)g)[row * ldg + e]),
+              d = W4Mem<TYPE>::get(((const T *)dv)[row * lddv + e]);
+  float slope;
+  const float rx = d * t8_act(act, gv, slope);
+  ((T *)dx)[row * lddx + e] = W4Mem<TYPE>::put(rx);
+  ((T *)dg)[row * lddg + e] = W4Mem<TYPE>::put(d * xv * slope);
+}
+
+template <int TYPE>
+static void gated_grad(const void *x, int64_t ldx, const void *g, int64_t ldg, int act, const void *dv, int64_t lddv, int64_t M, int64_t K, void *dx, int64_t lddx,
+                       void *dg, int64_t lddg, hipStream_t st) {
+  constexpr int VL = t8_vl<TYPE>;
+  // rows without anything between them are one row (of 32-bit numbers of elements)
+  if (M > 1 && ldx == K && ldg == K && lddv == K && lddx == K && lddg == K && M * K < (1ll << 31) - 4096) {
+    K *= M;
+    M = 1;
+  }
+  if (K < VL) {
+    t8_gated_grad_narrow_kernel<TYPE><<<(unsigned)((M * K + 255) / 256), 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, act, M, (int)K, dx, lddx, dg, lddg);
+    return;
+  }
+  const int vectors = (int)((K + VL - 1) / VL), rows = std::max(1, 512 / vectors);
+  const dim3 grid((unsigned)((M + rows - 1) / rows), (unsigned)std::max(1, std::min(M == 1 ? 8192 : 32, vectors / 512)));
+  t8_gated_grad_kernel<TYPE><<<grid, 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, act, M, (int)K, dx, lddx, dg, lddg, rows, vectors);
+}
+
 hipError_t launch_t8_gated_grad(const void *x, int64_t ldx, const void *g, int64_t ldg, int act, const void *dv, int64_t lddv, int type, int M, int K, void *dx,
                                 int64_t lddx, void *dg, int64_t lddg, hipStream_t st) {
-  const int vl = type == QC_TYPE_F32 ? 4 : 8, vectors = (K + vl - 1) / vl, rows = std::max(1, 512 / vectors);
-  const dim3 grid((unsigned)((M + rows - 1) / rows), (unsigned)std::max(1, std::min(32, vectors / 512)));
-  if (type == QC_TYPE_F32) t8_gated_grad_kernel<QC_TYPE_F32><<<grid, 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, act, M, K, dx, lddx, dg, lddg, rows, vectors);
-  else if (type == QC_TYPE_F16) t8_gated_grad_kernel<QC_TYPE_F16><<<grid, 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, act, M, K, dx, lddx, dg, lddg, rows, vectors);
-  else t8_gated_grad_kernel<QC_TYPE_BF16><<<grid, 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, act, M, K, dx, lddx, dg, lddg, rows, vectors);
+  if (type == QC_TYPE_F32) gated_grad<QC_TYPE_F32>(x, ldx, g, ldg, act, dv, lddv, M, K, dx, lddx, dg, lddg, st);
+  else if (type == QC_TYPE_F16) gated_grad<QC_TYPE_F16>(x, ldx, g, ldg, act, dv, lddv, M, K, dx, lddx, dg, lddg, st);
+  else gated_grad<QC_TYPE_BF16>(x, ldx, g, ldg, act, dv, lddv, M, K, dx, lddx, dg, lddg, st);
   return hipGetLastError();
 }
 

@@ -462,7 +462,7 @@ struct TileCost {
   int rows, cols, slots;
   float slab, ends, slab_rest, ends_rest;                  // all slots taken; half of them or fewer
 };
-constexpr TileCost LARGE = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL = {128, 128, 512, 0.93f, 3.2f, 0.6f, 2.5f};
+constexpr TileCost LARGE = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL = {128, 128, 512, 0.93f, 3.2f, 0.72f, 2.5f};
 
 static float tile_time(const TileCost &c, int64_t rows, int cols, int slabs) {
   const int64_t tiles = ((rows + c.rows - 1) / c.rows) * ((cols + c.cols - 1) / c.cols), rest = tiles % c.slots;
@@ -470,6 +470,12 @@ static float tile_time(const TileCost &c, int64_t rows, int cols, int slabs) {
   return (float)(tiles / c.slots) * full + last;
 }
 static bool large_tiles(int64_t rows, int cols, int slabs) { return tile_time(LARGE, rows, cols, slabs) < tile_time(SMALL, rows, cols, slabs); }
+
+float t8_tile_time(int M, int N, int K) {
+  const int slabs = (K + T8_BK - 1) / T8_BK;
+  // weights that nothing else shares come at 3.7 TB/s (1 x 28672 x 8192: 63 us)
+  return std::max(std::min(tile_time(LARGE, M, N, slabs), tile_time(SMALL, M, N, slabs)), (float)N * (float)K / 3.7e6f);
+}
 
 template <int TYPE, int P, bool PART>
 static hipError_t tile_of(const T8Product &a, hipStream_t st) {

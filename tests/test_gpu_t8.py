@@ -78,7 +78,7 @@ def _same_codes(q, scale, v, what):
 
 
 # rows, width: one element, one row, odd everything, a vector and a bit, several rows a wavefront, wide rows, rows that are read again
-SHAPES = [(1, 1), (1, 8192), (3, 7), (5, 64), (2, 1153), (77, 1152), (9, 3081), (515, 40), (130, 513), (6000, 72), (17000, 33), (1500, 1153), (2100, 700), (1030, 4608), (2000, 9001), (3, 16384),
+SHAPES = [(1, 1), (1, 8192), (3, 7), (40, 3), (6, 8), (7, 9), (5, 64), (2, 1153), (77, 1152), (9, 3081), (515, 40), (130, 513), (6000, 72), (17000, 33), (1500, 1153), (2100, 700), (1030, 4608), (2000, 9001), (3, 16384),
           (2, 16390), (1, 40000), (2, 131071)]
 
 
