@@ -7,9 +7,9 @@
 
 namespace qc {
 
-// `waves` wavefronts a row, as many rows a workgroup as make 16 of them; they walk in step.  C: vectors a lane.
+// `waves` wavefronts a row, as many rows a workgroup as make 8 of them; they walk in step (one wavefront a row: by themselves).  C: vectors a lane.
 template <int TYPE, int C>
-__global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
+__global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8NormGradArgs a) {
   using T = typename W4Mem<TYPE>::T;
   constexpr int VL = t8_vl<TYPE>;
   __shared__ double red[2][2][16];                          // alternating, as in t8_rows.hip
@@ -18,13 +18,14 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
   const int waves = a.waves, rows = ((int)blockDim.x >> 6) / waves, sub = wave / waves, first = sub * waves;
   const int step = 64 * waves * VL, e0 = ((wave - first) * 64 + lane) * VL;
   float dw[C][VL] = {};
-  constexpr bool AHEAD = C < 4;                             // the next row is on its way while this one is at work (registers)
-  w4_u4 nh[C], ng[C];
+  constexpr bool AHEAD = C <= 2, ALL = C * VL <= 8;        // the next row (ALL: and its dh) is on its way while this one is at work: registers
+  w4_u4 nh[C], ng[C], nd[C];
   const auto fetch = [&](int64_t row, int K) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       nh[c] = t8_raw<TYPE>((const T *)a.h + row * a.ldh, e0 + c * step, K);
       ng[c] = t8_raw<TYPE>((const T *)a.dy + row * a.lddy, e0 + c * step, K);
+      if (ALL && a.dh) nd[c] = t8_raw<TYPE>((const T *)a.dh + row * a.lddh, e0 + c * step, K);
     }
   };
   int64_t row = (int64_t)blockIdx.x * rows + sub;
@@ -41,8 +42,9 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
     for (int c = 0; c < C; ++c) {
       ch[c] = nh[c];
       cg[c] = ng[c];
+      if (ALL) cd[c] = nd[c];
     }
-    if (a.dh && there) {
+    if (!ALL && a.dh && there) {
 #pragma unroll
       for (int c = 0; c < C; ++c) cd[c] = t8_raw<TYPE>((const T *)a.dh + row * a.lddh, e0 + c * step, K);
     }
@@ -105,6 +107,14 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_kernel(T8NormGradArgs a) {
   if (!a.dw) return;
   float *part = a.part + (size_t)blockIdx.x * a.K;
   const int width = step * C;
+  if (rows == 1) {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < VL; ++i)
+        if (e0 + c * step + i < a.K) part[e0 + c * step + i] = dw[c][i];
+    return;
+  }
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -175,16 +185,17 @@ __global__ __launch_bounds__(1024) void t8_weight_grad_kernel(const float *part,
 struct NormGradShape {
   int waves, rows, c, groups;      // waves 0: the kernel of long rows
 };
-constexpr int NORM_GRAD_GROUPS = 256;
+constexpr int NORM_GRAD_GROUPS = 512;
 static NormGradShape norm_grad_shape(int M, int K, int type) {
-  const int vl = type == QC_TYPE_F32 ? 4 : 8, most = type == QC_TYPE_F32 ? 4 : 2, vectors = (K + vl - 1) / vl;      // most: vectors a lane
+  const int vl = type == QC_TYPE_F32 ? 4 : 8, vectors = (K + vl - 1) / vl;
   NormGradShape s{};
   s.groups = std::min(M, NORM_GRAD_GROUPS);
-  if (vectors > 64 * 16 * most || K < vl) return s;
-  s.waves = std::min((vectors + 127) / 128, 16);
-  while (s.waves < 16 && vectors > 64 * s.waves && (int64_t)M * s.waves < 1024) ++s.waves;
+  if (vectors > 64 * 8 * 4 || K < vl) return s;
+  s.waves = std::min((vectors + 64 * (16 / vl) - 1) / (64 * (16 / vl)), 8);
+  while (s.waves < 8 && vectors > 64 * s.waves && (int64_t)M * s.waves < 2048) ++s.waves;
   s.c = (vectors + 64 * s.waves - 1) / (64 * s.waves);
-  s.rows = 16 / s.waves;
+  s.c = s.c > 2 ? 4 : s.c;
+  s.rows = 8 / s.waves;
   // workgroups for every compute unit come before rows that share one
   while (s.rows > 1 && (M + s.rows - 1) / s.rows < NORM_GRAD_GROUPS) --s.rows;
   s.groups = std::min((M + s.rows - 1) / s.rows, NORM_GRAD_GROUPS);
@@ -199,17 +210,18 @@ static hipError_t norm_grad_launch(T8NormGradArgs a, hipStream_t st) {
   a.groups = s.groups;
   a.waves = s.waves;
   if (a.M > 0) {
-    const int threads = 64 * s.waves * s.rows, lds = threads * (s.c == 3 ? 4 : s.c) * t8_vl<TYPE> * 4;      // (the kernel's C; 64 KB at most)
-    if (s.waves == 0) t8_norm_grad_long_kernel<TYPE><<<s.groups, 1024, 0, st>>>(a);
-    else {
-      constexpr int MOST = TYPE == QC_TYPE_F32 ? 4 : 2;
-      const auto kern = s.c == 1 ? t8_norm_grad_kernel<TYPE, 1> : s.c == 2 ? t8_norm_grad_kernel<TYPE, 2> : t8_norm_grad_kernel<TYPE, MOST>;
+    const int threads = 64 * s.waves * s.rows, lds = a.dw && s.rows > 1 ? threads * s.c * t8_vl<TYPE> * 4 : 0;      // 64 KB at most
+    if (s.waves == 0) {
+      t8_norm_grad_long_kernel<TYPE><<<s.groups, 1024, 0, st>>>(a);
+    } else {
+      const int at = s.c / 2;
+      constexpr void (*kernels[3])(T8NormGradArgs) = {t8_norm_grad_kernel<TYPE, 1>, t8_norm_grad_kernel<TYPE, 2>, t8_norm_grad_kernel<TYPE, 4>};
       static std::atomic<unsigned long long> done[3];
       if (lds > 65536 - 1024) {
-        const hipError_t e = allow_lds((const void *)kern, 65536, done[std::min(s.c, 3) - 1]);
+        const hipError_t e = allow_lds((const void *)kernels[at], 131072, done[at]);
         if (e != hipSuccess) return e;
       }
-      kern<<<s.groups, threads, lds, st>>>(a);
+      kernels[at]<<<s.groups, threads, lds, st>>>(a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
