@@ -413,19 +413,30 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
   }
 }
 
-// Parts of the planes' sums to the gradient: four columns of a row a thread
-template <int TYPE>
+// Parts of the planes' sums to the gradient: four columns of a row a thread, or 16 threads where there are many parts
+template <int TYPE, int Z>
 __global__ __launch_bounds__(256) void t8_join_kernel(T8Product a) {
-  constexpr int P = t8_planes(TYPE);
+  constexpr int P = t8_planes(TYPE), ITEMS = 256 / Z;
   using T = typename W4Mem<TYPE>::T;
-  const int quads = a.K / 4;
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t >= (int64_t)a.M * quads) return;
-  const int m = (int)(t / quads), k = (int)(t % quads) * 4;
+  const int quads = a.K / 4, item = threadIdx.x % ITEMS, first = threadIdx.x / ITEMS;
+  const int64_t t = (int64_t)blockIdx.x * ITEMS + item;
+  const bool there = t < (int64_t)a.M * quads;
+  const int m = there ? (int)(t / quads) : 0, k = there ? (int)(t % quads) * 4 : 0;
   t8_i4 s[P] = {};
-  for (int z = 0; z < a.split; ++z)
+  for (int z = first; z < a.split; z += Z)
 #pragma unroll
     for (int p = 0; p < P; ++p) s[p] += *(const t8_i4 *)(a.part + ((int64_t)z * a.arows + t8_plane_row(m, p, P)) * a.K + k);
+  if constexpr (Z > 1) {
+    __shared__ t8_i4 red[Z][P][ITEMS];
+#pragma unroll
+    for (int p = 0; p < P; ++p) red[first][p][item] = s[p];
+    __syncthreads();
+    if (first) return;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      for (int z = 1; z < Z; ++z) s[p] += red[z][p][item];
+  }
+  if (!there) return;
   const float scale = a.xs[m];
   T *to = (T *)a.y + (int64_t)m * a.ldy + k;
 #pragma unroll
@@ -442,8 +453,10 @@ static hipError_t tile_launch(T8Product a, hipStream_t st) {
   using S = T8Tile<WM, WN, MI, NI>;
   a.tm = (a.arows + S::TM - 1) / S::TM;
   a.tn = ((P ? a.K : a.N) + S::TN - 1) / S::TN;
-  // results that outgrow the L2 caches stream past them (16384 x 4608 x 1152 bfloat16, 151 MB: 103 -> 97 us; 4096 rows, 38 MB: 32.7 -> 28.7)
-  a.stream = (int64_t)a.M * a.N * (TYPE == QC_TYPE_F32 ? 4 : 2) > (32 << 20);
+  // results of whole lines that outgrow the L2 caches stream past them (16384 x 4608 x 1152 bfloat16, 151 MB: 103 -> 97 us; 4096 rows, 38 MB: 32.7 ->
+  // 28.7); pieces of lines meet there
+  constexpr int ES = TYPE == QC_TYPE_F32 ? 4 : 2;
+  a.stream = (int64_t)a.M * a.N * ES > (32 << 20) && a.ldy * ES % 128 == 0 && (uintptr_t)a.y % 128 == 0;
   static std::atomic<unsigned long long> done;
   const auto kern = t8_tile_kernel<TYPE, P, PART, WM, WN, MI, NI>;
   if (S::LDS > 65536) {
@@ -477,49 +490,80 @@ float t8_tile_time(int M, int N, int K) {
   return std::max(std::min(tile_time(LARGE, M, N, slabs), tile_time(SMALL, M, N, slabs)), (float)N * (float)K / 3.7e6f);
 }
 
-template <int TYPE, int P, bool PART>
+template <int TYPE, int P>
 static hipError_t tile_of(const T8Product &a, hipStream_t st) {
-  if (!PART && large_tiles(a.arows, P ? a.K : a.N, ((P ? a.N : a.K) + T8_BK - 1) / T8_BK)) return tile_launch<TYPE, P, false, 2, 4, 8, 4>(a, st);
-  return tile_launch<TYPE, P, PART, 2, 2, 4, 4>(a, st);
+  if (large_tiles(a.arows, P ? a.K : a.N, ((P ? a.N : a.K) + T8_BK - 1) / T8_BK)) return tile_launch<TYPE, P, false, 2, 4, 8, 4>(a, st);
+  return tile_launch<TYPE, P, false, 2, 2, 4, 4>(a, st);
 }
 
 hipError_t launch_t8_tile(const T8Product &a, int type, hipStream_t st) {
-  if (type == QC_TYPE_F32) return tile_of<QC_TYPE_F32, 0, false>(a, st);
-  if (type == QC_TYPE_F16) return tile_of<QC_TYPE_F16, 0, false>(a, st);
-  return tile_of<QC_TYPE_BF16, 0, false>(a, st);
+  if (type == QC_TYPE_F32) return tile_of<QC_TYPE_F32, 0>(a, st);
+  if (type == QC_TYPE_F16) return tile_of<QC_TYPE_F16, 0>(a, st);
+  return tile_of<QC_TYPE_BF16, 0>(a, st);
 }
 
-// ---- the gradient: launches of fewer tiles than fill the chip split the summed axis
-struct GradShape {
-  int arows, split, per;
+// ---- The gradient: whole rounds of tiles first; the rows of what is left, or of a launch that makes no round, split the summed axis into parts
+// whose sums a second kernel joins, where that is sooner.
+struct GradPlan {
+  int arows, whole;          // rows of planes, and of them those that are not split
+  int split, per;            // parts, slabs of each
 };
-static GradShape grad_shape(int M, int N, int K, int type) {
-  GradShape s;
+static GradPlan grad_plan(int M, int N, int K, int type) {
   const int P = t8_planes(type), slabs = (N + T8_BK - 1) / T8_BK;
-  s.arows = (M + 15) / 16 * 16 * P;
-  const int64_t tiles = (int64_t)((s.arows + 127) / 128) * ((K + 127) / 128);
-  const int split = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, slabs / 2));
-  s.per = (slabs + split - 1) / split;
-  s.split = (slabs + s.per - 1) / s.per;
-  return s;
+  GradPlan best{(M + 15) / 16 * 16 * P, 0, 1, slabs};
+  best.whole = best.arows;
+  float time = std::min(tile_time(LARGE, best.arows, K, slabs), tile_time(SMALL, best.arows, K, slabs));
+  for (const TileCost &c : {LARGE, SMALL}) {
+    const int64_t tn = (K + c.cols - 1) / c.cols, tiles = (best.arows + c.rows - 1) / c.rows * tn;
+    const int whole = (int)(tiles / c.slots * c.slots / tn * c.rows), rest = best.arows - whole;
+    const int64_t left = (int64_t)((rest + SMALL.rows - 1) / SMALL.rows) * ((K + SMALL.cols - 1) / SMALL.cols);
+    if (left == 0 || left > SMALL.slots / 2) continue;
+    int split = (int)std::min<int64_t>(SMALL.slots / left, std::max(1, slabs / 2));
+    const int per = (slabs + split - 1) / split;
+    split = (slabs + per - 1) / per;
+    // a launch more, or two, and the sums' way to memory and back (8192 x 1152 from 4608, bfloat16: the last 117 tiles in four parts 27 us and 7
+    // for the join, no sooner than a round of them)
+    const float t = tile_time(c, whole, K, slabs) + SMALL.slab * per + SMALL.ends + 6.0f + (float)(left * split) * 65536.0f * 2.0f / 4e6f;
+    if (split > 1 && t < time) {
+      time = t;
+      best.whole = whole;
+      best.split = split;
+      best.per = per;
+    }
+  }
+  return best;
 }
 
 int64_t t8_grad_part_bytes(int M, int N, int K, int type) {
-  const GradShape s = grad_shape(M, N, K, type);
-  return s.split > 1 ? (int64_t)s.split * s.arows * K * 4 : 0;
+  const GradPlan p = grad_plan(M, N, K, type);
+  return p.split > 1 ? (int64_t)p.split * (p.arows - p.whole) * K * 4 : 0;
 }
 
 template <int TYPE>
 static hipError_t grad_launch(T8Product a, hipStream_t st) {
   constexpr int P = t8_planes(TYPE);
-  const GradShape s = grad_shape(a.M, a.N, a.K, TYPE);
-  a.arows = s.arows;
-  a.split = s.split;
-  a.per = s.per;
-  if (s.split == 1) return tile_of<TYPE, P, false>(a, st);
-  const hipError_t e = tile_of<TYPE, P, true>(a, st);
+  const GradPlan p = grad_plan(a.M, a.N, a.K, TYPE);
+  const int rows = p.whole / P;                            // of the result (a multiple of 16, or all)
+  a.arows = p.whole;
+  if (p.split == 1) return tile_of<TYPE, P>(a, st);
+  if (p.whole) {
+    T8Product w = a;
+    w.M = rows;
+    const hipError_t e = tile_of<TYPE, P>(w, st);
+    if (e != hipSuccess) return e;
+  }
+  a.arows = p.arows - p.whole;
+  a.split = p.split;
+  a.per = p.per;
+  a.M -= rows;
+  a.a += (int64_t)p.whole * a.lda;
+  a.xs += rows;
+  a.y = (typename W4Mem<TYPE>::T *)a.y + (int64_t)rows * a.ldy;
+  const hipError_t e = tile_launch<TYPE, P, true, 2, 2, 4, 4>(a, st);
   if (e != hipSuccess) return e;
-  t8_join_kernel<TYPE><<<(unsigned)(((int64_t)a.M * (a.K / 4) + 255) / 256), 256, 0, st>>>(a);
+  const int64_t items = (int64_t)a.M * (a.K / 4);
+  if (a.split > 8) t8_join_kernel<TYPE, 16><<<(unsigned)((items + 15) / 16), 256, 0, st>>>(a);
+  else t8_join_kernel<TYPE, 1><<<(unsigned)((items + 255) / 256), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
