@@ -35,7 +35,7 @@
  * those start at multiples of 16 bytes (QC_ERR_ALIGN), and K % 16 == 0 there.
  * Vectors (scales, weights of norms, biases) are float32.
  * Limits: M below 2^24, N and K from 1 (N from 0) and below 2^17, leading
- * dimensions below 2^22, M times the padded columns of a workspace below 2^40.
+ * dimensions below 2^22.
  * M = 0 and N = 0 are valid: nothing is written but the gradients of a sum
  * without terms, which are zero.
  */
@@ -101,8 +101,8 @@ int qc_t8_linear(const int8_t *qx, int64_t ldx, const float *x_scale, const int8
  *   dx[m, k] = sum_n dy[m, n] w_scale[n] qw[n, k]
  * The scales vary along the summed axis, so that dy w_scale enters the product: as a fixed-point number of 16 bits (float16,
  * bfloat16) or 32 bits (float32) of the row's largest |dy w_scale|, whose bytes meet the weights' in exact integer sums.  The
- * rounding of one term is thus at most 2^-16 (2^-32) of the largest in its row.  A row of dy w_scale that is not finite gives
- * NaN; |dy w_scale| below 2^-100 may be taken for 0.
+ * rounding of one term is thus at most 1 / 65024 (2^-31.9) of the largest in its row, whatever its own size.  A row of
+ * dy w_scale that is not finite gives NaN; one with nothing of 2^-100 or above may be taken for zeros.
  * dy: dev [M, N] of `type`; qw: as above; dx: dev [M, K] of `type`.  work: dev, at least qc_t8_linear_grad_bytes, 256-byte
  * aligned. */
 int qc_t8_linear_grad_bytes(int M, int N, int K, int type, size_t *bytes_out);

@@ -452,8 +452,8 @@ template <int TYPE>
 static void gated_grad(const void *x, int64_t ldx, const void *g, int64_t ldg, int act, const void *dv, int64_t lddv, int64_t M, int64_t K, void *dx, int64_t lddx,
                        void *dg, int64_t lddg, hipStream_t st) {
   constexpr int VL = t8_vl<TYPE>;
-  // rows without anything between them are one row (of 32-bit numbers of elements)
-  if (M > 1 && ldx == K && ldg == K && lddv == K && lddx == K && lddg == K && M * K < (1ll << 31) - 4096) {
+  // rows without anything between them are one row (of 32-bit offsets)
+  if (M > 1 && ldx == K && ldg == K && lddv == K && lddx == K && lddg == K && M * K < (1ll << 30) - 4096) {
     K *= M;
     M = 1;
   }
