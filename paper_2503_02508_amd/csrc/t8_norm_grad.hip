@@ -13,10 +13,30 @@ __global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8Nor
   using T = typename W4Mem<TYPE>::T;
   constexpr int VL = t8_vl<TYPE>;
   __shared__ double red[2][2][16];                          // alternating, as in t8_rows.hip
-  extern __shared__ float join[];                           // [rows of a workgroup, width]
+  extern __shared__ __align__(16) float own[];              // [rows of a workgroup, width]: each thread's weights, in the end its dweight
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = a.waves, rows = ((int)blockDim.x >> 6) / waves, sub = wave / waves, first = sub * waves;
   const int step = 64 * waves * VL, e0 = ((wave - first) * 64 + lane) * VL;
+  const int width = step * C;
+  float *mine = own + sub * width + e0;
+  // (from memory, twice a row, the weight would be as many bytes of the L2 caches as the rows are of memory)
+  if (a.w) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float w[VL];
+      t8_load_f32<VL>(a.w, e0 + c * step, a.K, w);
+#pragma unroll
+      for (int i = 0; i < VL; ++i) mine[c * step + i] = w[i];
+    }
+  }
+  const auto weight = [&](int c, float (&w)[VL]) {
+#pragma unroll
+    for (int i = 0; i < VL; i += 4) {
+      const w4_f4 r = *(const w4_f4 *)(mine + c * step + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[i + j] = r[j];
+    }
+  };
   float dw[C][VL] = {};
   constexpr bool AHEAD = C <= 2, ALL = C * VL <= 8;        // the next row (ALL: and its dh) is on its way while this one is at work: registers
   w4_u4 nh[C], ng[C], nd[C];
@@ -58,7 +78,7 @@ __global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8Nor
         t8_values<TYPE>(ch[c], h);
         t8_values<TYPE>(cg[c], g);
         if (a.w) {
-          t8_load_f32<VL>(a.w, e0 + c * step, K, w);
+          weight(c, w);
 #pragma unroll
           for (int i = 0; i < VL; ++i) g[i] *= w[i];
         }
@@ -88,7 +108,7 @@ __global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8Nor
       float h[VL], g[VL], w[VL], d[VL];
       t8_values<TYPE>(ch[c], h);
       t8_values<TYPE>(cg[c], g);
-      if (a.w) t8_load_f32<VL>(a.w, e0 + c * step, K, w);
+      if (a.w) weight(c, w);
 #pragma unroll
       for (int i = 0; i < VL; ++i) {
         dw[c][i] = __builtin_fmaf(g[i], h[i] * rho, dw[c][i]);
@@ -106,7 +126,6 @@ __global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8Nor
   }
   if (!a.dw) return;
   float *part = a.part + (size_t)blockIdx.x * a.K;
-  const int width = step * C;
   if (rows == 1) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -118,11 +137,11 @@ __global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8Nor
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int i = 0; i < VL; ++i) join[sub * width + e0 + c * step + i] = dw[c][i];
+    for (int i = 0; i < VL; ++i) mine[c * step + i] = dw[c][i];
   __syncthreads();
   for (int e = threadIdx.x; e < a.K; e += blockDim.x) {
-    float t = join[e];
-    for (int i = 1; i < rows; ++i) t += join[i * width + e];
+    float t = own[e];
+    for (int i = 1; i < rows; ++i) t += own[i * width + e];
     part[e] = t;
   }
 }
@@ -197,7 +216,7 @@ static NormGradShape norm_grad_shape(int M, int K, int type) {
   s.c = s.c > 2 ? 4 : s.c;
   s.rows = 8 / s.waves;
   // workgroups for every compute unit come before rows that share one
-  while (s.rows > 1 && (M + s.rows - 1) / s.rows < NORM_GRAD_GROUPS) --s.rows;
+  while (s.rows > 1 && (M + s.rows - 1) / s.rows < 256) --s.rows;
   s.groups = std::min((M + s.rows - 1) / s.rows, NORM_GRAD_GROUPS);
   return s;
 }
@@ -210,7 +229,7 @@ static hipError_t norm_grad_launch(T8NormGradArgs a, hipStream_t st) {
   a.groups = s.groups;
   a.waves = s.waves;
   if (a.M > 0) {
-    const int threads = 64 * s.waves * s.rows, lds = a.dw && s.rows > 1 ? threads * s.c * t8_vl<TYPE> * 4 : 0;      // 64 KB at most
+    const int threads = 64 * s.waves * s.rows, lds = threads * s.c * t8_vl<TYPE> * 4;      // 64 KB at most
     if (s.waves == 0) {
       t8_norm_grad_long_kernel<TYPE><<<s.groups, 1024, 0, st>>>(a);
     } else {
