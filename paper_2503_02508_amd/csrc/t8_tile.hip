@@ -1,7 +1,7 @@
 // Products of the 8-bit layers with a scale for each token, many rows: y = x W^T and, on the byte planes of gradients, dx = dy W.
 //
 // Slabs of 128 bytes of the summed axis (whole cache lines: slabs of 64 made 4096 x 8192 x 8192 a quarter slower) go from memory straight to one of
-// two places in LDS.  Wavefronts read 16 x 64 operands of v_mfma_i32_16x16x64_i8 from there half a slab ahead into registers: behind a
+// two or three places in LDS.  Wavefronts read 16 x 64 operands of v_mfma_i32_16x16x64_i8 from there half a slab ahead into registers: behind a
 // slab's barrier its products start at once, the next operands come in under them, and the place of the slab that was read is filled again.
 // The weights' rows run along the summed axis in the forward product; in the gradient they run across it, and ds_read_b64_tr_b8 turns 8 rows x
 // 16 bytes on their way to the registers.
@@ -15,12 +15,12 @@
 
 namespace qc {
 
-constexpr int T8_BK = 128, T8_ST = 2;
+constexpr int T8_BK = 128;
 
-template <int WM, int WN, int MI, int NI>
+template <int ST, int WM, int WN, int MI, int NI>
 struct T8Tile {
   static constexpr int W = WM * WN, TM = WM * MI * 16, TN = WN * NI * 16;
-  static constexpr int ABYTES = TM * T8_BK, BBYTES = TN * T8_BK, STAGE = ABYTES + BBYTES, RING = T8_ST * STAGE;
+  static constexpr int ABYTES = TM * T8_BK, BBYTES = TN * T8_BK, STAGE = ABYTES + BBYTES, RING = ST * STAGE;
   static constexpr int SCALES = (TM + 2 * TN) * 4, LDS = RING + 2 * SCALES;              // of two tiles: scales of rows and columns, biases
   static constexpr int LA = ABYTES / 1024 / W, LB = BBYTES / 1024 / W, L = LA + LB;      // loads of a wavefront
   static constexpr int PER_CU = 160 * 1024 / LDS < 2 ? 1 : 2;
@@ -107,10 +107,11 @@ __device__ __forceinline__ void t8_rows_out(const w4_f4 v[NI], int lane, typenam
 }
 
 // P: 0 the forward product, else planes of a gradient.  PART: sums to the workspace.
-template <int TYPE, int P, bool PART, int WM, int WN, int MI, int NI>
+template <int TYPE, int P, bool PART, int ST, int WM, int WN, int MI, int NI>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_kernel(T8Product a) {
-  using S = T8Tile<WM, WN, MI, NI>;
-  constexpr int W = S::W, TM = S::TM, TN = S::TN, BK = T8_BK, ST = T8_ST, L = S::L;
+  using S = T8Tile<ST, WM, WN, MI, NI>;
+  constexpr int W = S::W, TM = S::TM, TN = S::TN, BK = T8_BK, L = S::L;
+  static_assert(ST == 2 || ST == 3, "waits for the next of two or three slabs");
   constexpr bool GRAD = P > 0;
   constexpr int CB = TN / 16, RB = 1024 / TN;              // gradient: chunks of a row of weights, rows of a load
   static_assert(P == 0 || MI % P == 0, "whole blocks of planes");
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
   unsigned ao[S::LA], bo[S::LB];
   const int8_t *abase, *bbase;
   Walk fw = begin();                                       // tile, slab and place of the next load
-  int fs = 0, fstage = 0;
+  int fs = 0, fstage = 0, flying = 0;                      // and how many slabs have been asked for and not read
   At fat = at(fw);
   const auto aim = [&]() {
 #pragma unroll
@@ -212,6 +213,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
       }
     }
     fstage = fstage == ST - 1 ? 0 : fstage + 1;
+    ++flying;
     if (++fs == fat.ns) {
       fs = 0;
       advance(fw);
@@ -374,11 +376,16 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
     }
   };
   clear();
-  fetch();
-  const bool two = fw.left > 0;                            // a second slab, of this tile or another
-  fetch();
-  if (two) t8_wait_barrier<L>();
-  else t8_wait_barrier<0>();
+#pragma unroll
+  for (int i = 0; i < ST; ++i) fetch();
+  // the next slab, all loads but those of the slabs behind it (others that come in between make the wait longer)
+  const auto arrive = [&]() {
+    if (ST > 2 && flying >= 3) t8_wait_barrier<2 * (ST > 2) * L>();
+    else if (flying >= 2) t8_wait_barrier<L>();
+    else t8_wait_barrier<0>();
+    --flying;
+  };
+  arrive();
   if (ragged && cat.ns == 1) blank(0);
   read_w(bf[0], 0, 0);
 #pragma unroll
@@ -397,9 +404,10 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
     }
     const bool more = cw.left > 0;
     // the next slab is there, and this one's operands are in registers
-    t8_wait_barrier<0>();
+    if (ends) t8_wait_barrier<0>(), --flying;              // and the tile's scales
+    else arrive();
     fetch();
-    stage ^= 1;
+    stage = stage == ST - 1 ? 0 : stage + 1;
     if (ragged && more && cs + 1 == cat.ns) blank(stage);
     half(bf[1], bf[0], stage, 0);                          // (behind the last slab: some operands that nothing uses)
     if (ends) {                                            // the epilogue takes the operands' registers: they are read again
@@ -448,9 +456,9 @@ __global__ __launch_bounds__(256) void t8_join_kernel(T8Product a) {
   }
 }
 
-template <int TYPE, int P, bool PART, int WM, int WN, int MI, int NI>
+template <int TYPE, int P, bool PART, int ST, int WM, int WN, int MI, int NI>
 static hipError_t tile_launch(T8Product a, hipStream_t st) {
-  using S = T8Tile<WM, WN, MI, NI>;
+  using S = T8Tile<ST, WM, WN, MI, NI>;
   a.tm = (a.arows + S::TM - 1) / S::TM;
   a.tn = ((P ? a.K : a.N) + S::TN - 1) / S::TN;
   // results of whole lines that outgrow the L2 caches stream past them (16384 x 4608 x 1152 bfloat16, 151 MB: 103 -> 97 us; 4096 rows, 38 MB: 32.7 ->
@@ -458,7 +466,7 @@ static hipError_t tile_launch(T8Product a, hipStream_t st) {
   constexpr int ES = TYPE == QC_TYPE_F32 ? 4 : 2;
   a.stream = (int64_t)a.M * a.N * ES > (32 << 20) && a.ldy * ES % 128 == 0 && (uintptr_t)a.y % 128 == 0;
   static std::atomic<unsigned long long> done;
-  const auto kern = t8_tile_kernel<TYPE, P, PART, WM, WN, MI, NI>;
+  const auto kern = t8_tile_kernel<TYPE, P, PART, ST, WM, WN, MI, NI>;
   if (S::LDS > 65536) {
     const hipError_t e = allow_lds((const void *)kern, S::LDS, done);
     if (e != hipSuccess) return e;
@@ -469,31 +477,49 @@ static hipError_t tile_launch(T8Product a, hipStream_t st) {
 }
 
 // ---- Tiles: 256 x 256 by eight wavefronts, one workgroup a compute unit, or 128 x 128 by four, two.  The large one reads LDS half as often for a
-// product, the small one leaves fewer compute units without a tile.  us of a slab and of a tile's ends, by how much of the chip is taken
-// (measured at 16384 x 4608 x 128 - 4608, 16384 x 1152 x 4608 and 4096 x 8192 x 8192):
+// product, the small one leaves fewer compute units without a tile.  Where there is no tile for each compute unit, so that nothing works beside a
+// workgroup while it waits for memory, 128 x 128 by eight with three slabs on their way (2048 x 1152 x 4608: 24.5 us, by four with two 26.7; 512 x 8192 x 8192
+// 43.6 / 59; with more tiles than compute units it loses: 4096 x 4608 x 1152 33.7 / 28.2).  us of a slab and of a tile's ends, by how much of the
+// chip is taken (measured at 16384 x 4608 x 128 - 4608, 16384 x 1152 x 4608 and 4096 x 8192 x 8192, and for the third form at those above):
 struct TileCost {
   int rows, cols, slots;
   float slab, ends, slab_rest, ends_rest;                  // all slots taken; half of them or fewer
 };
-constexpr TileCost LARGE = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL = {128, 128, 512, 0.93f, 3.2f, 0.72f, 2.5f};
+constexpr TileCost LARGE = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL = {128, 128, 512, 0.93f, 3.2f, 0.72f, 2.5f},
+                   LONE = {128, 128, 256, 0.62f, 4.0f, 0.58f, 3.5f};
 
 static float tile_time(const TileCost &c, int64_t rows, int cols, int slabs) {
   const int64_t tiles = ((rows + c.rows - 1) / c.rows) * ((cols + c.cols - 1) / c.cols), rest = tiles % c.slots;
   const float full = c.slab * slabs + c.ends, last = rest == 0 ? 0.0f : rest > c.slots / 2 ? full : c.slab_rest * slabs + c.ends_rest;
   return (float)(tiles / c.slots) * full + last;
 }
-static bool large_tiles(int64_t rows, int cols, int slabs) { return tile_time(LARGE, rows, cols, slabs) < tile_time(SMALL, rows, cols, slabs); }
+// the form that is soonest (four planes of a row need four row blocks, which the third form's wavefronts have not)
+struct TileForm {
+  const TileCost *cost;
+  float time;
+};
+static TileForm tile_form(int64_t rows, int cols, int slabs, int planes) {
+  TileForm f{&SMALL, tile_time(SMALL, rows, cols, slabs)};
+  const float large = tile_time(LARGE, rows, cols, slabs), lone = tile_time(LONE, rows, cols, slabs);
+  if (large < f.time) f = {&LARGE, large};
+  const int64_t tiles = ((rows + LONE.rows - 1) / LONE.rows) * ((cols + LONE.cols - 1) / LONE.cols);
+  if (planes < 4 && tiles <= LONE.slots && lone < f.time) f = {&LONE, lone};
+  return f;
+}
 
 float t8_tile_time(int M, int N, int K) {
-  const int slabs = (K + T8_BK - 1) / T8_BK;
   // weights that nothing else shares come at 3.7 TB/s (1 x 28672 x 8192: 63 us)
-  return std::max(std::min(tile_time(LARGE, M, N, slabs), tile_time(SMALL, M, N, slabs)), (float)N * (float)K / 3.7e6f);
+  return std::max(tile_form(M, N, (K + T8_BK - 1) / T8_BK, 0).time, (float)N * (float)K / 3.7e6f);
 }
 
 template <int TYPE, int P>
 static hipError_t tile_of(const T8Product &a, hipStream_t st) {
-  if (large_tiles(a.arows, P ? a.K : a.N, ((P ? a.N : a.K) + T8_BK - 1) / T8_BK)) return tile_launch<TYPE, P, false, 2, 4, 8, 4>(a, st);
-  return tile_launch<TYPE, P, false, 2, 2, 4, 4>(a, st);
+  const TileCost *const c = tile_form(a.arows, P ? a.K : a.N, ((P ? a.N : a.K) + T8_BK - 1) / T8_BK, P).cost;
+  if (c == &LARGE) return tile_launch<TYPE, P, false, 2, 2, 4, 8, 4>(a, st);
+  if constexpr (P < 4) {
+    if (c == &LONE) return tile_launch<TYPE, P, false, 3, 4, 2, 2, 4>(a, st);
+  }
+  return tile_launch<TYPE, P, false, 2, 2, 2, 4, 4>(a, st);
 }
 
 hipError_t launch_t8_tile(const T8Product &a, int type, hipStream_t st) {
@@ -512,7 +538,7 @@ static GradPlan grad_plan(int M, int N, int K, int type) {
   const int P = t8_planes(type), slabs = (N + T8_BK - 1) / T8_BK;
   GradPlan best{(M + 15) / 16 * 16 * P, 0, 1, slabs};
   best.whole = best.arows;
-  float time = std::min(tile_time(LARGE, best.arows, K, slabs), tile_time(SMALL, best.arows, K, slabs));
+  float time = tile_form(best.arows, K, slabs, P).time;
   for (const TileCost &c : {LARGE, SMALL}) {
     const int64_t tn = (K + c.cols - 1) / c.cols, tiles = (best.arows + c.rows - 1) / c.rows * tn;
     const int whole = (int)(tiles / c.slots * c.slots / tn * c.rows), rest = best.arows - whole;
@@ -559,7 +585,7 @@ static hipError_t grad_launch(T8Product a, hipStream_t st) {
   a.a += (int64_t)p.whole * a.lda;
   a.xs += rows;
   a.y = (typename W4Mem<TYPE>::T *)a.y + (int64_t)rows * a.ldy;
-  const hipError_t e = tile_launch<TYPE, P, true, 2, 2, 4, 4>(a, st);
+  const hipError_t e = tile_launch<TYPE, P, true, 2, 2, 2, 4, 4>(a, st);
   if (e != hipSuccess) return e;
   const int64_t items = (int64_t)a.M * (a.K / 4);
   if (a.split > 8) t8_join_kernel<TYPE, 16><<<(unsigned)((items + 15) / 16), 256, 0, st>>>(a);

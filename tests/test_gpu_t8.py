@@ -310,7 +310,9 @@ PRODUCTS = [(1, 1, 16), (1, 17, 48), (2, 33, 144), (5, 100, 1168), (1, 700, 4608
             (77, 257, 1040), (128, 128, 128), (129, 200, 912), (300, 384, 1152), (513, 261, 400), (600, 300, 64), (1030, 515, 80), (1, 40, 14336),
             (2000, 1152, 208),
             # more tiles than workgroups, tiles of both sizes, ragged in every direction, one slab a tile, whole tiles
-            (4090, 4085, 272), (9000, 4608, 144), (2500, 8000, 48), (5000, 5120, 128), (8192, 1000, 1152), (3, 9000, 352), (8100, 2300, 1152), (3000, 1500, 2320)]
+            (4090, 4085, 272), (9000, 4608, 144), (2500, 8000, 48), (5000, 5120, 128), (8192, 1000, 1152), (3, 9000, 352), (8100, 2300, 1152), (3000, 1500, 2320),
+            # fewer tiles than compute units and a long summed axis, in either direction
+            (900, 515, 4112), (1100, 1000, 1168), (800, 4100, 1040), (700, 2900, 1200), (30, 4100, 4096)]
 
 
 def _codes(rng, M, K, pad):
