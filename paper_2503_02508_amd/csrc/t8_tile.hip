@@ -6,11 +6,13 @@
 // The weights' rows run along the summed axis in the forward product; in the gradient they run across it, and ds_read_b64_tr_b8 turns 8 rows x
 // 16 bytes on their way to the registers.
 // Workgroups stay and walk over the tiles: the slabs of the next tile are on their way while the last of this one are multiplied.
-// In the forward product a lane's columns are neighbours (block j's lane l reads weight row 4 l + j), so that 16 lanes write whole lines of a
+// In the forward product a lane's columns are neighbours (block j's lane l has weight row 4 l + j), so that 16 lanes write whole lines of a
 // row without any exchange: trading words between lanes took 16384 x 4608 x 1152 from 88 to 100 us.  The transposed reads of the gradient cannot
 // permute columns; its operands are exchanged (weights first) and lanes trade words instead.
-// What bounds it: the large tile's LDS traffic (96 KB read, 32 written for 1024 clocks of products) is as long as its products, and what ends a tile
-// is not overlapped: 4.4 us of 20 at K = 1152.  4096 x 8192 x 8192 runs at 2.5 POP/s (a loop of nothing but products: 4.1).
+// What bounds it: 4096 x 8192 x 8192 takes 218 - 238 us, 2.3 - 2.5 POP/s (the spread is the cards': their clocks fall to 2.15 GHz under it; on codes of
+// zero alone 198), where a loop of nothing but products runs at 4.1.  With every slab from the same lines of the caches it takes 8 % less, without any
+// loads 20 %; fewer LDS clocks (the places of the weights' chunks, a quarter fewer) gave 1 %, a barrier later among the products nothing.  What ends a
+// tile is not overlapped: 4.4 us of 20 at K = 1152.
 #include "t8_product.h"
 
 namespace qc {
@@ -171,8 +173,11 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
   const int lr = lane / 8, lc = (lane % 8) ^ t8_swz<BK>(lr);
   // forward: chunks of the last slab beyond K re-read its end, and become zeros on the activations' side
   const auto back = [&](int c) { return (unsigned)max((all - 1) * BK + c * 16 + 16 - a.K, 0); };
-  // of the forward product's weights, block j's lane l reads row NI l + j, so that a lane's columns are neighbours: swizzled by l
-  const auto wc = [&](int i) { return (lane % 8) ^ (((wave * S::LB + i) * 8 + lr) / NI & 7); };
+  // of the forward product's weights, block j's lane l has row NI l + j, so that a lane's columns are neighbours; they lie in LDS block by block (as
+  // they come, a read of every NI-th row met half of the banks)
+  const auto wrow = [&](int p) { return p / (16 * NI) * (16 * NI) + p % 16 * NI + p / 16 % NI; };
+  // of the gradient's, the chunks of rows 16 apart, which are read together, lie in different halves of the banks
+  const auto turned = [&](int r) { return (r ^ (r >> 4 & 1) * (CB > 8 ? 8 : 1)) & (CB - 1); };
   const unsigned lds0 = t8_lds_address(smem);
   unsigned ao[S::LA], bo[S::LB];
   const int8_t *abase, *bbase;
@@ -185,10 +190,10 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
 #pragma unroll
     for (int i = 0; i < S::LB; ++i) {
       if constexpr (GRAD) {
-        const int r = (wave * S::LB + i) * RB + lane / CB, c = (lane % CB) ^ (r & (CB - 1));
+        const int r = (wave * S::LB + i) * RB + lane / CB, c = (lane % CB) ^ turned(r);
         bo[i] = (unsigned)(min(fat.n0 + c * 16, a.K - 16) - fat.n0);
       } else {
-        bo[i] = (unsigned)(min(fat.n0 + (wave * S::LB + i) * 8 + lr, a.N - 1) - fat.n0) * (unsigned)a.ldw + wc(i) * 16;
+        bo[i] = (unsigned)(min(fat.n0 + wrow((wave * S::LB + i) * 8 + lr), a.N - 1) - fat.n0) * (unsigned)a.ldw + lc * 16;
       }
     }
     abase = a.a + (int64_t)fat.m0 * a.lda;
@@ -209,7 +214,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
         const int r = (wave * S::LB + i) * RB + lane / CB;
         t8_to_lds(to + S::ABYTES + (wave * S::LB + i) * 1024, bo[i] + (unsigned)min(r, a.N - 1 - row) * (unsigned)a.ldw, bbase + (int64_t)row * a.ldw);
       } else {
-        t8_to_lds(to + S::ABYTES + (wave * S::LB + i) * 1024, bo[i] - (last ? back(wc(i)) : 0u), bbase + (int64_t)s * BK);
+        t8_to_lds(to + S::ABYTES + (wave * S::LB + i) * 1024, bo[i] - (last ? back(lc) : 0u), bbase + (int64_t)s * BK);
       }
     }
     fstage = fstage == ST - 1 ? 0 : fstage + 1;
@@ -250,12 +255,12 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
         // lane l of 16 gives the place of row l / 2, half l % 2 of 16 columns, and gets column l of 8 rows
         const int r = kk * 64 + g * 16 + (r16 >> 1), c = (wn >> 4) + j;
         typedef __attribute__((address_space(3))) t8_i2 lds_i2;
-        const t8_i2 lo = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2 *)(bs + r * TN + ((c ^ (r & (CB - 1))) << 4) + (r16 & 1) * 8));
-        const t8_i2 hi = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2 *)(bs + (r + 8) * TN + ((c ^ ((r + 8) & (CB - 1))) << 4) + (r16 & 1) * 8));
+        const t8_i2 lo = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2 *)(bs + r * TN + ((c ^ turned(r)) << 4) + (r16 & 1) * 8));
+        const t8_i2 hi = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2 *)(bs + (r + 8) * TN + ((c ^ turned(r + 8)) << 4) + (r16 & 1) * 8));
         w[j] = t8_i4{lo[0], lo[1], hi[0], hi[1]};
       } else {
-        const int r = wn + r16 * NI + j;
-        w[j] = *(const t8_i4 *)(bs + r * BK + (((kk * 4 + g) ^ (r / NI & 7)) << 4));
+        const int r = wn + j * 16 + r16;
+        w[j] = *(const t8_i4 *)(bs + r * BK + (((kk * 4 + g) ^ t8_swz<BK>(r)) << 4));
       }
     }
   };
