@@ -264,7 +264,30 @@ constexpr float T8_DEEP = ACT == QC_ACT_SILU ? -69.0f : -9.0f;       // exp(-t) 
 template <int ACT>
 constexpr float T8_GONE = ACT == QC_ACT_SILU ? -400.0f : -20.0f;     // the product is below any float32, for finite x
 
-// value and derivative of the activation
+// Value and derivative of the activation, for gates of a magnitude below T8_FAR (2^-100, about): t8_logistic without what lies beyond.  The products with
+// log2(e) are float32 with what they lose (SiLU; of GELU's third power float64 is as short).
+template <int ACT>
+constexpr float T8_FAR = ACT == QC_ACT_SILU ? 69.0f : 9.0f;
+template <int ACT>
+__device__ __forceinline__ float t8_act_near(float gate, float &d) {
+  float hi, lo;
+  if constexpr (ACT == QC_ACT_SILU) {
+    const float a = fabsf(gate);
+    hi = a * -0x1.715476p+0f;
+    lo = __builtin_fmaf(a, 0x1.4ae0cp-26f, __builtin_fmaf(a, 0x1.715476p+0f, hi));
+  } else {
+    const double g = fabsf(gate), u = g * (2.302208198144325 + 0.1029432395800235 * (g * g));
+    hi = -(float)u;
+    lo = (float)(u + (double)hi);
+  }
+  const float e = __builtin_amdgcn_exp2f(hi), z = __builtin_fmaf(e, lo * -0.6931471805599453f, e), r = __builtin_amdgcn_rcpf(1.0f + z);
+  const float s = gate < 0.0f ? z * r : r, o = gate < 0.0f ? r : z * r;
+  if constexpr (ACT == QC_ACT_SILU) d = __builtin_fmaf(gate * o, s, s);
+  else d = __builtin_fmaf(gate * (1.5957691216057308f * (1.0f + 0.134145f * (gate * gate))) * o, s, s);
+  return gate * s;
+}
+
+// of any gate
 __device__ __forceinline__ float t8_act(int act, float gate, float &d) {
   float s, o;
   bool deep;

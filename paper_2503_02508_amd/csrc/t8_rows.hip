@@ -408,9 +408,10 @@ hipError_t launch_t8_expand(const int8_t *q, int64_t ldq, const float *scale, in
 }
 
 // Every element is read before any of the same thread's results is written, so that results may take their inputs' place.
-template <int TYPE>
-__global__ __launch_bounds__(256) void t8_gated_grad_kernel(const void *x, int64_t ldx, const void *g, int64_t ldg, const void *dv, int64_t lddv, int act,
-                                                            int64_t M, int K, void *dx, int64_t lddx, void *dg, int64_t lddg, int rows, int vectors) {
+// Bytes bound it, and not far below them the instructions: 4096 x 4608 float16, GELU, 32.7 us, 5.8 TB/s; 35.3 with two vectors a thread, 37.8 with
+// what far gates need in every element's way.
+template <int TYPE, int ACT>
+__global__ __launch_bounds__(256) void t8_gated_grad_kernel(const void *x, int64_t ldx, const void *g, int64_t ldg, const void *dv, int64_t lddv, int64_t M, int K, void *dx, int64_t lddx, void *dg, int64_t lddg, int rows, int vectors) {
   using T = typename W4Mem<TYPE>::T;
   constexpr int VL = t8_vl<TYPE>;
   const int64_t first = (int64_t)blockIdx.x * rows;
@@ -422,11 +423,21 @@ __global__ __launch_bounds__(256) void t8_gated_grad_kernel(const void *x, int64
     t8_load<TYPE>((const T *)x + row * ldx, e, K, xv);
     t8_load<TYPE>((const T *)g + row * ldg, e, K, gv);
     t8_load<TYPE>((const T *)dv + row * lddv, e, K, d);
+    float most = fabsf(gv[0]);
 #pragma unroll
-    for (int i = 0; i < VL; ++i) {
-      float slope;
-      rx[i] = d[i] * t8_act(act, gv[i], slope);
-      rg[i] = d[i] * xv[i] * slope;
+    for (int i = 1; i < VL; ++i) most = t8_larger(most, gv[i]);
+    if (most < T8_FAR<ACT>) {
+#pragma unroll
+      for (int i = 0; i < VL; ++i) {
+        rx[i] = d[i] * t8_act_near<ACT>(gv[i], rg[i]);
+        rg[i] *= d[i] * xv[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VL; ++i) {
+        rx[i] = d[i] * t8_act(ACT, gv[i], rg[i]);
+        rg[i] *= d[i] * xv[i];
+      }
     }
     t8_store<TYPE>((T *)dx + row * lddx, e, K, rx);
     t8_store<TYPE>((T *)dg + row * lddg, e, K, rg);
@@ -462,8 +473,9 @@ static void gated_grad(const void *x, int64_t ldx, const void *g, int64_t ldg, i
     return;
   }
   const int vectors = (int)((K + VL - 1) / VL), rows = std::max(1, 512 / vectors);
-  const dim3 grid((unsigned)((M + rows - 1) / rows), (unsigned)std::max(1, std::min(M == 1 ? 8192 : 32, vectors / 512)));
-  t8_gated_grad_kernel<TYPE><<<grid, 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, act, M, (int)K, dx, lddx, dg, lddg, rows, vectors);
+  const dim3 grid((unsigned)((M + rows - 1) / rows), (unsigned)std::max(1, std::min(M == 1 ? 16384 : 32, vectors / 256)));
+  const auto kern = act == QC_ACT_SILU ? t8_gated_grad_kernel<TYPE, QC_ACT_SILU> : t8_gated_grad_kernel<TYPE, QC_ACT_GELU>;
+  kern<<<grid, 256, 0, st>>>(x, ldx, g, ldg, dv, lddv, M, (int)K, dx, lddx, dg, lddg, rows, vectors);
 }
 
 hipError_t launch_t8_gated_grad(const void *x, int64_t ldx, const void *g, int64_t ldg, int act, const void *dv, int64_t lddv, int type, int M, int K, void *dx,
