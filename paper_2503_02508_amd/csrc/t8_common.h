@@ -240,24 +240,23 @@ __device__ __forceinline__ void t8_logistic(int act, float gate, float &s, float
   s = u < 0.0 ? z * r : r;
   o = u < 0.0 ? r : z * r;
 }
-// act(gate) x by the same formula without the cases, for gates above T8_DEEP: to 1.8e-6 of its value (9e-7 by what log2(e) loses in float32, at the
-// largest exponents).  The logistic function is 1 / (1 + exp(-t)), which keeps the digits of small values; beyond LIMIT it is 0 or 1 to any
+// act(gate) x by the same formula without the cases, for gates above T8_DEEP: to 1.8e-6 of its value.  The logistic function is 1 / (1 + exp(-t)), which keeps the digits of small values; beyond LIMIT it is 0 or 1 to any
 // product.  An infinite or NaN gate gives an infinite or NaN product.
 template <int ACT>
 __device__ __forceinline__ float t8_gate(float gate, float x) {
   constexpr float LIMIT = ACT == QC_ACT_SILU ? 85.0f : 9.9f;             // exp(-t) up to 2^123
   const float b = __builtin_amdgcn_fmed3f(gate, -LIMIT, LIMIT);
-  float hi, lo;
+  float hi, lo;                                          // -t = hi log(2) + lo
   if constexpr (ACT == QC_ACT_SILU) {
     hi = b * -1.4426950408889634f;
-    lo = __builtin_fmaf(b, -1.4426950408889634f, -hi);
+    lo = -__builtin_fmaf(hi, 0.6931471805599453f, b);
   } else {
     const double g = b, u = g * (-2.302208198144325 - 0.1029432395800235 * (g * g));
     hi = (float)u;
-    lo = (float)(u - (double)hi);
+    lo = (float)(u - (double)hi) * 0.6931471805599453f;
   }
   const float e = __builtin_amdgcn_exp2f(hi);
-  return gate * __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, lo * 0.6931471805599453f, e)) * x;
+  return gate * __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, lo, e)) * x;
 }
 template <int ACT>
 constexpr float T8_DEEP = ACT == QC_ACT_SILU ? -69.0f : -9.0f;       // exp(-t) = 2^100, about
