@@ -240,8 +240,8 @@ __device__ __forceinline__ void t8_logistic(int act, float gate, float &s, float
   s = u < 0.0 ? z * r : r;
   o = u < 0.0 ? r : z * r;
 }
-// act(gate) x by the same formula without the cases, for gates above T8_DEEP: to 1.8e-6 of its value.  The logistic function is 1 / (1 + exp(-t)), which keeps the digits of small values; beyond LIMIT it is 0 or 1 to any
-// product.  An infinite or NaN gate gives an infinite or NaN product.
+// act(gate) x by the same formula without the cases, for gates above T8_DEEP: to 1.8e-6 of its value.  The logistic function is
+// 1 / (1 + exp(-t)), which keeps the digits of small values; beyond LIMIT it is 0 or 1 to any product.  An infinite or NaN gate gives an infinite or NaN product.
 template <int ACT>
 __device__ __forceinline__ float t8_gate(float gate, float x) {
   constexpr float LIMIT = ACT == QC_ACT_SILU ? 85.0f : 9.9f;             // exp(-t) up to 2^123

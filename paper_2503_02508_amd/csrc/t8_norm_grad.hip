@@ -3,6 +3,9 @@
 // A row's h and dy are read once and stay in registers while its two sums are formed, so that the kernel moves what it has to: h, dy, dh in,
 // dx out.  A workgroup walks rows M / groups apart and keeps its columns' part of dweight in registers from row to row; the groups' parts
 // go to the workspace, and a second kernel adds them in their order.
+// Bytes bound it: 8192 x 4096 bfloat16 with dh 52.7 us, 5.1 TB/s, and 4.9 for the parts (8 MB; workgroups of eight wavefronts, two a compute unit, the next
+// row on its way: 99 us with one row at a time, 66 with the weight read from memory in every row); 1000 x 1153 float32 8.0 and 4.8, a row's latency and
+// two rows a workgroup.
 #include "t8_common.h"
 
 namespace qc {

@@ -3,6 +3,9 @@
 // All of them move bytes: a row is read once, held in registers as float32 while its largest value is found, and written.  One wavefront
 // takes a row of up to 256 vectors of 16 bytes, a workgroup of 2 - 16 wavefronts a longer one (or a short one where there are few rows:
 // then nothing but latency counts), and rows beyond 16 wavefronts' registers are read again for each of the steps.
+// Kernels alone: codes of 16384 x 4608 bfloat16 37.3 us, 6.1 TB/s; of its gated rows 75.7 us, 5.0 TB/s (the instructions take 50 of them, and two wavefronts
+// in three wait); the norm of 16384 x 1152 bfloat16 with its residual 27.6 us, 4.8 TB/s; planes of 8192 x 4608 bfloat16 29.8 us, 5.1 TB/s; codes
+// read back, 16384 x 4608 to bfloat16, 36 us, 6.3 TB/s.  One row of 8192 takes 3.6 us, 77 of 4608 float32 3.4: a read, two reductions, a write.
 //
 // Exact decisions.  The codes are those of the definition: float32 quotients, rounded half to even.  Each is formed as v (1 / scale), which is off by
 // at most 1.2e-5 for quotients of up to 127, and where it is nearer than 2e-5 to a border the division decides.  The gated product is
@@ -21,8 +24,8 @@ __device__ __forceinline__ unsigned t8_code(float v, float scale) {
   return (unsigned)(int)n;
 }
 
-// One row's reductions over the wavefronts of a workgroup.  The slots alternate from row to row and from use to use: a wavefront that
-// writes one again is at least one barrier behind the last that read it.
+// One row's reductions over the wavefronts of a workgroup, a slot for each use.  Where a workgroup walks over rows the slots alternate from row to
+// row: a wavefront that writes one again is at least one barrier behind the last that read it.
 struct T8Across {
   double d[2][16];
   unsigned u[2][2][16];
@@ -38,213 +41,211 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = FULL ? (int)blockDim.x >> 6 : 1, step = 64 * waves * VL, e0 = (FULL ? (int)threadIdx.x : lane) * VL;
   const int width = SOURCE == T8_PLANES ? a.pitch : a.K;
-  // (one row: what does not depend on it would be worked out ahead of a loop, in registers that then hold nothing else)
+  // (one row a workgroup or wavefront: what does not depend on the row would be worked out ahead of a loop, in registers that then hold nothing else)
   const int64_t row = FULL ? blockIdx.x + (int64_t)blockIdx.y * gridDim.x : (blockIdx.x + (int64_t)blockIdx.y * gridDim.x) * 4 + wave;
-  {
-    if (row >= a.M) return;
-    const T *x = (const T *)a.x + row * a.ldx, *add = (const T *)a.add + row * a.lda;
-    float v[C][VL], w[C][VL];
-    w4_u4 second[C];
+  if (row >= a.M) return;
+  const T *x = (const T *)a.x + row * a.ldx, *add = (const T *)a.add + row * a.lda;
+  float v[C][VL], w[C][VL];
+  w4_u4 second[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) t8_load<TYPE>(x, e0 + c * step, a.K, v[c]);
-    if (GATED || (SOURCE == T8_NORM && a.add)) {
+  for (int c = 0; c < C; ++c) t8_load<TYPE>(x, e0 + c * step, a.K, v[c]);
+  if (GATED || (SOURCE == T8_NORM && a.add)) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) second[c] = t8_raw<TYPE>(add, e0 + c * step, a.K);
-    }
-    if constexpr (SOURCE == T8_PLANES) {
+    for (int c = 0; c < C; ++c) second[c] = t8_raw<TYPE>(add, e0 + c * step, a.K);
+  }
+  if constexpr (SOURCE == T8_PLANES) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
-    }
-    if constexpr (SOURCE == T8_NORM) {
-      if (a.add) {
-        T *h = (T *)a.h + row * a.ldh;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          float r[VL];
-          t8_values<TYPE>(second[c], r);
-#pragma unroll
-          for (int i = 0; i < VL; ++i) v[c][i] = W4Mem<TYPE>::get(W4Mem<TYPE>::put(v[c][i] + r[i]));
-          t8_store<TYPE>(h, e0 + c * step, a.K, v[c]);
-        }
-      }
-      double ss = 0.0;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < VL; ++i) ss = __builtin_fma((double)v[c][i], (double)v[c][i], ss);
-      ss = wave_sum_dpp(ss);
-      if constexpr (FULL) {
-        if (lane == 0) across.d[0][wave] = ss;
-        t8_lds_barrier();
-        ss = t8_across_sum(across.d[0], waves, lane);
-      }
-      const float rho = (float)t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
-      asm volatile("" ::: "memory");                      // the weight is not loaded sooner: registers, and with them wavefronts
+    for (int c = 0; c < C; ++c) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
+  }
+  if constexpr (SOURCE == T8_NORM) {
+    if (a.add) {
+      T *h = (T *)a.h + row * a.ldh;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
+        float r[VL];
+        t8_values<TYPE>(second[c], r);
 #pragma unroll
-        for (int i = 0; i < VL; ++i) v[c][i] *= rho;
-        if (a.w) {
-          t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
-#pragma unroll
-          for (int i = 0; i < VL; ++i) v[c][i] *= w[c][i];
-        }
-      }
-      if (a.y) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) t8_store<TYPE>((T *)a.y + row * a.ldy, e0 + c * step, a.K, v[c]);
-      }
-      if (!a.q) return;
-    }
-    uint32_t deep = 0;                                    // elements (c VL + i) whose gate is far below zero: float64 decides them
-    if constexpr (GATED) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float g[VL], least = 0.0f;
-        t8_values<TYPE>(second[c], g);
-#pragma unroll
-        for (int i = 0; i < VL; ++i) {
-          v[c][i] = t8_gate<ACT>(g[i], v[c][i]);
-          least = fminf(least, g[i]);
-        }
-        if (least < T8_DEEP<ACT>) {
-#pragma unroll
-          for (int i = 0; i < VL; ++i) deep |= g[i] < T8_DEEP<ACT> ? 1u << (c * VL + i) : 0u;
-        }
+        for (int i = 0; i < VL; ++i) v[c][i] = W4Mem<TYPE>::get(W4Mem<TYPE>::put(v[c][i] + r[i]));
+        t8_store<TYPE>(h, e0 + c * step, a.K, v[c]);
       }
     }
-    if constexpr (SOURCE == T8_PLANES) {
+    double ss = 0.0;
 #pragma unroll
-      for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < VL; ++i) v[c][i] *= w[c][i];
+      for (int i = 0; i < VL; ++i) ss = __builtin_fma((double)v[c][i], (double)v[c][i], ss);
+    ss = wave_sum_dpp(ss);
+    if constexpr (FULL) {
+      if (lane == 0) across.d[0][wave] = ss;
+      t8_lds_barrier();
+      ss = t8_across_sum(across.d[0], waves, lane);
     }
-    float tops[C];
+    const float rho = (float)t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
+    asm volatile("" ::: "memory");                      // the weight is not loaded sooner: registers, and with them wavefronts
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      tops[c] = fabsf(v[c][0]);
 #pragma unroll
-      for (int i = 1; i < VL; ++i) tops[c] = t8_larger(tops[c], v[c][i]);
+      for (int i = 0; i < VL; ++i) v[c][i] *= rho;
+      if (a.w) {
+        t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
+#pragma unroll
+        for (int i = 0; i < VL; ++i) v[c][i] *= w[c][i];
+      }
     }
-    unsigned top = t8_mag(tops[0]);
+    if (a.y) {
 #pragma unroll
-    for (int c = 1; c < C; ++c) top = max(top, t8_mag(tops[c]));
-    const auto over_row = [&](unsigned t, int use) {
-      t = t8_wave_max(t);
-      if constexpr (FULL) {
-        if (lane == 0) across.u[0][use][wave] = t;
-        t8_lds_barrier();
-        t = t8_across_max(across.u[0][use], waves, lane);
+      for (int c = 0; c < C; ++c) t8_store<TYPE>((T *)a.y + row * a.ldy, e0 + c * step, a.K, v[c]);
+    }
+    if (!a.q) return;
+  }
+  uint32_t deep = 0;                                    // elements (c VL + i) whose gate is far below zero: float64 decides them
+  if constexpr (GATED) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float g[VL], least = 0.0f;
+      t8_values<TYPE>(second[c], g);
+#pragma unroll
+      for (int i = 0; i < VL; ++i) {
+        v[c][i] = t8_gate<ACT>(g[i], v[c][i]);
+        least = fminf(least, g[i]);
       }
-      return t;
-    };
-    top = over_row(top, 0);
-    const bool lost = top >= 0x7F800000u;                 // an infinity or a NaN
+      if (least < T8_DEEP<ACT>) {
+#pragma unroll
+        for (int i = 0; i < VL; ++i) deep |= g[i] < T8_DEEP<ACT> ? 1u << (c * VL + i) : 0u;
+      }
+    }
+  }
+  if constexpr (SOURCE == T8_PLANES) {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < VL; ++i) v[c][i] *= w[c][i];
+  }
+  float tops[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    tops[c] = fabsf(v[c][0]);
+#pragma unroll
+    for (int i = 1; i < VL; ++i) tops[c] = t8_larger(tops[c], v[c][i]);
+  }
+  unsigned top = t8_mag(tops[0]);
+#pragma unroll
+  for (int c = 1; c < C; ++c) top = max(top, t8_mag(tops[c]));
+  const auto over_row = [&](unsigned t, int use) {
+    t = t8_wave_max(t);
+    if constexpr (FULL) {
+      if (lane == 0) across.u[0][use][wave] = t;
+      t8_lds_barrier();
+      t = t8_across_max(across.u[0][use], waves, lane);
+    }
+    return t;
+  };
+  top = over_row(top, 0);
+  const bool lost = top >= 0x7F800000u;                 // an infinity or a NaN
 
-    if constexpr (SOURCE == T8_PLANES) {
-      constexpr int P = t8_planes(TYPE);
-      const float most = __builtin_bit_cast(float, top);
-      const bool empty = most < T8_EMPTY;
-      const double full = P == 2 ? 127.0 * 256.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
-      if (e0 == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / full);
+  if constexpr (SOURCE == T8_PLANES) {
+    constexpr int P = t8_planes(TYPE);
+    const float most = __builtin_bit_cast(float, top);
+    const bool empty = most < T8_EMPTY;
+    const double full = P == 2 ? 127.0 * 256.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
+    if (e0 == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / full);
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        unsigned b[VL];
-        int t[VL];
+    for (int c = 0; c < C; ++c) {
+      unsigned b[VL];
+      int t[VL];
+#pragma unroll
+      for (int i = 0; i < VL; ++i) {
+        if constexpr (P == 2) t[i] = lost ? 0 : (int)__builtin_rintf(v[c][i] * (float)mult);
+        else t[i] = lost ? 0 : (int)__builtin_rint((double)v[c][i] * mult);
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
-          if constexpr (P == 2) t[i] = lost ? 0 : (int)__builtin_rintf(v[c][i] * (float)mult);
-          else t[i] = lost ? 0 : (int)__builtin_rint((double)v[c][i] * mult);
+          b[i] = (unsigned)t[i];
+          t[i] = (t[i] >> 8) + ((t[i] >> 7) & 1);       // what is left when a signed byte is taken away
         }
+        t8_store_bytes<VL>(a.q + t8_plane_row((int)row, p, P) * a.pitch, e0 + c * step, a.pitch, b);
+      }
+    }
+  } else {
+    // elements that float64 or the division decides, as a word of bits (c VL + i), read again; few
+    uint32_t flags = deep;
+    const auto element = [&](int bit) { return e0 + bit / VL * step + bit % VL; };
+    const auto exact = [&](int e) {
+      const float g = W4Mem<TYPE>::get(add[e]), f = W4Mem<TYPE>::get(x[e]);
+      return g == 0.0f || f == 0.0f || g < T8_GONE<ACT> ? 0.0f : (float)t8_gate_exact(ACT, g, f);      // rows of padding are zeros
+    };
+    const bool tiny = GATED && __builtin_bit_cast(float, top) < T8_TINY;
+    if constexpr (GATED) {
+      if (!lost) {
+        const float near = __builtin_bit_cast(float, top) * (1.0f - 5e-6f);
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
+        for (int c = 0; c < C; ++c)
+          if (tops[c] >= near) {
 #pragma unroll
-          for (int i = 0; i < VL; ++i) {
-            b[i] = (unsigned)t[i];
-            t[i] = (t[i] >> 8) + ((t[i] >> 7) & 1);       // what is left when a signed byte is taken away
+            for (int i = 0; i < VL; ++i) flags |= (tiny ? e0 + c * step + i < width : fabsf(v[c][i]) >= near) ? 1u << (c * VL + i) : 0u;
           }
-          t8_store_bytes<VL>(a.q + t8_plane_row((int)row, p, P) * a.pitch, e0 + c * step, a.pitch, b);
+        top = 0;
+        while (flags) {
+          const int bit = __builtin_ctz(flags);
+          flags &= flags - 1;
+          top = max(top, t8_mag(exact(element(bit))));
+        }
+        top = over_row(top, 1);
+      }
+      flags = deep;
+    }
+    float scale = __builtin_bit_cast(float, top) / 127.0f;
+    if (scale == 0.0f) scale = 1.0f;
+    const bool none = lost || top >= 0x7F800000u, all = tiny || scale < 0x1p-100f;
+    if (e0 == 0) a.scale[row] = none ? __builtin_nanf("") : scale;
+    const float inv = 1.0f / (all ? 1.0f : scale);
+    int8_t *q = a.q + row * a.ldq;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      unsigned b[VL];
+      float far = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VL; ++i) {
+        const float m = __builtin_fmaf(v[c][i], inv, T8_MAGIC), n = m - T8_MAGIC, d = __builtin_fmaf(v[c][i], inv, -n);
+        b[i] = __builtin_bit_cast(unsigned, m);
+        if constexpr (GATED) far = fmaxf(far, __builtin_fmaf(fabsf(n), 2.5e-6f, fabsf(d)));
+        else far = fmaxf(far, fabsf(d));
+      }
+      if (none) {
+#pragma unroll
+        for (int i = 0; i < VL; ++i) b[i] = 0;
+      }
+      t8_store_bytes<VL>(q, e0 + c * step, width, b);
+      if (far > 0.5f - T8_NEAR) {
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+          const float n = __builtin_fmaf(v[c][i], inv, T8_MAGIC) - T8_MAGIC, d = fabsf(__builtin_fmaf(v[c][i], inv, -n));
+          flags |= (GATED ? __builtin_fmaf(fabsf(n), 2.5e-6f, d) : d) > 0.5f - T8_NEAR ? 1u << (c * VL + i) : 0u;
         }
       }
-    } else {
-      // elements that float64 or the division decides, as a word of bits (c VL + i), read again; few
-      uint32_t flags = deep;
-      const auto element = [&](int bit) { return e0 + bit / VL * step + bit % VL; };
-      const auto exact = [&](int e) {
-        const float g = W4Mem<TYPE>::get(add[e]), f = W4Mem<TYPE>::get(x[e]);
-        return g == 0.0f || f == 0.0f || g < T8_GONE<ACT> ? 0.0f : (float)t8_gate_exact(ACT, g, f);      // rows of padding are zeros
-      };
-      const bool tiny = GATED && __builtin_bit_cast(float, top) < T8_TINY;
+    }
+    if (all) flags = ~0u >> (32 - C * VL);
+    if (none) flags = 0;
+    while (flags) {                                     // a byte behind its vector, from the same lane: in this order
+      const int bit = __builtin_ctz(flags), e = element(bit);
+      flags &= flags - 1;
+      if (e >= width) continue;
+      float t;
       if constexpr (GATED) {
-        if (!lost) {
-          const float near = __builtin_bit_cast(float, top) * (1.0f - 5e-6f);
+        t = exact(e);
+      } else if constexpr (SOURCE == T8_NORM) {
+        t = 0.0f;
 #pragma unroll
-          for (int c = 0; c < C; ++c)
-            if (tops[c] >= near) {
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-              for (int i = 0; i < VL; ++i) flags |= (tiny ? e0 + c * step + i < width : fabsf(v[c][i]) >= near) ? 1u << (c * VL + i) : 0u;
-            }
-          top = 0;
-          while (flags) {
-            const int bit = __builtin_ctz(flags);
-            flags &= flags - 1;
-            top = max(top, t8_mag(exact(element(bit))));
-          }
-          top = over_row(top, 1);
-        }
-        flags = deep;
+          for (int i = 0; i < VL; ++i)
+            if (bit == c * VL + i) t = v[c][i];
+      } else {
+        t = W4Mem<TYPE>::get(x[e]);
       }
-      float scale = __builtin_bit_cast(float, top) / 127.0f;
-      if (scale == 0.0f) scale = 1.0f;
-      const bool none = lost || top >= 0x7F800000u, all = tiny || scale < 0x1p-100f;
-      if (e0 == 0) a.scale[row] = none ? __builtin_nanf("") : scale;
-      const float inv = 1.0f / (all ? 1.0f : scale);
-      int8_t *q = a.q + row * a.ldq;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        unsigned b[VL];
-        float far = 0.0f;
-#pragma unroll
-        for (int i = 0; i < VL; ++i) {
-          const float m = __builtin_fmaf(v[c][i], inv, T8_MAGIC), n = m - T8_MAGIC, d = __builtin_fmaf(v[c][i], inv, -n);
-          b[i] = __builtin_bit_cast(unsigned, m);
-          if constexpr (GATED) far = fmaxf(far, __builtin_fmaf(fabsf(n), 2.5e-6f, fabsf(d)));
-          else far = fmaxf(far, fabsf(d));
-        }
-        if (none) {
-#pragma unroll
-          for (int i = 0; i < VL; ++i) b[i] = 0;
-        }
-        t8_store_bytes<VL>(q, e0 + c * step, width, b);
-        if (far > 0.5f - T8_NEAR) {
-#pragma unroll
-          for (int i = 0; i < VL; ++i) {
-            const float n = __builtin_fmaf(v[c][i], inv, T8_MAGIC) - T8_MAGIC, d = fabsf(__builtin_fmaf(v[c][i], inv, -n));
-            flags |= (GATED ? __builtin_fmaf(fabsf(n), 2.5e-6f, d) : d) > 0.5f - T8_NEAR ? 1u << (c * VL + i) : 0u;
-          }
-        }
-      }
-      if (all) flags = ~0u >> (32 - C * VL);
-      if (none) flags = 0;
-      while (flags) {                                     // a byte behind its vector, from the same lane: in this order
-        const int bit = __builtin_ctz(flags), e = element(bit);
-        flags &= flags - 1;
-        if (e >= width) continue;
-        float t;
-        if constexpr (GATED) {
-          t = exact(e);
-        } else if constexpr (SOURCE == T8_NORM) {
-          t = 0.0f;
-#pragma unroll
-          for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < VL; ++i)
-              if (bit == c * VL + i) t = v[c][i];
-        } else {
-          t = W4Mem<TYPE>::get(x[e]);
-        }
-        q[e] = (int8_t)t8_code(t, scale);
-      }
+      q[e] = (int8_t)t8_code(t, scale);
     }
   }
 }
@@ -411,7 +412,8 @@ hipError_t launch_t8_expand(const int8_t *q, int64_t ldq, const float *scale, in
 // Bytes bound it, and not far below them the instructions: 4096 x 4608 float16, GELU, 32.7 us, 5.8 TB/s; 35.3 with two vectors a thread, 37.8 with
 // what far gates need in every element's way.
 template <int TYPE, int ACT>
-__global__ __launch_bounds__(256) void t8_gated_grad_kernel(const void *x, int64_t ldx, const void *g, int64_t ldg, const void *dv, int64_t lddv, int64_t M, int K, void *dx, int64_t lddx, void *dg, int64_t lddg, int rows, int vectors) {
+__global__ __launch_bounds__(256) void t8_gated_grad_kernel(const void *x, int64_t ldx, const void *g, int64_t ldg, const void *dv, int64_t lddv, int64_t M,
+                                                            int K, void *dx, int64_t lddx, void *dg, int64_t lddg, int rows, int vectors) {
   using T = typename W4Mem<TYPE>::T;
   constexpr int VL = t8_vl<TYPE>;
   const int64_t first = (int64_t)blockIdx.x * rows;

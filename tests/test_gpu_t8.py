@@ -306,13 +306,61 @@ def test_gated_grad(qc, M, K, t, act):
 
 
 # M, N, K
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("t", TYPES)
+def test_gated_grad_of_far_gates(qc, t, act):
+    """Gates on both sides of every case of the activation, beside ordinary ones and alone in their vectors, and gates that are not finite."""
+    import torch
+    code = qc.QC_ACT_SILU if act == "silu" else qc.QC_ACT_GELU
+    sizes = [0.0, 2.0 ** -20, 0.3, 5.0, 8.9, 9.0, 9.1, 9.9, 10.5, 13.0, 14.1, 15.2, 30.0, 31.0, 68.5, 69.0, 69.5, 85.0, 90.0, 103.0, 104.5, 150.0, 210.0, 280.0, 400.0, 6e4]
+    far = np.array([v for a in sizes for v in (a, -a)])
+    rng = np.random.default_rng(5)
+    K = 8 * len(far)
+    gates = np.stack([np.repeat(far, 8), np.tile(far, 8)[rng.permutation(K)], np.where(np.arange(K) % 8 == 3, np.repeat(far, 8), rng.standard_normal(K))])
+    x, d = [_dev(rng.standard_normal((3, K))).to(_type(t)) for _ in range(2)]
+    g = _dev(gates).to(_type(t))
+    gn = _np(g)
+    dx, dg = torch.empty_like(x), torch.empty_like(x)
+    qc.qc_t8_gated_grad(x, g, d, dx, dg, act=code)
+    wx, wg = O.gated_grad(_np(x), gn, act, _np(d))
+    # as above; results that are less than the least float32 are zero
+    tt = gn if act == "silu" else 2 * np.sqrt(2 / np.pi) * (gn + 0.044715 * gn ** 3)
+    with np.errstate(over="ignore"):
+        s = 1 / (1 + np.exp(-tt))
+        o = 1 / (1 + np.exp(tt))
+    slope = 1.0 if act == "silu" else 2 * np.sqrt(2 / np.pi) * (1 + 3 * 0.044715 * gn ** 2)
+    with np.errstate(invalid="ignore"):
+        along = np.nan_to_num(np.abs(gn) * slope * s * o)
+    # float16 has nothing from 65520 on, the middle between its largest value, 65504, and 2^16: such results round to infinities
+    over = (np.abs(wx) >= 65520) & (t == "f16")
+    assert np.array_equal(_np(dx)[over], np.copysign(np.inf, wx[over]))
+    fits = _dev(~over)
+    wx = np.where(over, 0.0, wx)
+    _check(torch.where(fits, dx, torch.zeros_like(dx)), wx, 16 * E * np.abs(wx) + 2.0 ** -149 * (1 + np.abs(_np(d))), t, "dx")
+    _check(dg, wg, (32 * E * (s + along) + 2.0 ** -149 + 1e-12) * np.abs(_np(d) * _np(x)) + 2.0 ** -149, t, "dgate")
+    # a gate that is not finite leaves its neighbours as they were
+    for bad in (np.inf, -np.inf, np.nan):
+        g2 = g.clone()
+        g2[:, 5::16] = bad
+        dx2, dg2 = torch.empty_like(x), torch.empty_like(x)
+        qc.qc_t8_gated_grad(x, g2, d, dx2, dg2, act=code)
+        same = torch.ones(K, dtype=torch.bool, device="cuda")
+        same[5::16] = False
+        dx2 = torch.where(fits | ~same, dx2, torch.zeros_like(dx2))
+        _check(dx2[:, same], wx[:, _np(same) > 0], (16 * E * np.abs(wx) + 2.0 ** -149 * (1 + np.abs(_np(d))))[:, _np(same) > 0], t, "dx beside %s" % bad)
+        if np.isnan(bad):
+            assert torch.isnan(dx2[:, ~same]).all() and torch.isnan(dg2[:, ~same]).all()
+
+
 PRODUCTS = [(1, 1, 16), (1, 17, 48), (2, 33, 144), (5, 100, 1168), (1, 700, 4608), (16, 48, 384), (17, 64, 272), (33, 31, 656), (64, 130, 1152),
             (77, 257, 1040), (128, 128, 128), (129, 200, 912), (300, 384, 1152), (513, 261, 400), (600, 300, 64), (1030, 515, 80), (1, 40, 14336),
             (2000, 1152, 208),
             # more tiles than workgroups, tiles of both sizes, ragged in every direction, one slab a tile, whole tiles
             (4090, 4085, 272), (9000, 4608, 144), (2500, 8000, 48), (5000, 5120, 128), (8192, 1000, 1152), (3, 9000, 352), (8100, 2300, 1152), (3000, 1500, 2320),
             # fewer tiles than compute units and a long summed axis, in either direction
-            (900, 515, 4112), (1100, 1000, 1168), (800, 4100, 1040), (700, 2900, 1200), (30, 4100, 4096)]
+            (900, 515, 4112), (1100, 1000, 1168), (800, 4100, 1040), (700, 2900, 1200), (30, 4100, 4096),
+            # gradients whose rows are longer than a workgroup's registers, in all types and in float32 alone
+            (5, 40000, 48), (40, 20000, 16)]
 
 
 def _codes(rng, M, K, pad):
