@@ -213,7 +213,8 @@ static NormGradShape norm_grad_shape(int M, int K, int type) {
   NormGradShape s{};
   s.groups = std::min(M, NORM_GRAD_GROUPS);
   if (vectors > 64 * 8 * 4 || K < vl) return s;
-  s.waves = std::min((vectors + 64 * (16 / vl) - 1) / (64 * (16 / vl)), 8);
+  // two vectors a lane, so that the next row is on its way (16384 x 1152 float32 55 us; with four 76, with one 60)
+  s.waves = std::min((vectors + 127) / 128, 8);
   while (s.waves < 8 && vectors > 64 * s.waves && (int64_t)M * s.waves < 2048) ++s.waves;
   s.c = (vectors + 64 * s.waves - 1) / (64 * s.waves);
   s.c = s.c > 2 ? 4 : s.c;

@@ -375,32 +375,36 @@ hipError_t launch_t8_rows(const T8RowArgs &a, int type, int source, hipStream_t 
 template <int TYPE>
 __global__ __launch_bounds__(256) void t8_expand_kernel(const int8_t *q, int64_t ldq, const float *scale, int M, int K, typename W4Mem<TYPE>::T *out, int64_t ldo,
                                                         int rows, int vectors) {
+  constexpr int VL = t8_vl<TYPE>;                          // one store: 16 bytes beside 16 bytes, whole lines (two of float32 in turn: 151 us for 79)
   const int64_t first = (int64_t)blockIdx.x * rows;
   const int count = (int)min((int64_t)rows, M - first) * vectors;
   for (int t = blockIdx.y * 256 + threadIdx.x; t < count; t += gridDim.y * 256) {
-    const int r = t / vectors, e = (t - r * vectors) * 8;
+    const int r = t / vectors, e = (t - r * vectors) * VL;
     const int64_t row = first + r;
     const float s = scale[row];
     const int8_t *from = q + row * ldq;
     typename W4Mem<TYPE>::T *to = out + row * ldo;
-    float v[8];
-    if (e + 8 <= K) {
-      const w4_u2 b = *(const t8_u2 *)(from + e);
+    float v[VL];
+    if (e + VL <= K) {
+      unsigned b[2];
+      if constexpr (VL == 8) {
+        const w4_u2 both = *(const t8_u2 *)(from + e);
+        b[0] = both[0], b[1] = both[1];
+      } else {
+        b[0] = *(const t8_u1 *)(from + e);
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)(b[i / 4] >> (8 * (i % 4))) * s;
+      for (int i = 0; i < VL; ++i) v[i] = (float)(int8_t)(b[i / 4] >> (8 * (i % 4))) * s;
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = e + i < K ? (float)from[e + i] * s : 0.0f;
+      for (int i = 0; i < VL; ++i) v[i] = e + i < K ? (float)from[e + i] * s : 0.0f;
     }
-    constexpr int VL = t8_vl<TYPE>;
-#pragma unroll
-    for (int i = 0; i < 8; i += VL)
-      if (e + i < K) t8_store<TYPE>(to, e + i, K, v + i);
+    t8_store<TYPE>(to, e, K, v);
   }
 }
 
 hipError_t launch_t8_expand(const int8_t *q, int64_t ldq, const float *scale, int M, int K, void *out, int type, int64_t ldo, hipStream_t st) {
-  const int vectors = (K + 7) / 8, rows = std::max(1, 1024 / vectors);
+  const int vl = type == QC_TYPE_F32 ? 4 : 8, vectors = (K + vl - 1) / vl, rows = std::max(1, 1024 / vectors);
   const dim3 grid((unsigned)((M + rows - 1) / rows), (unsigned)std::max(1, std::min(16, vectors / 1024)));
   if (type == QC_TYPE_F32) t8_expand_kernel<QC_TYPE_F32><<<grid, 256, 0, st>>>(q, ldq, scale, M, K, (float *)out, ldo, rows, vectors);
   else if (type == QC_TYPE_F16) t8_expand_kernel<QC_TYPE_F16><<<grid, 256, 0, st>>>(q, ldq, scale, M, K, (_Float16 *)out, ldo, rows, vectors);
