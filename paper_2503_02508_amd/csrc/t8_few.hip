@@ -121,13 +121,15 @@ static hipError_t few_launch(T8Product a, hipStream_t st) {
 
 // us of a tile's launch: what its workgroups load, over the chip at 13 TB/s (from the L2 caches, mostly) and over one compute unit's share of them at
 // 70 GB/s (50 where it has one workgroup of a large tile); the weights once, from memory, at 5.2 TB/s (3.9 where a compute unit has one workgroup of
-// 32 x 32, too few loads on their way); and what a launch takes.  Measured (the best of these | the others): 1 x 28672 x 8192 40.7 with 16 x 16 | 44 with
-// 16 x 64; 32 x 8192 x 8192 16.4 with 16 x 64 | 18.9 - 21.6; 64 x 8192 x 8192 19.5 with 32 x 64 | 22 - 24, tiles of 128 x 128 (t8_tile.hip) 44; 256 x 8192 x
-// 8192 42 with 64 x 64 | 59 - 72 | 44; 256 x 1152 x 4608 10.5 with 32 x 32 | 10.6 - 16 | 24; 256 x 4608 x 1152 9.4 with 128 x 128 | 10.1 - 12.
+// 32 x 32, too few loads on their way); and what a launch and the sum over the wavefronts take.  Measured (the best of these | the others | tiles of
+// 64 x 128, t8_tile.hip): 1 x 28672 x 8192 40.7 with 16 x 16 | 44 with 16 x 64; 32 x 8192 x 8192 16.4 with 16 x 64 | 18.9 - 21.6; 64 x 8192 x 8192 19.5 with
+// 32 x 64 | 22 - 24 | 33; 128 x 8192 x 8192 25.4 with 64 x 64 | | 32; 256 x 8192 x 8192 42 with 64 x 64 | 59 - 72 | 33; 256 x 1152 x 4608 10.5 with 32 x 32 |
+// 10.6 - 16 | 20; 256 x 4608 x 1152 10.1 - 12 | 8.3.
 static float few_time(const T8Product &a, int MT, int NT) {
   const int64_t groups = (int64_t)((a.M + 16 * MT - 1) / (16 * MT)) * ((a.N + 16 * NT - 1) / (16 * NT));
   const float each = (float)((a.K + 127) / 128) * (float)(MT + NT) * 2048.0f, memory = MT + NT == 4 && groups <= 256 ? 3.9e6f : 5.2e6f;
-  return 4.0f + std::max(std::max((float)groups * each / 13e6f, (float)((groups + 255) / 256) * each / (MT + NT > 4 ? 50e3f : 70e3f)), (float)a.N * (float)a.K / memory);
+  const float load = std::max((float)groups * each / 13e6f, (float)((groups + 255) / 256) * each / (MT + NT > 4 ? 50e3f : 70e3f));
+  return 4.0f + 0.25f * (float)(MT * NT) + std::max(load, (float)a.N * (float)a.K / memory);
 }
 
 template <int TYPE>

@@ -484,31 +484,37 @@ static hipError_t tile_launch(T8Product a, hipStream_t st) {
 // ---- Tiles: 256 x 256 by eight wavefronts, one workgroup a compute unit, or 128 x 128 by four, two.  The large one reads LDS half as often for a
 // product, the small one leaves fewer compute units without a tile.  Where there is no tile for each compute unit, so that nothing works beside a
 // workgroup while it waits for memory, 128 x 128 by eight with three slabs on their way (2048 x 1152 x 4608: 24.5 us, by four with two 26.7; 512 x 8192 x 8192
-// 43.6 / 59; with more tiles than compute units it loses: 4096 x 4608 x 1152 33.7 / 28.2).  us of a slab and of a tile's ends, by how much of the
-// chip is taken (measured at 16384 x 4608 x 128 - 4608, 16384 x 1152 x 4608 and 4096 x 8192 x 8192, and for the third form at those above):
+// 43.6 / 59; with more tiles than compute units it loses: 4096 x 4608 x 1152 33.7 / 28.2), and where there is none of half the size either, 64 x 128 by four
+// with three (1000 x 1152 x 1152 8.1, 256 x 8192 x 4096 18.2, the gradient of 300 x 2304 from 2304 12.4; 128 x 128 10.0 / 11.4, 22.4 / 24.0, 14.4 / 15.1).
+// us of a slab and of a tile's ends, by how much of the chip is taken (measured at 16384 x 4608 x 128 - 4608, 16384 x 1152 x 4608 and 4096 x 8192 x 8192,
+// and for the last two forms at those above):
 struct TileCost {
   int rows, cols, slots;
   float slab, ends, slab_rest, ends_rest;                  // all slots taken; half of them or fewer
 };
-constexpr TileCost LARGE = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL = {128, 128, 512, 0.93f, 3.2f, 0.72f, 2.5f},
-                   LONE = {128, 128, 256, 0.62f, 4.0f, 0.58f, 3.5f};
+constexpr TileCost LARGE = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL = {128, 128, 512, 0.93f, 3.2f, 0.68f, 4.5f},
+                   LONE = {128, 128, 256, 0.61f, 4.8f, 0.56f, 4.8f}, HALF = {64, 128, 256, 0.45f, 4.2f, 0.44f, 4.2f};
 
 static float tile_time(const TileCost &c, int64_t rows, int cols, int slabs) {
   const int64_t tiles = ((rows + c.rows - 1) / c.rows) * ((cols + c.cols - 1) / c.cols), rest = tiles % c.slots;
   const float full = c.slab * slabs + c.ends, last = rest == 0 ? 0.0f : rest > c.slots / 2 ? full : c.slab_rest * slabs + c.ends_rest;
   return (float)(tiles / c.slots) * full + last;
 }
-// the form that is soonest (four planes of a row need four row blocks, which the third form's wavefronts have not)
+// the form that is soonest (four planes of a row need four row blocks, which the last two forms' wavefronts have not)
 struct TileForm {
   const TileCost *cost;
   float time;
 };
 static TileForm tile_form(int64_t rows, int cols, int slabs, int planes) {
   TileForm f{&SMALL, tile_time(SMALL, rows, cols, slabs)};
-  const float large = tile_time(LARGE, rows, cols, slabs), lone = tile_time(LONE, rows, cols, slabs);
-  if (large < f.time) f = {&LARGE, large};
-  const int64_t tiles = ((rows + LONE.rows - 1) / LONE.rows) * ((cols + LONE.cols - 1) / LONE.cols);
-  if (planes < 4 && tiles <= LONE.slots && lone < f.time) f = {&LONE, lone};
+  const auto compare = [&](const TileCost &c) {
+    const float t = tile_time(c, rows, cols, slabs);
+    if (t < f.time) f = {&c, t};
+  };
+  const auto lone = [&](const TileCost &c) { return ((rows + c.rows - 1) / c.rows) * ((cols + c.cols - 1) / c.cols) <= c.slots; };
+  compare(LARGE);
+  if (planes < 4 && lone(LONE)) compare(LONE);
+  if (planes < 4 && lone(HALF)) compare(HALF);
   return f;
 }
 
@@ -523,6 +529,7 @@ static hipError_t tile_of(const T8Product &a, hipStream_t st) {
   if (c == &LARGE) return tile_launch<TYPE, P, false, 2, 2, 4, 8, 4>(a, st);
   if constexpr (P < 4) {
     if (c == &LONE) return tile_launch<TYPE, P, false, 3, 4, 2, 2, 4>(a, st);
+    if (c == &HALF) return tile_launch<TYPE, P, false, 3, 2, 2, 2, 4>(a, st);
   }
   return tile_launch<TYPE, P, false, 2, 2, 2, 4, 4>(a, st);
 }
