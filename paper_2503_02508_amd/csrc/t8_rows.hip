@@ -3,9 +3,9 @@
 // All of them move bytes: a row is read once, held in registers as float32 while its largest value is found, and written.  One wavefront
 // takes a row of up to 256 vectors of 16 bytes, a workgroup of 2 - 16 wavefronts a longer one (or a short one where there are few rows:
 // then nothing but latency counts), and rows beyond 16 wavefronts' registers are read again for each of the steps.
-// Kernels alone: codes of 16384 x 4608 bfloat16 37.3 us, 6.1 TB/s; of its gated rows 75.7 us, 5.0 TB/s (the instructions take 50 of them, and two wavefronts
-// in three wait); the norm of 16384 x 1152 bfloat16 with its residual 27.6 us, 4.8 TB/s; planes of 8192 x 4608 bfloat16 29.8 us, 5.1 TB/s; codes
-// read back, 16384 x 4608 to bfloat16, 36 us, 6.3 TB/s.  One row of 8192 takes 3.6 us, 77 of 4608 float32 3.4: a read, two reductions, a write.
+// Kernels alone: codes of 16384 x 4608 bfloat16 37.3 us, 6.1 TB/s; of its gated rows 73.6 us, 5.1 TB/s (the instructions take 60 of them); the norm of
+// 16384 x 1152 bfloat16 with its residual 26.8 us, 4.9 TB/s; planes of 8192 x 4608 bfloat16 29.8 us, 5.1 TB/s; codes read back, 16384 x 4608 to
+// bfloat16, 36 us, 6.3 TB/s.  One row of 8192 takes 3.6 us, 77 of 4608 float32 3.4: a read, two reductions, a write.
 //
 // Exact decisions.  The codes are those of the definition: float32 quotients, rounded half to even.  Each is formed as v (1 / scale), which is off by
 // at most 1.2e-5 for quotients of up to 127, and where it is nearer than 2e-5 to a border the division decides.  The gated product is
@@ -46,13 +46,24 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
   if (row >= a.M) return;
   const T *x = (const T *)a.x + row * a.ldx, *add = (const T *)a.add + row * a.lda;
   float v[C][VL], w[C][VL];
-  w4_u4 second[C];
+  w4_u4 first[C], second[C];
+  // Gated rows: a wavefront whose elements all exist loads them without the masks, one behind the other (16384 x 4608 bfloat16 77 -> 73.6 us, 8192 x 14336
+  // 114 -> 106; the other sources, whose instructions do not count, gain nothing: 16384 x 1152 float32 15.8 -> 17.3)
+  if (GATED && ((FULL ? wave : 0) + 1) * 64 * VL + (C - 1) * step <= a.K) {
 #pragma unroll
-  for (int c = 0; c < C; ++c) t8_load<TYPE>(x, e0 + c * step, a.K, v[c]);
-  if (GATED || (SOURCE == T8_NORM && a.add)) {
+    for (int c = 0; c < C; ++c) first[c] = *(const t8_u4 *)((const char *)x + (unsigned)(e0 + c * step) * (unsigned)sizeof(T));
 #pragma unroll
-    for (int c = 0; c < C; ++c) second[c] = t8_raw<TYPE>(add, e0 + c * step, a.K);
+    for (int c = 0; c < C; ++c) second[c] = *(const t8_u4 *)((const char *)add + (unsigned)(e0 + c * step) * (unsigned)sizeof(T));
+  } else {
+#pragma unroll
+    for (int c = 0; c < C; ++c) first[c] = t8_raw<TYPE>(x, e0 + c * step, a.K);
+    if (GATED || (SOURCE == T8_NORM && a.add)) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) second[c] = t8_raw<TYPE>(add, e0 + c * step, a.K);
+    }
   }
+#pragma unroll
+  for (int c = 0; c < C; ++c) t8_values<TYPE>(first[c], v[c]);
   if constexpr (SOURCE == T8_PLANES) {
 #pragma unroll
     for (int c = 0; c < C; ++c) t8_load_f32<VL>(a.w, e0 + c * step, a.K, w[c]);
