@@ -339,14 +339,13 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
   const auto finish = [&](const At &p, int turn) {
     const int col0 = p.n0 + wn;
     if constexpr (PART) {
-      int32_t *to = a.part + (int64_t)p.part * a.arows * a.K;
+      // as they lie in the registers: 1024 bytes a store
+      int32_t *to = a.part + (((int64_t)p.part * tiles + p.m0 / TM * a.tn + p.n0 / TN) * W + wave) * (MI * NI * 256) + lane * 4;
 #pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        const int r = p.m0 + wm + i * 16 + r16;
+      for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NI; ++j)
-          if (r < a.arows && col0 + j * 16 < a.K) *(t8_i4 *)(to + (int64_t)r * a.K + col0 + j * 16 + 4 * g) = acc[i][j];
-      }
+          if (p.m0 + wm + i * 16 < a.arows && col0 + j * 16 < a.K) *(t8_i4 *)(to + (i * NI + j) * 256) = acc[i][j];
     } else if ((P ? (p.m0 + TM) / (P ? P : 1) : p.m0 + TM) <= a.M && p.n0 + TN <= cols) {
       if (!GRAD && a.stream) rows_of(p, turn, std::true_type(), std::true_type());
       else rows_of(p, turn, std::true_type(), std::false_type());
@@ -426,19 +425,24 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
   }
 }
 
-// Parts of the planes' sums to the gradient: four columns of a row a thread, or 16 threads where there are many parts
-template <int TYPE, int Z>
+// Parts of the planes' sums to the gradient.  A thread has what one lane of a tile's wavefront had of a row block's planes, four columns of a row; or 16
+// threads share its parts where they are many
+template <int TYPE, int Z, int WM, int WN, int MI, int NI>
 __global__ __launch_bounds__(256) void t8_join_kernel(T8Product a) {
-  constexpr int P = t8_planes(TYPE), ITEMS = 256 / Z;
+  constexpr int P = t8_planes(TYPE), ITEMS = 256 / Z, W = WM * WN, TILE = W * MI * NI * 256;
   using T = typename W4Mem<TYPE>::T;
-  const int quads = a.K / 4, item = threadIdx.x % ITEMS, first = threadIdx.x / ITEMS;
-  const int64_t t = (int64_t)blockIdx.x * ITEMS + item;
-  const bool there = t < (int64_t)a.M * quads;
-  const int m = there ? (int)(t / quads) : 0, k = there ? (int)(t % quads) * 4 : 0;
+  const int item = threadIdx.x % ITEMS, first = threadIdx.x / ITEMS;
+  int64_t t = (int64_t)blockIdx.x * ITEMS + item;
+  const int lane = (int)(t % 64), j = (int)(t / 64 % NI), q = (int)(t / (64 * NI) % (MI / P)), wave = (int)(t / (64 * NI * (MI / P)) % W);
+  const int tile = (int)(t / (64 * NI * (MI / P) * W)), tm = tile / a.tn, tn = tile - tm * a.tn;
+  const int m = ((tm * WM + wave / WN) * (MI / P) + q) * 16 + lane % 16, k = ((tn * WN + wave % WN) * NI + j) * 16 + lane / 16 * 4;
+  const bool there = m < a.M && k < a.K;
+  const int32_t *from = a.part + (int64_t)tile * TILE + (wave * MI + q * P) * (NI * 256) + j * 256 + lane * 4;
   t8_i4 s[P] = {};
-  for (int z = first; z < a.split; z += Z)
+  if (there)
+    for (int z = first; z < a.split; z += Z)
 #pragma unroll
-    for (int p = 0; p < P; ++p) s[p] += *(const t8_i4 *)(a.part + ((int64_t)z * a.arows + t8_plane_row(m, p, P)) * a.K + k);
+      for (int p = 0; p < P; ++p) s[p] += *(const t8_i4 *)(from + (int64_t)z * a.tm * a.tn * TILE + p * (NI * 256));
   if constexpr (Z > 1) {
     __shared__ t8_i4 red[Z][P][ITEMS];
 #pragma unroll
@@ -559,9 +563,9 @@ static GradPlan grad_plan(int M, int N, int K, int type) {
     int split = (int)std::min<int64_t>(SMALL.slots / left, std::max(1, slabs / 2));
     const int per = (slabs + split - 1) / split;
     split = (slabs + per - 1) / per;
-    // a launch more, or two, and the sums' way to memory and back (8192 x 1152 from 4608, bfloat16: the last 117 tiles in four parts 27 us and 7
-    // for the join, no sooner than a round of them)
-    const float t = tile_time(c, whole, K, slabs) + SMALL.slab * per + SMALL.ends + 6.0f + (float)(left * split) * 65536.0f * 2.0f / 4e6f;
+    // a launch more, or two, and the sums' way to memory and back (kernels of 64 x 4096 from 14336 bfloat16 in 16 parts, 34 MB: 17.2 and 7.4 us; 100 x 1152 from
+    // 8192 float32 in 13, 25 MB: 13.7 and 6.5; 15 x 2640 from 8838 in 24, 8 MB: 11.4 and 4.0; the last tiles of 8192 x 1152 from 4608 no sooner than whole)
+    const float t = tile_time(c, whole, K, slabs) + SMALL.slab * per + SMALL.ends + 7.0f + (float)split * (float)rest * (float)K * 4.0f / 3.1e6f;
     if (split > 1 && t < time) {
       time = t;
       best.whole = whole;
@@ -574,7 +578,8 @@ static GradPlan grad_plan(int M, int N, int K, int type) {
 
 int64_t t8_grad_part_bytes(int M, int N, int K, int type) {
   const GradPlan p = grad_plan(M, N, K, type);
-  return p.split > 1 ? (int64_t)p.split * (p.arows - p.whole) * K * 4 : 0;
+  const int64_t tiles = (int64_t)((p.arows - p.whole + SMALL.rows - 1) / SMALL.rows) * ((K + SMALL.cols - 1) / SMALL.cols);
+  return p.split > 1 ? p.split * tiles * SMALL.rows * SMALL.cols * 4 : 0;
 }
 
 template <int TYPE>
@@ -599,9 +604,11 @@ static hipError_t grad_launch(T8Product a, hipStream_t st) {
   a.y = (typename W4Mem<TYPE>::T *)a.y + (int64_t)rows * a.ldy;
   const hipError_t e = tile_launch<TYPE, P, true, 2, 2, 2, 4, 4>(a, st);
   if (e != hipSuccess) return e;
-  const int64_t items = (int64_t)a.M * (a.K / 4);
-  if (a.split > 8) t8_join_kernel<TYPE, 16><<<(unsigned)((items + 15) / 16), 256, 0, st>>>(a);
-  else t8_join_kernel<TYPE, 1><<<(unsigned)((items + 255) / 256), 256, 0, st>>>(a);
+  a.tm = (a.arows + SMALL.rows - 1) / SMALL.rows;
+  a.tn = (a.K + SMALL.cols - 1) / SMALL.cols;
+  const unsigned items = (unsigned)a.tm * a.tn * (SMALL.rows * SMALL.cols / 4 / P);
+  if (a.split > 8) t8_join_kernel<TYPE, 16, 2, 2, 4, 4><<<items / 16, 256, 0, st>>>(a);
+  else t8_join_kernel<TYPE, 1, 2, 2, 4, 4><<<items / 256, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -360,7 +360,9 @@ PRODUCTS = [(1, 1, 16), (1, 17, 48), (2, 33, 144), (5, 100, 1168), (1, 700, 4608
             # fewer tiles than compute units and a long summed axis, in either direction
             (900, 515, 4112), (1100, 1000, 1168), (800, 4100, 1040), (700, 2900, 1200), (30, 4100, 4096),
             # gradients whose rows are longer than a workgroup's registers, in all types and in float32 alone
-            (5, 40000, 48), (40, 20000, 16)]
+            (5, 40000, 48), (40, 20000, 16),
+            # whole tiles, and a rest whose summed axis is split: in 16-bit types and in float32
+            (1851, 2965, 2208), (775, 2201, 2656)]
 
 
 def _codes(rng, M, K, pad):
