@@ -6,7 +6,7 @@
 // The weights' rows run along the summed axis in the forward product; in the gradient they run across it, and ds_read_b64_tr_b8 turns 8 rows x
 // 16 bytes on their way to the registers.
 // Workgroups stay and walk over the tiles: the slabs of the next tile are on their way while the last of this one are multiplied.
-// In the forward product a lane's columns are neighbours (block j's lane l has weight row 4 l + j), so that 16 lanes write whole lines of a
+// In the forward product a lane's columns are neighbours (of NI blocks, block j's lane l has weight row NI l + j), so that 16 lanes write whole lines of a
 // row without any exchange: trading words between lanes took 16384 x 4608 x 1152 from 88 to 100 us.  The transposed reads of the gradient cannot
 // permute columns; its operands are exchanged (weights first) and lanes trade words instead.
 // What bounds it: 4096 x 8192 x 8192 takes 218 - 238 us, 2.3 - 2.5 POP/s (the spread is the cards': their clocks fall to 2.15 GHz under it; on codes of
@@ -530,7 +530,12 @@ float t8_tile_time(int M, int N, int K) {
 template <int TYPE, int P>
 static hipError_t tile_of(const T8Product &a, hipStream_t st) {
   const TileCost *const c = tile_form(a.arows, P ? a.K : a.N, ((P ? a.N : a.K) + T8_BK - 1) / T8_BK, P).cost;
-  if (c == &LARGE) return tile_launch<TYPE, P, false, 2, 2, 4, 8, 4>(a, st);
+  if (c == &LARGE) {
+    // 64 x 128 a wavefront instead of 128 x 64: 16-bit results go out in 256 bytes a row (8192 x 8192 x 1152 84 -> 81 us, 8192 x 8192 x 8192 438 -> 433; float32
+    // and the gradients, which spill, lose)
+    if constexpr (P == 0 && TYPE != QC_TYPE_F32) return tile_launch<TYPE, P, false, 2, 4, 2, 4, 8>(a, st);
+    else return tile_launch<TYPE, P, false, 2, 2, 4, 8, 4>(a, st);
+  }
   if constexpr (P < 4) {
     if (c == &LONE) return tile_launch<TYPE, P, false, 3, 4, 2, 2, 4>(a, st);
     if (c == &HALF) return tile_launch<TYPE, P, false, 3, 2, 2, 2, 4>(a, st);
