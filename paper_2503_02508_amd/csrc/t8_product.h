@@ -23,10 +23,9 @@ template <int N>
 __device__ __forceinline__ void t8_wait_barrier() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void t8_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// A matrix instruction's 16 x 64 operand, rows of BK bytes in LDS: row r's 16-byte chunk c lies at place c ^ swz(r), so that eight rows of one
+// A matrix instruction's 16 x 64 operand, rows of 128 bytes in LDS: row r's 16-byte chunk c lies at place c ^ swz(r), so that eight rows of one
 // chunk lie in different banks
-template <int BK>
-__device__ __forceinline__ int t8_swz(int r) { return BK == 128 ? r & 7 : (r >> 1) & 3; }
+__device__ __forceinline__ int t8_swz(int r) { return r & 7; }
 
 // Values of P planes of sums: plane p counts 256^p
 template <int P>

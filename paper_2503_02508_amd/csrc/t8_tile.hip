@@ -170,7 +170,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
   };
 
   // ---- slabs to LDS: this lane's places in a wavefront's loads, row and chunk of what belongs there
-  const int lr = lane / 8, lc = (lane % 8) ^ t8_swz<BK>(lr);
+  const int lr = lane / 8, lc = (lane % 8) ^ t8_swz(lr);
   // forward: chunks of the last slab beyond K re-read its end, and become zeros on the activations' side
   const auto back = [&](int c) { return (unsigned)max((all - 1) * BK + c * 16 + 16 - a.K, 0); };
   // of the forward product's weights, block j's lane l has row NI l + j, so that a lane's columns are neighbours; they lie in LDS block by block (as
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
     const int valid = a.K % BK / 16;
     for (int t = threadIdx.x; t < TM * 8; t += 64 * W) {
       const int r = t / 8, c = t % 8;
-      if (c >= valid) *(w4_u4 *)(as + r * BK + ((c ^ t8_swz<BK>(r)) << 4)) = w4_u4{};
+      if (c >= valid) *(w4_u4 *)(as + r * BK + ((c ^ t8_swz(r)) << 4)) = w4_u4{};
     }
     t8_barrier();
   };
@@ -260,13 +260,13 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
         w[j] = t8_i4{lo[0], lo[1], hi[0], hi[1]};
       } else {
         const int r = wn + j * 16 + r16;
-        w[j] = *(const t8_i4 *)(bs + r * BK + (((kk * 4 + g) ^ t8_swz<BK>(r)) << 4));
+        w[j] = *(const t8_i4 *)(bs + r * BK + (((kk * 4 + g) ^ t8_swz(r)) << 4));
       }
     }
   };
   const auto read_x = [&](int stage, int kk, int i) {
     const int r = wm + i * 16 + r16;
-    return *(const t8_i4 *)(smem + stage * S::STAGE + r * BK + (((kk * 4 + g) ^ t8_swz<BK>(r)) << 4));
+    return *(const t8_i4 *)(smem + stage * S::STAGE + r * BK + (((kk * 4 + g) ^ t8_swz(r)) << 4));
   };
 
   using T = typename W4Mem<TYPE>::T;
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_ker
     for (int i = 0; i < MI; ++i) {
 #pragma unroll
       for (int j = 0; j < NI; ++j)
-        acc[i][j] = GRAD ? __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], af[i], acc[i][j], 0, 0, 0) : __builtin_amdgcn_mfma_i32_16x16x64_i8(af[i], w[j], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(GRAD ? w[j] : af[i], GRAD ? af[i] : w[j], acc[i][j], 0, 0, 0);
       af[i] = read_x(from, kk, i);
     }
     // in this order
