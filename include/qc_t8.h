@@ -99,10 +99,11 @@ int qc_t8_linear(const int8_t *qx, int64_t ldx, const float *x_scale, const int8
 
 /* Gradient of its input (of v, the row that the codes stand for); the weights are fixed:
  *   dx[m, k] = sum_n dy[m, n] w_scale[n] qw[n, k]
- * The scales vary along the summed axis, so that dy w_scale enters the product: as a fixed-point number of 16 bits (float16,
- * bfloat16) or 32 bits (float32) of the row's largest |dy w_scale|, whose bytes meet the weights' in exact integer sums.  The
- * rounding of one term is thus at most 1 / 65024 (2^-31.9) of the largest in its row, whatever its own size.  A row of
- * dy w_scale that is not finite gives NaN; one with nothing of 2^-100 or above may be taken for zeros.
+ * The scales vary along the summed axis, so that dy w_scale enters the product: the float32 product, as a fixed-point number of
+ * 24 bits (float16, bfloat16) or 32 bits (float32) of the row's largest |dy w_scale|, whose bytes meet the weights' in exact
+ * integer sums.  The rounding of one term is thus at most 2^-23.9 (2^-31.9) of the largest in its row, whatever its own size:
+ * beside an outlier a thousand times its size a term keeps 14 (22) bits.  A row of dy w_scale that is not finite gives NaN; one
+ * with nothing of 2^-100 or above may be taken for zeros.
  * dy: dev [M, N] of `type`; qw: as above; dx: dev [M, K] of `type`.  work: dev, at least qc_t8_linear_grad_bytes, 256-byte
  * aligned. */
 int qc_t8_linear_grad_bytes(int M, int N, int K, int type, size_t *bytes_out);

@@ -38,9 +38,10 @@ struct T8NormGradArgs {
   int waves;                // of a row
 };
 
-// T8_PLANES: bytes that stand for a gradient, and the rows of the matrix of planes.  Row m's plane p (the lowest byte is 0) is row
+// T8_PLANES: bytes that stand for a gradient, and the rows of the matrix of planes.  Three hold as much of the row's largest number as a float32 product
+// does (two left the others of a row with an outlier fewer bits than float16 has: 1 % off beside one of a thousand times their size).  Row m's plane p (the lowest byte is 0) is row
 // (m / 16 P + p) 16 + m % 16: the 16-row operands of a matrix instruction, a row block's planes one behind the other.
-constexpr int t8_planes(int type) { return type == QC_TYPE_F32 ? 4 : 2; }
+constexpr int t8_planes(int type) { return type == QC_TYPE_F32 ? 4 : 3; }
 __host__ __device__ inline int64_t t8_plane_row(int m, int p, int planes) { return ((int64_t)(m >> 4) * planes + p) * 16 + (m & 15); }
 
 struct T8Product {

@@ -158,17 +158,14 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
     constexpr int P = t8_planes(TYPE);
     const float most = __builtin_bit_cast(float, top);
     const bool empty = most < T8_EMPTY;
-    const double full = P == 2 ? 127.0 * 256.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
+    const double full = P == 3 ? 127.0 * 65536.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
     if (e0 == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / full);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       unsigned b[VL];
       int t[VL];
 #pragma unroll
-      for (int i = 0; i < VL; ++i) {
-        if constexpr (P == 2) t[i] = lost ? 0 : (int)__builtin_rintf(v[c][i] * (float)mult);
-        else t[i] = lost ? 0 : (int)__builtin_rint((double)v[c][i] * mult);
-      }
+      for (int i = 0; i < VL; ++i) t[i] = lost ? 0 : (int)__builtin_rint((double)v[c][i] * mult);
 #pragma unroll
       for (int p = 0; p < P; ++p) {
 #pragma unroll
@@ -318,11 +315,11 @@ __global__ __launch_bounds__(1024) void t8_long_rows_kernel(T8RowArgs a) {
       constexpr int P = t8_planes(TYPE);
       const float most = __builtin_bit_cast(float, top);
       const bool empty = most < T8_EMPTY;
-      const double full = P == 2 ? 127.0 * 256.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
+      const double full = P == 3 ? 127.0 * 65536.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
       if (threadIdx.x == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / full);
       for (int e = threadIdx.x; e < a.pitch; e += 1024) {
         int t = 0;
-        if (!lost && e < a.K) t = P == 2 ? (int)__builtin_rintf(value(e) * (float)mult) : (int)__builtin_rint((double)value(e) * mult);
+        if (!lost && e < a.K) t = (int)__builtin_rint((double)value(e) * mult);
         for (int p = 0; p < P; ++p) {
           a.q[t8_plane_row((int)row, p, P) * a.pitch + e] = (int8_t)t;
           t = (t >> 8) + ((t >> 7) & 1);

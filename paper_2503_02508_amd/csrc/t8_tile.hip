@@ -19,11 +19,11 @@ namespace qc {
 
 constexpr int T8_BK = 128;
 
-template <int ST, int WM, int WN, int MI, int NI>
+template <bool GRAD, int ST, int WM, int WN, int MI, int NI>
 struct T8Tile {
   static constexpr int W = WM * WN, TM = WM * MI * 16, TN = WN * NI * 16;
   static constexpr int ABYTES = TM * T8_BK, BBYTES = TN * T8_BK, STAGE = ABYTES + BBYTES, RING = ST * STAGE;
-  static constexpr int SCALES = (TM + 2 * TN) * 4, LDS = RING + 2 * SCALES;              // of two tiles: scales of rows and columns, biases
+  static constexpr int SCALES = GRAD ? 0 : (TM + 2 * TN) * 4, LDS = RING + 2 * SCALES;   // of two tiles: scales of rows and columns, biases
   static constexpr int LA = ABYTES / 1024 / W, LB = BBYTES / 1024 / W, L = LA + LB;      // loads of a wavefront
   static constexpr int PER_CU = 160 * 1024 / LDS < 2 ? 1 : 2;
   static_assert(ABYTES % (1024 * W) == 0 && BBYTES % (1024 * W) == 0, "whole loads");
@@ -111,7 +111,7 @@ __device__ __forceinline__ void t8_rows_out(const w4_f4 v[NI], int lane, typenam
 // P: 0 the forward product, else planes of a gradient.  PART: sums to the workspace.
 template <int TYPE, int P, bool PART, int ST, int WM, int WN, int MI, int NI>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN > 4 ? 1 : 2) void t8_tile_kernel(T8Product a) {
-  using S = T8Tile<ST, WM, WN, MI, NI>;
+  using S = T8Tile<(P > 0), ST, WM, WN, MI, NI>;
   constexpr int W = S::W, TM = S::TM, TN = S::TN, BK = T8_BK, L = S::L;
   static_assert(ST == 2 || ST == 3, "waits for the next of two or three slabs");
   constexpr bool GRAD = P > 0;
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(256) void t8_join_kernel(T8Product a) {
 
 template <int TYPE, int P, bool PART, int ST, int WM, int WN, int MI, int NI>
 static hipError_t tile_launch(T8Product a, hipStream_t st) {
-  using S = T8Tile<ST, WM, WN, MI, NI>;
+  using S = T8Tile<(P > 0), ST, WM, WN, MI, NI>;
   a.tm = (a.arows + S::TM - 1) / S::TM;
   a.tn = ((P ? a.K : a.N) + S::TN - 1) / S::TN;
   // results of whole lines that outgrow the L2 caches stream past them (16384 x 4608 x 1152 bfloat16, 151 MB: 103 -> 97 us; 4096 rows, 38 MB: 32.7 ->
@@ -489,36 +489,46 @@ static hipError_t tile_launch(T8Product a, hipStream_t st) {
 // product, the small one leaves fewer compute units without a tile.  Where there is no tile for each compute unit, so that nothing works beside a
 // workgroup while it waits for memory, 128 x 128 by eight with three slabs on their way (2048 x 1152 x 4608: 24.5 us, by four with two 26.7; 512 x 8192 x 8192
 // 43.6 / 59; with more tiles than compute units it loses: 4096 x 4608 x 1152 33.7 / 28.2), and where there is none of half the size either, 64 x 128 by four
-// with three (1000 x 1152 x 1152 8.1, 256 x 8192 x 4096 18.2, the gradient of 300 x 2304 from 2304 12.4; 128 x 128 10.0 / 11.4, 22.4 / 24.0, 14.4 / 15.1).
+// with three (1000 x 1152 x 1152 8.1, 256 x 8192 x 4096 18.2; 128 x 128 10.0 / 11.4, 22.4 / 24.0).
+// Three planes of a row need three row blocks, so that tiles have 192 or 96 rows of planes: 192 x 128 by four, two workgroups a compute unit (8192 x 1152 from
+// 4608: 129 us; 192 x 256 by eight 157, and at 2048 x 8192 from 8192 366 / 373), where they are few 96 x 128, two workgroups (1000 x 1152 from 4608: 31 us, 192 x 128 34),
+// and where those are fewer than compute units one with three slabs on their way (128 x 8192 from 8192: 42 us, two 47).  Four need four: the first two.
 // us of a slab and of a tile's ends, by how much of the chip is taken (measured at 16384 x 4608 x 128 - 4608, 16384 x 1152 x 4608 and 4096 x 8192 x 8192,
-// and for the last two forms at those above):
+// and for LONE and HALF at those above; three planes: all slots and half of them, 1152 and 4608 deep):
 struct TileCost {
-  int rows, cols, slots;
+  int rows, cols, slots;                                   // 0 rows: there is no such form
   float slab, ends, slab_rest, ends_rest;                  // all slots taken; half of them or fewer
 };
-constexpr TileCost LARGE = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL = {128, 128, 512, 0.93f, 3.2f, 0.68f, 4.5f},
-                   LONE = {128, 128, 256, 0.61f, 4.8f, 0.56f, 4.8f}, HALF = {64, 128, 256, 0.45f, 4.2f, 0.44f, 4.2f};
+enum { LARGE, SMALL, LONE, HALF };                         // the last two where no slot has more than one tile
+struct TileCosts {
+  TileCost form[4];
+  int parts;                                               // the form of gradients' parts
+};
+constexpr TileCost LARGE_COST = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL_COST = {128, 128, 512, 0.93f, 3.2f, 0.68f, 4.5f};
+constexpr TileCosts FORWARD = {{LARGE_COST, SMALL_COST, {128, 128, 256, 0.61f, 4.8f, 0.56f, 4.8f}, {64, 128, 256, 0.45f, 4.2f, 0.44f, 4.2f}}, 0},
+                    THREE = {{{}, {192, 128, 512, 1.40f, 5.7f, 0.83f, 5.0f}, {96, 128, 512, 0.87f, 4.0f, 0.60f, 3.9f}, {96, 128, 256, 0.58f, 3.8f, 0.57f, 3.4f}}, LONE},
+                    FOUR = {{LARGE_COST, SMALL_COST, {}, {}}, SMALL};
+constexpr const TileCosts &tile_costs(int planes) { return planes == 0 ? FORWARD : planes == 3 ? THREE : FOUR; }
 
 static float tile_time(const TileCost &c, int64_t rows, int cols, int slabs) {
   const int64_t tiles = ((rows + c.rows - 1) / c.rows) * ((cols + c.cols - 1) / c.cols), rest = tiles % c.slots;
   const float full = c.slab * slabs + c.ends, last = rest == 0 ? 0.0f : rest > c.slots / 2 ? full : c.slab_rest * slabs + c.ends_rest;
   return (float)(tiles / c.slots) * full + last;
 }
-// the form that is soonest (four planes of a row need four row blocks, which the last two forms' wavefronts have not)
+// the form that is soonest
 struct TileForm {
-  const TileCost *cost;
+  int form;
   float time;
 };
 static TileForm tile_form(int64_t rows, int cols, int slabs, int planes) {
-  TileForm f{&SMALL, tile_time(SMALL, rows, cols, slabs)};
-  const auto compare = [&](const TileCost &c) {
+  const TileCosts &costs = tile_costs(planes);
+  TileForm f{SMALL, tile_time(costs.form[SMALL], rows, cols, slabs)};
+  for (const int form : {LARGE, LONE, HALF}) {
+    const TileCost &c = costs.form[form];
+    if (c.rows == 0 || (form != LARGE && ((rows + c.rows - 1) / c.rows) * ((cols + c.cols - 1) / c.cols) > c.slots)) continue;
     const float t = tile_time(c, rows, cols, slabs);
-    if (t < f.time) f = {&c, t};
-  };
-  const auto lone = [&](const TileCost &c) { return ((rows + c.rows - 1) / c.rows) * ((cols + c.cols - 1) / c.cols) <= c.slots; };
-  compare(LARGE);
-  if (planes < 4 && lone(LONE)) compare(LONE);
-  if (planes < 4 && lone(HALF)) compare(HALF);
+    if (t < f.time) f = {form, t};
+  }
   return f;
 }
 
@@ -529,18 +539,24 @@ float t8_tile_time(int M, int N, int K) {
 
 template <int TYPE, int P>
 static hipError_t tile_of(const T8Product &a, hipStream_t st) {
-  const TileCost *const c = tile_form(a.arows, P ? a.K : a.N, ((P ? a.N : a.K) + T8_BK - 1) / T8_BK, P).cost;
-  if (c == &LARGE) {
-    // 64 x 128 a wavefront instead of 128 x 64: 16-bit results go out in 256 bytes a row (8192 x 8192 x 1152 84 -> 81 us, 8192 x 8192 x 8192 438 -> 433; float32
-    // and the gradients, which spill, lose)
-    if constexpr (P == 0 && TYPE != QC_TYPE_F32) return tile_launch<TYPE, P, false, 2, 4, 2, 4, 8>(a, st);
-    else return tile_launch<TYPE, P, false, 2, 2, 4, 8, 4>(a, st);
+  const int form = tile_form(a.arows, P ? a.K : a.N, ((P ? a.N : a.K) + T8_BK - 1) / T8_BK, P).form;
+  if constexpr (P == 3) {
+    if (form == LONE) return tile_launch<TYPE, P, false, 2, 2, 2, 3, 4>(a, st);
+    if (form == HALF) return tile_launch<TYPE, P, false, 3, 2, 2, 3, 4>(a, st);
+    return tile_launch<TYPE, P, false, 2, 2, 2, 6, 4>(a, st);
+  } else {
+    if (form == LARGE) {
+      // 64 x 128 a wavefront instead of 128 x 64: 16-bit results go out in 256 bytes a row (8192 x 8192 x 1152 84 -> 81 us, 8192 x 8192 x 8192 438 -> 433;
+      // float32 and the gradients, which spill, lose)
+      if constexpr (P == 0 && TYPE != QC_TYPE_F32) return tile_launch<TYPE, P, false, 2, 4, 2, 4, 8>(a, st);
+      else return tile_launch<TYPE, P, false, 2, 2, 4, 8, 4>(a, st);
+    }
+    if constexpr (P == 0) {
+      if (form == LONE) return tile_launch<TYPE, P, false, 3, 4, 2, 2, 4>(a, st);
+      if (form == HALF) return tile_launch<TYPE, P, false, 3, 2, 2, 2, 4>(a, st);
+    }
+    return tile_launch<TYPE, P, false, 2, 2, 2, 4, 4>(a, st);
   }
-  if constexpr (P < 4) {
-    if (c == &LONE) return tile_launch<TYPE, P, false, 3, 4, 2, 2, 4>(a, st);
-    if (c == &HALF) return tile_launch<TYPE, P, false, 3, 2, 2, 2, 4>(a, st);
-  }
-  return tile_launch<TYPE, P, false, 2, 2, 2, 4, 4>(a, st);
 }
 
 hipError_t launch_t8_tile(const T8Product &a, int type, hipStream_t st) {
@@ -560,17 +576,21 @@ static GradPlan grad_plan(int M, int N, int K, int type) {
   GradPlan best{(M + 15) / 16 * 16 * P, 0, 1, slabs};
   best.whole = best.arows;
   float time = tile_form(best.arows, K, slabs, P).time;
-  for (const TileCost &c : {LARGE, SMALL}) {
+  const TileCosts &costs = tile_costs(P);
+  const TileCost &part = costs.form[costs.parts];
+  for (const int form : {LARGE, SMALL}) {
+    const TileCost &c = costs.form[form];
+    if (c.rows == 0) continue;
     const int64_t tn = (K + c.cols - 1) / c.cols, tiles = (best.arows + c.rows - 1) / c.rows * tn;
     const int whole = (int)(tiles / c.slots * c.slots / tn * c.rows), rest = best.arows - whole;
-    const int64_t left = (int64_t)((rest + SMALL.rows - 1) / SMALL.rows) * ((K + SMALL.cols - 1) / SMALL.cols);
-    if (left == 0 || left > SMALL.slots / 2) continue;
-    int split = (int)std::min<int64_t>(SMALL.slots / left, std::max(1, slabs / 2));
+    const int64_t left = (int64_t)((rest + part.rows - 1) / part.rows) * ((K + part.cols - 1) / part.cols);
+    if (left == 0 || left > part.slots / 2) continue;
+    int split = (int)std::min<int64_t>(part.slots / left, std::max(1, slabs / 2));
     const int per = (slabs + split - 1) / split;
     split = (slabs + per - 1) / per;
     // a launch more, or two, and the sums' way to memory and back (kernels of 64 x 4096 from 14336 bfloat16 in 16 parts, 34 MB: 17.2 and 7.4 us; 100 x 1152 from
     // 8192 float32 in 13, 25 MB: 13.7 and 6.5; 15 x 2640 from 8838 in 24, 8 MB: 11.4 and 4.0; the last tiles of 8192 x 1152 from 4608 no sooner than whole)
-    const float t = tile_time(c, whole, K, slabs) + SMALL.slab * per + SMALL.ends + 7.0f + (float)split * (float)rest * (float)K * 4.0f / 3.1e6f;
+    const float t = tile_time(c, whole, K, slabs) + part.slab * per + part.ends + 7.0f + (float)split * (float)rest * (float)K * 4.0f / 3.1e6f;
     if (split > 1 && t < time) {
       time = t;
       best.whole = whole;
@@ -583,8 +603,10 @@ static GradPlan grad_plan(int M, int N, int K, int type) {
 
 int64_t t8_grad_part_bytes(int M, int N, int K, int type) {
   const GradPlan p = grad_plan(M, N, K, type);
-  const int64_t tiles = (int64_t)((p.arows - p.whole + SMALL.rows - 1) / SMALL.rows) * ((K + SMALL.cols - 1) / SMALL.cols);
-  return p.split > 1 ? p.split * tiles * SMALL.rows * SMALL.cols * 4 : 0;
+  const TileCosts &costs = tile_costs(t8_planes(type));
+  const TileCost &part = costs.form[costs.parts];
+  const int64_t tiles = (int64_t)((p.arows - p.whole + part.rows - 1) / part.rows) * ((K + part.cols - 1) / part.cols);
+  return p.split > 1 ? p.split * tiles * part.rows * part.cols * 4 : 0;
 }
 
 template <int TYPE>
@@ -607,13 +629,15 @@ static hipError_t grad_launch(T8Product a, hipStream_t st) {
   a.a += (int64_t)p.whole * a.lda;
   a.xs += rows;
   a.y = (typename W4Mem<TYPE>::T *)a.y + (int64_t)rows * a.ldy;
-  const hipError_t e = tile_launch<TYPE, P, true, 2, 2, 2, 4, 4>(a, st);
+  constexpr TileCost part = tile_costs(P).form[tile_costs(P).parts];
+  constexpr int MI = part.rows / 32;
+  const hipError_t e = tile_launch<TYPE, P, true, 2, 2, 2, MI, 4>(a, st);
   if (e != hipSuccess) return e;
-  a.tm = (a.arows + SMALL.rows - 1) / SMALL.rows;
-  a.tn = (a.K + SMALL.cols - 1) / SMALL.cols;
-  const unsigned items = (unsigned)a.tm * a.tn * (SMALL.rows * SMALL.cols / 4 / P);
-  if (a.split > 8) t8_join_kernel<TYPE, 16, 2, 2, 4, 4><<<items / 16, 256, 0, st>>>(a);
-  else t8_join_kernel<TYPE, 1, 2, 2, 4, 4><<<items / 256, 256, 0, st>>>(a);
+  a.tm = (a.arows + part.rows - 1) / part.rows;
+  a.tn = (a.K + part.cols - 1) / part.cols;
+  const unsigned items = (unsigned)a.tm * a.tn * (part.rows * part.cols / 4 / P);
+  if (a.split > 8) t8_join_kernel<TYPE, 16, 2, 2, MI, 4><<<items / 16, 256, 0, st>>>(a);
+  else t8_join_kernel<TYPE, 1, 2, 2, MI, 4><<<items / 256, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 

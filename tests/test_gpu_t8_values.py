@@ -1,0 +1,32 @@
+"""8-bit layers with a scale for each token (include/qc_t8.h) on values of very different sizes, against the float64 oracle: outliers within a row,
+the ends of the types' ranges.  (e = 2^-24, half a float32 step; helpers and the other tolerances: test_gpu_t8.py)"""
+import numpy as np
+import pytest
+
+from oracle import t8 as O
+from test_gpu_t8 import E, EPS, PRODUCTS, _check, _dev, _np, _rows, _same_codes, _type, _untouched, qc  # noqa: F401  (qc: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+def test_linear_grad_beside_an_outlier(qc, M, N, K, t):  # noqa: F811
+    """One gradient of a row a thousand times the others, and columns that it does not reach (its weights there are 0): what is left there are the
+    others.  A term dy w_s is a float32 product (e of itself) and a number of 24 bits of its row's largest (half a step of 1 / (127 2^16): 1.01 e
+    of the largest); the integer sum and its float64 product with the scale are off by the scale's e: 4 e of the terms are counted."""
+    import torch
+    rng = np.random.default_rng(M + 2 * N + 3 * K)
+    dy = 0.01 * rng.standard_normal((M, N))
+    qw = rng.integers(-128, 128, (N, K)).astype(np.int8)
+    out = int(rng.integers(0, N))
+    dy[:, out] *= 1000
+    qw[out, rng.permutation(K)[:K // 2]] = 0
+    ws = rng.uniform(0.005, 0.01, N).astype(np.float32)
+    d, _ = _rows(M, N, _type(t), 3, 1, _dev(dy).to(_type(t)))
+    dx, buf = _rows(M, K, _type(t), 5, 2)
+    work = torch.full((qc.qc_t8_linear_grad_bytes(M, N, K, _type(t)),), 255, dtype=torch.uint8, device="cuda")
+    qc.qc_t8_linear_grad(d, _dev(qw), _dev(ws), dx, work)
+    v, aq = np.abs(_np(d) * ws), np.abs(qw.astype(np.float64))
+    _check(dx, O.linear_grad(_np(d), qw, ws), 1.01 * E * v.max(1, keepdims=True) * aq.sum(0) + 4 * E * (v @ aq), t, t)
+    assert _untouched(dx, buf)
