@@ -39,8 +39,9 @@ struct T8NormGradArgs {
 };
 
 // T8_PLANES: bytes that stand for a gradient, and the rows of the matrix of planes.  Three hold as much of the row's largest number as a float32 product
-// does (two left the others of a row with an outlier fewer bits than float16 has: 1 % off beside one of a thousand times their size).  Row m's plane p (the lowest byte is 0) is row
-// (m / 16 P + p) 16 + m % 16: the 16-row operands of a matrix instruction, a row block's planes one behind the other.
+// does (two left the others of a row with an outlier fewer bits than float16 has: 1 % off beside one of a thousand times their size).
+// Row m's plane p (the lowest byte is 0) is row (m / 16 P + p) 16 + m % 16: the 16-row operands of a matrix instruction, a row block's planes one
+// behind the other.
 constexpr int t8_planes(int type) { return type == QC_TYPE_F32 ? 4 : 3; }
 __host__ __device__ inline int64_t t8_plane_row(int m, int p, int planes) { return ((int64_t)(m >> 4) * planes + p) * 16 + (m & 15); }
 
@@ -242,7 +243,8 @@ __device__ __forceinline__ void t8_logistic(int act, float gate, float &s, float
   o = u < 0.0 ? r : z * r;
 }
 // act(gate) x by the same formula without the cases, for gates above T8_DEEP: to 1.8e-6 of its value.  The logistic function is
-// 1 / (1 + exp(-t)), which keeps the digits of small values; beyond LIMIT it is 0 or 1 to any product.  An infinite or NaN gate gives an infinite or NaN product.
+// 1 / (1 + exp(-t)), which keeps the digits of small values; above LIMIT it is 1, below -LIMIT it is what it is there: too large, so that products of gates
+// below T8_DEEP are not to be used.  An infinite or NaN gate gives an infinite or NaN product.
 template <int ACT>
 __device__ __forceinline__ float t8_gate(float gate, float x) {
   constexpr float LIMIT = ACT == QC_ACT_SILU ? 85.0f : 9.9f;             // exp(-t) up to 2^123

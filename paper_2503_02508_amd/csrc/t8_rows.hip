@@ -121,8 +121,15 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
         least = fminf(least, g[i]);
       }
       if (least < T8_DEEP<ACT>) {
+        // (until then they are nothing: a gate at its type's lowest value would be the row's largest.  What is not finite stays.)
+        float f[VL];
+        t8_values<TYPE>(first[c], f);
 #pragma unroll
-        for (int i = 0; i < VL; ++i) deep |= g[i] < T8_DEEP<ACT> ? 1u << (c * VL + i) : 0u;
+        for (int i = 0; i < VL; ++i)
+          if (g[i] < T8_DEEP<ACT>) {
+            deep |= 1u << (c * VL + i);
+            if (t8_mag(g[i]) < 0x7F800000u && t8_mag(f[i]) < 0x7F800000u) v[c][i] = 0.0f;
+          }
       }
     }
   }

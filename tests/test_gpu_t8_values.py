@@ -30,3 +30,37 @@ def test_linear_grad_beside_an_outlier(qc, M, N, K, t):  # noqa: F811
     v, aq = np.abs(_np(d) * ws), np.abs(qw.astype(np.float64))
     _check(dx, O.linear_grad(_np(d), qw, ws), 1.01 * E * v.max(1, keepdims=True) * aq.sum(0) + 4 * E * (v @ aq), t, t)
     assert _untouched(dx, buf)
+
+
+def _gated(qc, x, g, act, t):
+    """Codes and scales of rows, against the oracle's."""
+    import torch
+    xt, gt = _dev(x).to(_type(t)), _dev(g).to(_type(t))
+    q, s = torch.full(x.shape, 55, dtype=torch.int8, device="cuda"), torch.empty(len(x), device="cuda")
+    qc.qc_t8_quantize(xt, q, s, gate=gt, act=qc.QC_ACT_SILU if act == "silu" else qc.QC_ACT_GELU)
+    with np.errstate(over="ignore"):
+        _same_codes(q, s, O.gated(_np(xt), _np(gt), act), "%s %s" % (act, t))
+    return s
+
+
+# a wavefront a row, one vector a lane and four; a workgroup a row; rows that are read again
+GATED_WIDTHS = [64, 300, 1000, 4608, 40000]
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("K", GATED_WIDTHS)
+def test_gates_at_the_types_lowest_value_beside_ordinary_ones(qc, K, act, t):  # noqa: F811
+    """act(gate) is 0 or next to it whatever x is: what such an element makes of its row is nothing."""
+    import torch
+    rng = np.random.default_rng(K)
+    rows = 2100 if K == 300 else 9                           # (2100: one wavefront a row whatever the width)
+    x, g = rng.standard_normal((rows, K)), rng.standard_normal((rows, K))
+    lowest = float(torch.finfo(_type(t)).min)
+    at = rng.integers(0, K, rows)
+    far = [(lowest, 1.0), (lowest, 3e38), (-1e36, 1.0), (-1e38, 1e38), (-100.0, 3e38), (-100.0, -1e36), (-86.0, 1e37), (-20.0, 3e38)]
+    for m in range(rows - 1):                                 # the last row has none
+        g[m, at[m]], x[m, at[m]] = far[m % len(far)]
+    g[0, K // 2:] = lowest                                    # a masked half
+    s = _gated(qc, x, g, act, t)
+    assert torch.isfinite(s).all()
