@@ -259,7 +259,9 @@ __device__ __forceinline__ float t8_gate(float gate, float x) {
     lo = (float)(u - (double)hi) * 0.6931471805599453f;
   }
   const float e = __builtin_amdgcn_exp2f(hi);
-  return gate * __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, lo, e)) * x;
+  // (the gate last: a subnormal one times the logistic function would have lost its digits when a large x brings it back.  A subnormal x meets a
+  // logistic function below 1 only where the gate, and with it the product, is small.)
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, lo, e)) * x * gate;
 }
 template <int ACT>
 constexpr float T8_DEEP = ACT == QC_ACT_SILU ? -69.0f : -9.0f;       // exp(-t) = 2^100, about

@@ -197,7 +197,7 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
         const float near = __builtin_bit_cast(float, top) * (1.0f - 5e-6f);
 #pragma unroll
         for (int c = 0; c < C; ++c)
-          if (tops[c] >= near) {
+          if (tiny || tops[c] >= near) {
 #pragma unroll
             for (int i = 0; i < VL; ++i) flags |= (tiny ? e0 + c * step + i < width : fabsf(v[c][i]) >= near) ? 1u << (c * VL + i) : 0u;
           }

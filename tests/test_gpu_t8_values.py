@@ -64,3 +64,31 @@ def test_gates_at_the_types_lowest_value_beside_ordinary_ones(qc, K, act, t):  #
     g[0, K // 2:] = lowest                                    # a masked half
     s = _gated(qc, x, g, act, t)
     assert torch.isfinite(s).all()
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("K", GATED_WIDTHS)
+def test_gated_rows_of_subnormal_factors(qc, K, act, t):  # noqa: F811
+    """Products of a subnormal gate (or row) and a large factor: a float32 product that is rounded on its way among the subnormal numbers has lost its
+    digits when the other factor brings it back."""
+    rng = np.random.default_rng(K + 1)
+    step = 2.0 ** (-149 if t == "f32" else -133)              # the type's least number
+    x, g = rng.standard_normal((12, K)), rng.standard_normal((12, K))
+    at = rng.integers(0, K // 2, 12)
+    for m, (size, gate, factor) in enumerate([(1e-14, 3, 2.0 ** 127), (1e-14, 1, 2.0 ** 127), (1e-14, -5, 2.0 ** 127), (1e-15, 7, -2.0 ** 125), (0, 1, 2.0 ** 127),
+                                              (1e-12, 11, 2.0 ** 127)]):
+        x[m] *= size if t == "f32" else size * 2.0 ** 16
+        g[m, at[m]], x[m, at[m]] = gate * step, factor
+    # rows of nothing but subnormal products: gates, then rows
+    g[6], x[6] = np.round(g[6] * 1000) * step, x[6] * 1000
+    g[7], x[7] = np.round(g[7] * 30) * step, 2.0 ** 20
+    g[8], x[8] = g[8] * 8, np.round(x[8] * 1000) * step
+    # two elements that are nearly the largest: which one is, the nearer of the approximations does not know
+    if t == "f32":
+        for m, (a, b) in ((9, ((1001 * step, 1024.0), (100.0, 5122 * step))), (10, ((9.0, 4086 * step), (36766.0, step))),
+                             (11, ((3.5, 3103 * step), (10858.0, step)))):
+            x[m] = 0
+            g[m, at[m]], x[m, at[m]] = a
+            g[m, K - 2], x[m, K - 2] = b
+    _gated(qc, x, g, act, t)
