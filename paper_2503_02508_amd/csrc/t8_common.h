@@ -43,6 +43,8 @@ struct T8NormGradArgs {
 // Row m's plane p (the lowest byte is 0) is row (m / 16 P + p) 16 + m % 16: the 16-row operands of a matrix instruction, a row block's planes one
 // behind the other.
 constexpr int t8_planes(int type) { return type == QC_TYPE_F32 ? 4 : 3; }
+// A row's scale counts its number's high bytes from the third on, so that it is a normal float32 for all rows that are kept (most / 127 2^24 would not be)
+constexpr double T8_PLANE_TOP = 127.0 * 65536.0;
 __host__ __device__ inline int64_t t8_plane_row(int m, int p, int planes) { return ((int64_t)(m >> 4) * planes + p) * 16 + (m & 15); }
 
 struct T8Product {

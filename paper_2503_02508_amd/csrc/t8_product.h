@@ -27,13 +27,14 @@ __device__ __forceinline__ void t8_barrier() { asm volatile("s_waitcnt lgkmcnt(0
 // chunk lie in different banks
 __device__ __forceinline__ int t8_swz(int r) { return r & 7; }
 
-// Values of P planes of sums: plane p counts 256^p.  (float64: sums of two planes may cancel to less than either's float32 rounding)
+// Values of P planes of sums: plane p counts 256^(p + 3 - P) of the row's scale.  (float64: sums of two planes may cancel to less than either's float32
+// rounding)
 template <int P>
 __device__ __forceinline__ float t8_join(const int s[P], float scale) {
   double v = (double)s[P - 1];
 #pragma unroll
   for (int p = P - 2; p >= 0; --p) v = __builtin_fma(v, 256.0, (double)s[p]);
-  return (float)(v * (double)scale);
+  return (float)(v * ((double)scale * (P == 4 ? 0x1p-8 : 1.0)));
 }
 
 }  // namespace qc

@@ -165,8 +165,8 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
     constexpr int P = t8_planes(TYPE);
     const float most = __builtin_bit_cast(float, top);
     const bool empty = most < T8_EMPTY;
-    const double full = P == 3 ? 127.0 * 65536.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
-    if (e0 == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / full);
+    const double full = P == 3 ? T8_PLANE_TOP : T8_PLANE_TOP * 256.0, mult = lost || empty ? 0.0 : full / (double)most;
+    if (e0 == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / T8_PLANE_TOP);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       unsigned b[VL];
@@ -322,8 +322,8 @@ __global__ __launch_bounds__(1024) void t8_long_rows_kernel(T8RowArgs a) {
       constexpr int P = t8_planes(TYPE);
       const float most = __builtin_bit_cast(float, top);
       const bool empty = most < T8_EMPTY;
-      const double full = P == 3 ? 127.0 * 65536.0 : 127.0 * 16777216.0, mult = lost || empty ? 0.0 : full / (double)most;
-      if (threadIdx.x == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / full);
+      const double full = P == 3 ? T8_PLANE_TOP : T8_PLANE_TOP * 256.0, mult = lost || empty ? 0.0 : full / (double)most;
+      if (threadIdx.x == 0) a.scale[row] = lost ? __builtin_nanf("") : empty ? 0.0f : (float)((double)most / T8_PLANE_TOP);
       for (int e = threadIdx.x; e < a.pitch; e += 1024) {
         int t = 0;
         if (!lost && e < a.K) t = (int)__builtin_rint((double)value(e) * mult);

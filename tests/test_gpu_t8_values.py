@@ -92,3 +92,20 @@ def test_gated_rows_of_subnormal_factors(qc, K, act, t):  # noqa: F811
             g[m, at[m]], x[m, at[m]] = a
             g[m, K - 2], x[m, K - 2] = b
     _gated(qc, x, g, act, t)
+
+
+@pytest.mark.parametrize("N", [3, 5, 40, 700, 20000])
+def test_linear_grad_of_small_float32_rows(qc, N):  # noqa: F811
+    """Rows whose largest dy w_s lies between 2^-100, below which they may be zeros, and 2^-94.  No term is of another sign than the others, so
+    that the result's error is its terms': a float32 product (e), 32 bits of the row's largest, the scale and the last product (4 e)."""
+    import torch
+    rng = np.random.default_rng(N)
+    M, K = 300, 48
+    dy = rng.uniform(0.5, 1, (M, N)) * 2.0 ** rng.uniform(-99, -94, (M, 1))
+    ws = np.ones(N, np.float32)
+    qw = rng.integers(1, 128, (N, K)).astype(np.int8)
+    d, dx = _dev(dy.astype(np.float32)), torch.empty((M, K), device="cuda")
+    work = torch.empty(qc.qc_t8_linear_grad_bytes(M, N, K, torch.float32), dtype=torch.uint8, device="cuda")
+    qc.qc_t8_linear_grad(d, _dev(qw), _dev(ws), dx, work)
+    v, aq = _np(d), qw.astype(np.float64)
+    _check(dx, O.linear_grad(v, qw, ws), 1.01 * 2.0 ** -32 * v.max(1, keepdims=True) * aq.sum(0) + 4 * E * (v @ aq), "f32", "N %d" % N)
