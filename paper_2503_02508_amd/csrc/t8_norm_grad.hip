@@ -1,5 +1,7 @@
 // Gradient of the root-mean-square norm of rows:
 //   dx = rho (g - h rho^2 mean(g h)) + dh,  g = dy weight;   dweight = sum over the rows of dy h rho
+// as rho g - (h rho) (rho^2 mean(g h)): h rho is of the size of 1 and the other factor of that of the result, where rho^3 mean(g h) of large rows would
+// be below any float32.
 // A row's h and dy are read once and stay in registers while its two sums are formed, so that the kernel moves what it has to: h, dy, dh in,
 // dx out.  A workgroup walks rows M / groups apart and keeps its columns' part of dweight in registers from row to row; the groups' parts
 // go to the workspace, and a second kernel adds them in their order.
@@ -105,7 +107,7 @@ __global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8Nor
     }
     if (!there) continue;
     const double r = t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
-    const float rho = (float)r, along = (float)(r * r * r * (dot * a.share));
+    const float rho = (float)r, along = (float)(r * r * (dot * a.share));
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       float h[VL], g[VL], w[VL], d[VL];
@@ -114,9 +116,10 @@ __global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8Nor
       if (a.w) weight(c, w);
 #pragma unroll
       for (int i = 0; i < VL; ++i) {
-        dw[c][i] = __builtin_fmaf(g[i], h[i] * rho, dw[c][i]);
+        const float n = h[i] * rho;
+        dw[c][i] = __builtin_fmaf(g[i], n, dw[c][i]);
         if (a.w) g[i] *= w[i];
-        d[i] = __builtin_fmaf(-h[i], along, rho * g[i]);
+        d[i] = __builtin_fmaf(-n, along, rho * g[i]);
       }
       if (a.dh) {
         float add[VL];
@@ -178,12 +181,13 @@ __global__ __launch_bounds__(1024) void t8_norm_grad_long_kernel(T8NormGradArgs 
     ss = t8_across_sum(red[turn][0], 16, lane);
     dot = t8_across_sum(red[turn][1], 16, lane);
     const double r = t8_rsqrt(__builtin_fma(ss, a.share, (double)a.eps));
-    const float rho = (float)r, along = (float)(r * r * r * (dot * a.share));
+    const float rho = (float)r, along = (float)(r * r * (dot * a.share));
     for (int e = threadIdx.x; e < a.K; e += 1024) {
       const float v = Mem::get(h[e]), g = Mem::get(dy[e]);
-      float d = __builtin_fmaf(-v, along, rho * (a.w ? g * a.w[e] : g));
+      const float n = v * rho;
+      float d = __builtin_fmaf(-n, along, rho * (a.w ? g * a.w[e] : g));
       if (a.dh) d += Mem::get(dh[e]);
-      if (part) part[e] = __builtin_fmaf(g, v * rho, row == blockIdx.x ? 0.0f : part[e]);
+      if (part) part[e] = __builtin_fmaf(g, n, row == blockIdx.x ? 0.0f : part[e]);
       dx[e] = Mem::put(d);
     }
   }

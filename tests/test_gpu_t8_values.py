@@ -109,3 +109,35 @@ def test_linear_grad_of_small_float32_rows(qc, N):  # noqa: F811
     qc.qc_t8_linear_grad(d, _dev(qw), _dev(ws), dx, work)
     v, aq = _np(d), qw.astype(np.float64)
     _check(dx, O.linear_grad(v, qw, ws), 1.01 * 2.0 ** -32 * v.max(1, keepdims=True) * aq.sum(0) + 4 * E * (v @ aq), "f32", "N %d" % N)
+
+
+def _norm_grad(qc, hn, dyn, w, t):
+    """dx and dweight of qc_t8_norm_grad against the oracle's, by the bounds of test_norm_grad."""
+    import torch
+    M, K = hn.shape
+    h, dy = _dev(hn).to(_type(t)), _dev(dyn).to(_type(t))
+    dx, dw = torch.empty_like(h), torch.empty(K, device="cuda")
+    work = torch.empty(qc.qc_t8_norm_grad_bytes(M, K), dtype=torch.uint8, device="cuda")
+    qc.qc_t8_norm_grad(h, dy, dx, weight=_dev(w), dweight=dw, work=work, eps=EPS)
+    hn, dyn = _np(h), _np(dy)
+    want, dww = O.norm_grad(hn, w, EPS, dyn)
+    r = O.rho(hn, EPS)[:, None]
+    g = np.abs(dyn * w)
+    along = r ** 3 * np.abs(hn) / K
+    gh = dyn * w * hn
+    _check(dx, want, E * (4 * r * g + along * 8 * np.abs(gh.sum(1, keepdims=True)) + along * 33 * np.abs(gh).sum(1, keepdims=True)), t, "dx")
+    _check(dw, dww, (M + 8) * E * (np.abs(dyn * hn) * r).sum(0), "f32", "dweight")
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K", [(9, 5), (9, 64), (300, 1153), (9, 4608), (5, 9001), (3, 20000)])
+def test_norm_grad_of_large_rows(qc, M, K, t):  # noqa: F811
+    """Rows of 1e15 to 1e32, gradients along them (what is left is a hundredth of the two terms) and across them: rho^3 mean(g h) is below any float32 there,
+    its product with h is not."""
+    rng = np.random.default_rng(M + K)
+    u = rng.standard_normal((M, K))
+    size = 10.0 ** np.linspace(15, 32, M)[:, None]
+    u /= np.abs(u).max(1, keepdims=True)
+    dy = u + 0.01 * rng.standard_normal((M, K))
+    dy[::3] = rng.standard_normal(dy[::3].shape)
+    _norm_grad(qc, u * size, dy * 1e3, (1 + 0.2 * rng.standard_normal(K)).astype(np.float32), t)
