@@ -74,8 +74,7 @@ __global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8Nor
       for (int c = 0; c < C; ++c) cd[c] = t8_raw<TYPE>((const T *)a.dh + row * a.lddh, e0 + c * step, K);
     }
     if (AHEAD && row + ahead < a.M) fetch(row + ahead, K);
-    double ss = 0.0;
-    float gh = 0.0f;
+    double ss = 0.0, dot = 0.0;                             // (float64: products of two float32 numbers pass its range)
     if (there) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -90,12 +89,12 @@ __global__ __launch_bounds__(512, C <= 2 ? 4 : 2) void t8_norm_grad_kernel(T8Nor
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
           ss = __builtin_fma((double)h[i], (double)h[i], ss);
-          gh = __builtin_fmaf(g[i], h[i], gh);
+          dot = __builtin_fma((double)g[i], (double)h[i], dot);
         }
       }
     }
     ss = wave_sum_dpp(ss);
-    double dot = wave_sum_dpp((double)gh);
+    dot = wave_sum_dpp(dot);
     if (waves > 1) {
       if (lane == 0) {
         red[turn][0][wave] = ss;

@@ -141,3 +141,12 @@ def test_norm_grad_of_large_rows(qc, M, K, t):  # noqa: F811
     dy = u + 0.01 * rng.standard_normal((M, K))
     dy[::3] = rng.standard_normal(dy[::3].shape)
     _norm_grad(qc, u * size, dy * 1e3, (1 + 0.2 * rng.standard_normal(K)).astype(np.float32), t)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K", [(9, 5), (9, 64), (300, 1153), (9, 4608), (5, 9001), (3, 20000)])
+def test_norm_grad_of_large_rows_and_gradients(qc, M, K, t):  # noqa: F811
+    """Products g h beyond float32, their sums of either size: results that are ordinary numbers."""
+    rng = np.random.default_rng(M + 2 * K)
+    h, dy = rng.standard_normal((M, K)), rng.standard_normal((M, K))
+    _norm_grad(qc, h * 10.0 ** np.linspace(18, 36, M)[:, None], dy * 10.0 ** np.linspace(28, 20, M)[:, None], (1 + 0.2 * rng.standard_normal(K)).astype(np.float32), t)
