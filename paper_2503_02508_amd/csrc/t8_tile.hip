@@ -494,7 +494,7 @@ static hipError_t tile_launch(T8Product a, hipStream_t st) {
 // 4608: 129 us; 192 x 256 by eight 157, and at 2048 x 8192 from 8192 366 / 373), where they are few 96 x 128, two workgroups (1000 x 1152 from 4608: 31 us, 192 x 128 34),
 // and where those are fewer than compute units one with three slabs on their way (128 x 8192 from 8192: 42 us, two 47).  Four need four: the first two.
 // us of a slab and of a tile's ends, by how much of the chip is taken (measured at 16384 x 4608 x 128 - 4608, 16384 x 1152 x 4608 and 4096 x 8192 x 8192,
-// and for LONE and HALF at those above; three planes: all slots and half of them, 1152 and 4608 deep):
+// and for LONE and HALF at those above; three planes: all slots and half of them, 1152 and 4608 deep, of LONE, which has 257 - 512 tiles, between 288 and 512):
 struct TileCost {
   int rows, cols, slots;                                   // 0 rows: there is no such form
   float slab, ends, slab_rest, ends_rest;                  // all slots taken; half of them or fewer
@@ -506,7 +506,7 @@ struct TileCosts {
 };
 constexpr TileCost LARGE_COST = {256, 256, 256, 1.72f, 4.4f, 1.3f, 4.0f}, SMALL_COST = {128, 128, 512, 0.93f, 3.2f, 0.68f, 4.5f};
 constexpr TileCosts FORWARD = {{LARGE_COST, SMALL_COST, {128, 128, 256, 0.61f, 4.8f, 0.56f, 4.8f}, {64, 128, 256, 0.45f, 4.2f, 0.44f, 4.2f}}, 0},
-                    THREE = {{{}, {192, 128, 512, 1.40f, 5.7f, 0.83f, 5.0f}, {96, 128, 512, 0.87f, 4.0f, 0.60f, 3.9f}, {96, 128, 256, 0.58f, 3.8f, 0.57f, 3.4f}}, LONE},
+                    THREE = {{{}, {192, 128, 512, 1.40f, 5.7f, 0.83f, 5.0f}, {96, 128, 512, 0.82f, 3.7f, 0.60f, 3.9f}, {96, 128, 256, 0.58f, 3.8f, 0.57f, 3.4f}}, LONE},
                     FOUR = {{LARGE_COST, SMALL_COST, {}, {}}, SMALL};
 constexpr const TileCosts &tile_costs(int planes) { return planes == 0 ? FORWARD : planes == 3 ? THREE : FOUR; }
 
@@ -588,8 +588,8 @@ static GradPlan grad_plan(int M, int N, int K, int type) {
     int split = (int)std::min<int64_t>(part.slots / left, std::max(1, slabs / 2));
     const int per = (slabs + split - 1) / split;
     split = (slabs + per - 1) / per;
-    // a launch more, or two, and the sums' way to memory and back (kernels of 64 x 4096 from 14336 bfloat16 in 16 parts, 34 MB: 17.2 and 7.4 us; 100 x 1152 from
-    // 8192 float32 in 13, 25 MB: 13.7 and 6.5; 15 x 2640 from 8838 in 24, 8 MB: 11.4 and 4.0; the last tiles of 8192 x 1152 from 4608 no sooner than whole)
+    // a launch more, or two, and the sums' way to memory and back (kernels of 64 x 4096 from 14336 bfloat16 in 8 parts, 25 MB: 23.8 and 5.0 us; 100 x 1152 from
+    // 8192 float32 in 13, 25 MB: 14.0 and 6.5; 15 x 2640 from 8838 bfloat16 in 24, 25 MB with what lies beyond row 15: 12.1 and 4.4)
     const float t = tile_time(c, whole, K, slabs) + part.slab * per + part.ends + 7.0f + (float)split * (float)rest * (float)K * 4.0f / 3.1e6f;
     if (split > 1 && t < time) {
       time = t;
