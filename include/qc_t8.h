@@ -85,7 +85,8 @@ int qc_t8_expand(const int8_t *q, int64_t ldq, const float *scale, int M, int K,
                  void *stream);
 
 /* Gradient of v = act(gate) x, from dv (rounding to codes passed through):
- *   dx = dv act(gate),  dgate = dv x act'(gate)
+ *   dx = dv act(gate),  dgate = (dv x) act'(gate)
+ * (dv x is a float32 product; where it is beyond float32 so is dgate, or NaN.)
  * All dev [M, K] of `type`; dx and dgate may each be x, gate or dv itself, but not each other. */
 int qc_t8_gated_grad(const void *x, int64_t ldx, const void *gate, int64_t ldg, int act, const void *dv, int64_t lddv, int type,
                      int M, int K, void *dx, int64_t lddx, void *dgate, int64_t lddg, void *stream);

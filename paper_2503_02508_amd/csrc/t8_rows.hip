@@ -3,9 +3,9 @@
 // All of them move bytes: a row is read once, held in registers as float32 while its largest value is found, and written.  One wavefront
 // takes a row of up to 256 vectors of 16 bytes, a workgroup of 2 - 16 wavefronts a longer one (or a short one where there are few rows:
 // then nothing but latency counts), and rows beyond 16 wavefronts' registers are read again for each of the steps.
-// Kernels alone: codes of 16384 x 4608 bfloat16 37.3 us, 6.1 TB/s; of its gated rows 73.6 us, 5.1 TB/s (the instructions take 60 of them); the norm of
-// 16384 x 1152 bfloat16 with its residual 26.8 us, 4.9 TB/s; planes of 8192 x 4608 bfloat16 29.8 us, 5.1 TB/s; codes read back, 16384 x 4608 to
-// bfloat16, 36 us, 6.3 TB/s.  One row of 8192 takes 3.6 us, 77 of 4608 float32 3.4: a read, two reductions, a write.
+// Kernels alone: codes of 16384 x 4608 bfloat16 37.3 us, 6.1 TB/s; of its gated rows 70.9 us, 5.3 TB/s (the instructions take 60 of them); the norm of
+// 16384 x 1152 bfloat16 with its residual 27.1 us, 4.9 TB/s; planes of 8192 x 4608 bfloat16 37.4 us, 5.1 TB/s; codes read back, 16384 x 4608 to
+// bfloat16, 36 us, 6.3 TB/s.  One row of 8192 takes 3.6 us, 77 of 4608 float32 3.3: a read, two reductions, a write.
 //
 // Exact decisions.  The codes are those of the definition: float32 quotients, rounded half to even.  Each is formed as v (1 / scale), which is off by
 // at most 1.2e-5 for quotients of up to 127, and where it is nearer than 2e-5 to a border the division decides.  The gated product is
@@ -265,7 +265,8 @@ __global__ __launch_bounds__(FULL ? 1024 : 256) void t8_rows_kernel(T8RowArgs a)
   }
 }
 
-// Rows of any length, read again for each step; element after element.
+// Rows of any length, read again for each step; element after element, the gate in float64 twice: codes of 256 x 53248 bfloat16 35 us a call, of gated
+// ones 70, where the bytes would take 8 and 14.
 template <int TYPE, int SOURCE>
 __global__ __launch_bounds__(1024) void t8_long_rows_kernel(T8RowArgs a) {
   using T = typename W4Mem<TYPE>::T;
@@ -428,8 +429,8 @@ hipError_t launch_t8_expand(const int8_t *q, int64_t ldq, const float *scale, in
 }
 
 // Every element is read before any of the same thread's results is written, so that results may take their inputs' place.
-// Bytes bound it, and not far below them the instructions: 4096 x 4608 float16, GELU, 32.7 us, 5.8 TB/s; 35.3 with two vectors a thread, 37.8 with
-// what far gates need in every element's way.
+// Bytes bound it, and not far below them the instructions: 4096 x 4608 float16, GELU, 33.3 us a call among others, 5.7 TB/s (35.3 alone under a profiler).  When it
+// was measured beside them, 32.7 against 35.3 with two vectors a thread and 37.8 with what far gates need in every element's way.
 template <int TYPE, int ACT>
 __global__ __launch_bounds__(256) void t8_gated_grad_kernel(const void *x, int64_t ldx, const void *g, int64_t ldg, const void *dv, int64_t lddv, int64_t M,
                                                             int K, void *dx, int64_t lddx, void *dg, int64_t lddg, int rows, int vectors) {

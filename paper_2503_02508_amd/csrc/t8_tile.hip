@@ -490,11 +490,13 @@ static hipError_t tile_launch(T8Product a, hipStream_t st) {
 // workgroup while it waits for memory, 128 x 128 by eight with three slabs on their way (2048 x 1152 x 4608: 24.5 us, by four with two 26.7; 512 x 8192 x 8192
 // 43.6 / 59; with more tiles than compute units it loses: 4096 x 4608 x 1152 33.7 / 28.2), and where there is none of half the size either, 64 x 128 by four
 // with three (1000 x 1152 x 1152 8.1, 256 x 8192 x 4096 18.2; 128 x 128 10.0 / 11.4, 22.4 / 24.0).
-// Three planes of a row need three row blocks, so that tiles have 192 or 96 rows of planes: 192 x 128 by four, two workgroups a compute unit (8192 x 1152 from
-// 4608: 129 us; 192 x 256 by eight 157, and at 2048 x 8192 from 8192 366 / 373), where they are few 96 x 128, two workgroups (1000 x 1152 from 4608: 31 us, 192 x 128 34),
-// and where those are fewer than compute units one with three slabs on their way (128 x 8192 from 8192: 42 us, two 47).  Four need four: the first two.
+// Three planes of a row need three row blocks, so that tiles have 192 or 96 rows of planes: 192 x 128 by four, two workgroups a compute unit (8192 x 1152
+// from 4608: 129 us; 192 x 256 by eight 157, and at 2048 x 8192 from 8192 366 / 373), where they are few 96 x 128, two workgroups (1000 x 1152 from 4608:
+// 31 us, 192 x 128 34), and where those are fewer than compute units one with three slabs on their way (128 x 8192 from 8192: 42 us, two 47).  Four need
+// four: the first two.
 // us of a slab and of a tile's ends, by how much of the chip is taken (measured at 16384 x 4608 x 128 - 4608, 16384 x 1152 x 4608 and 4096 x 8192 x 8192,
-// and for LONE and HALF at those above; three planes: all slots and half of them, 1152 and 4608 deep, of LONE, which has 257 - 512 tiles, between 288 and 512):
+// and for LONE and HALF at those above; three planes: all slots and half of them, 1152 and 4608 deep, of LONE, which has 257 - 512 tiles, between 288 and
+// 512):
 struct TileCost {
   int rows, cols, slots;                                   // 0 rows: there is no such form
   float slab, ends, slab_rest, ends_rest;                  // all slots taken; half of them or fewer
